@@ -210,6 +210,109 @@ fq_status flatquant_mxfp4_gemm(const uint8_t* x_codes, const uint8_t* x_scales, 
                                int64_t T, int m, int n, void* out, int64_t out_stride, void* stream);
 
 /*
+ * The paged key/value cache (Sec. 3.2 "Self-Attention", Sec. 4.1: keys and values as b-bit codes, one step and one zero point per
+ * (token, head) group of 128 channels) of one layer, and the batch of sequences that a call works on.  Both are HOST structs that
+ * hold device pointers; a program makes them once and passes their addresses.
+ *
+ * Pages: a page holds the keys and values of page_tokens consecutive tokens of one sequence, head by head:
+ *   k_codes   u8  [pages, H, page_tokens, 128 * k_bits / 8], rows as flatquant_kv_transform_quant_bits writes them; 16-byte aligned
+ *   k_params  u32 [pages, H, page_tokens]: the fp16 step in the low half, the zero point (0 .. 2^k_bits - 1) in the high half; 16-byte aligned
+ *   v_codes, v_params  the same with v_bits.
+ * A value is step * (code - zero point).  k_bits, v_bits in {2, 3, 4}; page_tokens a power of two, 16 .. 1024; 1 <= H <= 65535.
+ */
+typedef struct fq_kv_cache {
+    uint8_t* k_codes;
+    uint32_t* k_params;
+    uint8_t* v_codes;
+    uint32_t* v_params;
+    int64_t pages;
+    int32_t page_tokens;
+    int32_t H;
+    int32_t k_bits;
+    int32_t v_bits;
+} fq_kv_cache;
+
+/*
+ * The batch: B sequences, and rows of which the last ones of every sequence are the call's (its new tokens).
+ *   row_starts  i32 [B + 1]: sequence b has rows row_starts[b] .. row_starts[b + 1] - 1 of the call's row tensors (n_b of them, none is
+ *               fine); ascending.  Rows from row_starts[B] on (padding) are neither read nor written.
+ *   lengths     i32 [B]: tokens of the sequence with the new ones.  Row i of sequence b is the token at position lengths[b] - n_b + i;
+ *               a row whose position is negative is no token.
+ *   page_table  i32 [B, table_width], rows table_stride apart: the page of tokens page_tokens * j .. of the sequence.  A number outside
+ *               [0, pages) is no page, and neither is what lies behind table_width: such tokens are not written, read as zeros and are
+ *               not visible to attention.  Pages that two sequences share are only read.
+ *   T           rows of the row tensors; row_starts is taken as if cut to 0 .. T.
+ *   max_rows, max_length  upper bounds of n_b and lengths[b] as the host knows them: they choose the launch and say how much
+ *               work there is; results do not depend on them.
+ * The arrays are read on the stream, so one captured graph serves lengths and pages as they change.
+ */
+typedef struct fq_kv_batch {
+    const int32_t* row_starts;
+    const int32_t* lengths;
+    const int32_t* page_table;
+    int64_t B;
+    int64_t T;
+    int64_t table_width;
+    int64_t table_stride;
+    int64_t max_rows;
+    int64_t max_length;
+} fq_kv_batch;
+
+/*
+ * Writes the batch's rows into their pages, quantized: per (row, head) group, with 2^b - 1 intervals as in
+ * flatquant_kv_transform_quant_bits and y = k (or k P_k),
+ *     mx = clip * max(max y, 0),  mn = clip * min(min y, 0),  s = fp16( (mx - mn) / (2^b - 1) ),
+ *     z = clamp( round_half_even( -mn / s ), 0, 2^b - 1 ),  q[d] = clamp( round_half_even( y[d] / s ) + z, 0, 2^b - 1 );
+ * a step of zero stores zero codes and z = 0.  Without a matrix (P_k or P_v NULL: values whose transform sits in the weights, keys that
+ * flatquant_head_transform has been over) every operation is a correctly rounded fp32 one, in this order: the codes are those of the
+ * formulas, ties included.  With one they are the bits of flatquant_kv_transform_quant_bits on the same rows.
+ *   k, v   fp16 [T, H, 128], row t at k + t * k_stride halves; 16-byte aligned, strides multiples of 8 and >= 128 H.  Either may be NULL:
+ *          that half of the cache is left as it is.
+ *   P_k, P_v  fp16 [Hp, 128, 128] or NULL; Hp == 1 or H, for both.
+ *   k_clip, v_clip > 0.
+ * No two of the batch's tokens may share a place in the pages (sequences write into pages of their own).
+ */
+fq_status flatquant_cache_write(const fq_kv_cache* cache, const fq_kv_batch* batch, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                                const void* P_k, const void* P_v, int Hp, float k_clip, float v_clip, void* stream);
+
+/*
+ * Reads the batch's rows (the last n_b tokens of every sequence) back: k[t, h, d] = fp16( step * (code - zero point) ), v the same.
+ * Row tensors as above, either NULL.  The tokens' pages are only read.
+ */
+fq_status flatquant_cache_read(const fq_kv_cache* cache, const fq_kv_batch* batch, void* k, int64_t k_stride, void* v, int64_t v_stride, void* stream);
+
+/*
+ * Attention of the batch's rows over their sequences' cached tokens, the rows' own among them (write them first):
+ *     out[t, h, :] = sum_j w_j v_j,   w = softmax over the visible tokens j of ( scale * q[t, h, :] . k_j ),
+ * k_j and v_j the de-quantized rows of key/value head h / (Hq / H).  A row at position p sees token j of its sequence if j <= p and, with a
+ * window (window > 0), j > p - window or j < sinks: the last `window` tokens and the first `sinks`.  window == 0 is no window, and sinks
+ * is then not looked at.  A row that sees nothing gets zeros.  Pages whose tokens no row sees are not touched.
+ * Scores, maxima and sums are fp32; the weights (times the value's step) are rounded to fp16 for the matrix instructions.
+ *   q, out  fp16 [T, Hq, 128], rows q_stride / out_stride halves apart (multiples of 8, >= 128 Hq), 16-byte aligned, not overlapping.
+ *   Hq      a multiple of H.
+ *   workspace  fq_cache_attention_workspace(cache, batch, Hq) bytes, 16-byte aligned (NULL if that is 0): partial results of a long
+ *           axis that several workgroups share.  Its contents mean nothing between calls; calls that may run at the same time need
+ *           one each.
+ */
+fq_status flatquant_cache_attention(const fq_kv_cache* cache, const fq_kv_batch* batch, const void* q, int64_t q_stride, int Hq, float scale,
+                                    int window, int sinks, void* out, int64_t out_stride, void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * The same while a tree of drafted tokens is verified: the rows of a sequence are its drafted tokens, at most 64, in any order; row i
+ * sees every token before them (positions < lengths[b] - n_b) and drafted token j (position lengths[b] - n_b + j) if bit j of
+ * visible[t] is set (its own bit among them, if it is to see itself).
+ *   visible  u64 [T], 8-byte aligned.
+ * max_rows above 64 is FQ_UNSUPPORTED_SHAPE; if a sequence has more rows all the same, nobody sees its drafted tokens behind the 64th.
+ */
+fq_status flatquant_cache_tree_attention(const fq_kv_cache* cache, const fq_kv_batch* batch, const void* q, int64_t q_stride, int Hq, float scale,
+                                         const uint64_t* visible, void* out, int64_t out_stride, void* workspace, int64_t workspace_bytes,
+                                         void* stream);
+
+/* Workspace of the two attention calls for this cache and batch, from the host's figures alone (B, T, H, Hq, max_rows, max_length); 0 if they
+ * need none, -1 for arguments they refuse. */
+int64_t fq_cache_attention_workspace(const fq_kv_cache* cache, const fq_kv_batch* batch, int Hq);
+
+/*
  * De-quantization check helper (Sec. 2.1: W^ = s * Pi(W / s)).
  *   zeros == NULL : out[r, c] = s[r] * q[r, c]            (signed nibbles)
  *   zeros != NULL : out[r, c] = s[r] * (q[r, c] - z[r])   (unsigned nibbles)

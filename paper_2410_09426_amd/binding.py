@@ -29,6 +29,7 @@ EXPORTS = (
     "flatquant_weight_transform_quant", "fq_inverse_transpose", "flatquant_head_transform", "flatquant_w4a4_gemm",
     "fq_supported", "fq_choose_factors", "fq_default_design_fits", "fq_lds_bytes",
     "fq_status_string", "fq_last_hip_error", "fq_abi_version", "fq_set_tuning",
+    "flatquant_cache_write", "flatquant_cache_read", "flatquant_cache_attention", "flatquant_cache_tree_attention", "fq_cache_attention_workspace",
 )
 
 # parameters of the launching entry points without the stream, and their C types: pointer, int, long (int64_t), float
@@ -46,6 +47,15 @@ _NATIVE_PARAMS = {
     "flatquant_head_transform": ("x P Hp T H D out", "ppiliip"),
 }
 NATIVE = tuple(_NATIVE_PARAMS)
+
+# the paged key/value cache: `cache` is a KvCache, `batch` a KvBatch
+_CACHE_PARAMS = {
+    "flatquant_cache_write": ("cache batch k k_stride v v_stride P_k P_v Hp k_clip v_clip", "ppplplppiff"),
+    "flatquant_cache_read": ("cache batch k k_stride v v_stride", "ppplpl"),
+    "flatquant_cache_attention": ("cache batch q q_stride Hq scale window sinks out out_stride workspace workspace_bytes", "ppplifiiplpl"),
+    "flatquant_cache_tree_attention": ("cache batch q q_stride Hq scale visible out out_stride workspace workspace_bytes", "ppplifpplpl"),
+}
+CACHE_CALLS = tuple(_CACHE_PARAMS)
 
 _lib = None
 _fqcall = None
@@ -67,9 +77,11 @@ def lib() -> ctypes.CDLL:
                 "(there is no CPU fallback for the FlatQuant kernels)")
         L = ctypes.CDLL(LIB_PATH)
         vp, i32, i64, f32 = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_float
-        for name, (params, types) in _NATIVE_PARAMS.items():
+        for name, (params, types) in {**_NATIVE_PARAMS, **_CACHE_PARAMS}.items():
             getattr(L, name).argtypes = [{"p": vp, "i": i32, "l": i64, "f": f32}[t] for t in types] + [vp]
             getattr(L, name).restype = i32
+        L.fq_cache_attention_workspace.argtypes = [vp, vp, i32]
+        L.fq_cache_attention_workspace.restype = i64
         L.fq_mxfp4_tiled_scale_bytes.argtypes = [i64, i64]
         L.fq_mxfp4_tiled_scale_bytes.restype = i64
         L.flatquant_dequant_mxfp4.argtypes = [vp, vp, i64, i32, vp, vp]
@@ -122,7 +134,7 @@ def _stream(stream) -> Optional[int]:
 
 def _ctypes_call(name: str):
     """A launching entry point through ctypes, written out from its parameters."""
-    params, types = _NATIVE_PARAMS[name]
+    params, types = (_NATIVE_PARAMS.get(name) or _CACHE_PARAMS[name])
     convert = {"p": "_ptr", "i": "int", "l": "int", "f": "float"}
     values = ", ".join(f"{convert[t]}({p})" for p, t in zip(params.split(), types))
     scope = {}
@@ -142,6 +154,55 @@ except ModuleNotFoundError:                     # not built, or built for anothe
 else:
     _fqcall.connect(lib, FlatQuantError)
     globals().update((n, getattr(_fqcall, n)) for n in NATIVE)
+
+
+globals().update((n, _ctypes_call(n)) for n in CACHE_CALLS)
+
+
+class _HostStruct:
+    """A host struct of the C interface whose address the calls take; keeps what its pointers point to."""
+
+    def __init__(self, **values):
+        self._kept = tuple(values.values())
+        self._struct = self._Fields(**{n: _ptr(values[n]) if t is ctypes.c_void_p else int(values[n]) for n, t in self._Fields._fields_})
+        self._address = ctypes.addressof(self._struct)
+
+    def data_ptr(self) -> int:
+        return self._address
+
+
+class KvCache(_HostStruct):
+    """fq_kv_cache: the pages of one layer's keys and values (tensors or device addresses)."""
+
+    class _Fields(ctypes.Structure):
+        _fields_ = [("k_codes", ctypes.c_void_p), ("k_params", ctypes.c_void_p), ("v_codes", ctypes.c_void_p), ("v_params", ctypes.c_void_p),
+                    ("pages", ctypes.c_int64), ("page_tokens", ctypes.c_int32), ("H", ctypes.c_int32), ("k_bits", ctypes.c_int32),
+                    ("v_bits", ctypes.c_int32)]
+
+    def __init__(self, k_codes, k_params, v_codes, v_params, pages: int, page_tokens: int, H: int, k_bits: int, v_bits: int):
+        super().__init__(k_codes=k_codes, k_params=k_params, v_codes=v_codes, v_params=v_params, pages=pages, page_tokens=page_tokens, H=H,
+                         k_bits=k_bits, v_bits=v_bits)
+
+
+class KvBatch(_HostStruct):
+    """fq_kv_batch: the sequences and rows of a call (tensors or device addresses, and what the host knows of them)."""
+
+    class _Fields(ctypes.Structure):
+        _fields_ = [("row_starts", ctypes.c_void_p), ("lengths", ctypes.c_void_p), ("page_table", ctypes.c_void_p), ("B", ctypes.c_int64),
+                    ("T", ctypes.c_int64), ("table_width", ctypes.c_int64), ("table_stride", ctypes.c_int64), ("max_rows", ctypes.c_int64),
+                    ("max_length", ctypes.c_int64)]
+
+    def __init__(self, row_starts, lengths, page_table, B: int, T: int, table_width: int, table_stride: int, max_rows: int, max_length: int):
+        super().__init__(row_starts=row_starts, lengths=lengths, page_table=page_table, B=B, T=T, table_width=table_width,
+                         table_stride=table_stride, max_rows=max_rows, max_length=max_length)
+
+
+def fq_cache_attention_workspace(cache, batch, Hq: int) -> int:
+    """Bytes of workspace of the attention calls; raises for arguments that they refuse."""
+    n = int(lib().fq_cache_attention_workspace(_ptr(cache), _ptr(batch), int(Hq)))
+    if n < 0:
+        raise FlatQuantError(FQ_INVALID_ARG, "fq_cache_attention_workspace")
+    return n
 
 
 def status_string(status: int) -> str:

@@ -262,6 +262,144 @@ fq_status flatquant_mxfp4_gemm(const uint8_t* x_codes, const uint8_t* x_scales, 
     return fq::finish(fq::mxfp4_gemm_launch(a, static_cast<hipStream_t>(stream)));
 }
 
+// The checks that every call on a paged cache shares, and the kernels' view of it.  FQ_OK with *empty set: nothing to do.
+static fq_status cache_args(const fq_kv_cache* cache, const fq_kv_batch* batch, fq::CacheDev& d, bool& empty) {
+    empty = false;
+    if (!cache || !batch) return FQ_INVALID_ARG;
+    if (cache->pages < 1 || cache->H < 1 || cache->page_tokens < 1) return FQ_INVALID_ARG;
+    if (cache->k_bits < 2 || cache->k_bits > 4 || cache->v_bits < 2 || cache->v_bits > 4) return FQ_INVALID_ARG;
+    if (batch->B < 0 || batch->T < 0 || batch->table_width < 0 || batch->table_stride < batch->table_width || batch->max_rows < 0 || batch->max_length < 0)
+        return FQ_INVALID_ARG;
+    const int page = cache->page_tokens;
+    if (page < 16 || page > 1024 || (page & (page - 1)) || cache->H > 65535 || cache->pages > 0x7fffffffLL) return FQ_UNSUPPORTED_SHAPE;
+    if (batch->T > (1LL << 29) || batch->B > 0xffffff / cache->H || batch->table_width > 0x7fffffffLL) return FQ_UNSUPPORTED_SHAPE;   // grid and index limits
+    if (cache->pages > (1LL << 48) / cache->H / page) return FQ_UNSUPPORTED_SHAPE;
+    if (batch->T == 0 || batch->B == 0) {
+        empty = true;
+        return FQ_OK;
+    }
+    if (!cache->k_codes || !cache->k_params || !cache->v_codes || !cache->v_params) return FQ_INVALID_ARG;
+    if (!batch->row_starts || !batch->lengths || (!batch->page_table && batch->table_width > 0)) return FQ_INVALID_ARG;
+    auto bad = [](const void* p, int a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; };
+    if (bad(cache->k_codes, 16) || bad(cache->v_codes, 16) || bad(cache->k_params, 16) || bad(cache->v_params, 16) || bad(batch->row_starts, 4) ||
+        bad(batch->lengths, 4) || bad(batch->page_table, 4))
+        return FQ_MISALIGNED;
+    d.codes[0] = cache->k_codes; d.codes[1] = cache->v_codes;
+    d.params[0] = cache->k_params; d.params[1] = cache->v_params;
+    d.row_starts = batch->row_starts; d.lengths = batch->lengths; d.page_table = batch->page_table;
+    d.table_stride = batch->table_stride; d.T = batch->T;
+    d.B = (int)batch->B; d.pages = (int)cache->pages; d.table_width = (int)batch->table_width; d.H = cache->H;
+    d.page_shift = __builtin_ctz((unsigned)page);
+    d.bits[0] = cache->k_bits; d.bits[1] = cache->v_bits;
+    return FQ_OK;
+}
+// Whether `n` bytes at p meet one of the cache's four arrays, or the batch's
+static bool in_cache(const fq_kv_cache* c, const fq_kv_batch* b, const void* p, int64_t n) {
+    const int64_t groups = c->pages * c->H * c->page_tokens;
+    return fq::overlap(p, n, c->k_codes, groups * 16 * c->k_bits) || fq::overlap(p, n, c->v_codes, groups * 16 * c->v_bits) ||
+           fq::overlap(p, n, c->k_params, groups * 4) || fq::overlap(p, n, c->v_params, groups * 4) ||
+           fq::overlap(p, n, b->row_starts, (b->B + 1) * 4) || fq::overlap(p, n, b->lengths, b->B * 4) ||
+           (b->table_width > 0 && fq::overlap(p, n, b->page_table, ((b->B - 1) * b->table_stride + b->table_width) * 4));
+}
+// Row tensors of a write or a read
+static fq_status cache_rows(const fq_kv_cache* cache, const fq_kv_batch* batch, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                            fq::CacheRows& r) {
+    const void* x[2] = {k, v};
+    const int64_t stride[2] = {k_stride, v_stride}, row = 128LL * cache->H;
+    for (int i = 0; i < 2; ++i) {
+        r.rows[i] = const_cast<void*>(x[i]);
+        r.stride[i] = stride[i];
+        if (!x[i]) continue;
+        if (stride[i] < row) return FQ_INVALID_ARG;
+        if ((reinterpret_cast<uintptr_t>(x[i]) & 15) || (stride[i] & 7)) return FQ_MISALIGNED;
+        if (stride[i] > (1LL << 40)) return FQ_UNSUPPORTED_SHAPE;
+        if (in_cache(cache, batch, x[i], ((batch->T - 1) * stride[i] + row) * 2)) return FQ_INVALID_ARG;
+    }
+    return FQ_OK;
+}
+
+fq_status flatquant_cache_write(const fq_kv_cache* cache, const fq_kv_batch* batch, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                                const void* P_k, const void* P_v, int Hp, float k_clip, float v_clip, void* stream) {
+    fq::CacheDev d;
+    fq::CacheRows r;
+    bool empty;
+    fq_status st = cache_args(cache, batch, d, empty);
+    if (st != FQ_OK) return st;
+    if (!(k_clip > 0.0f) || !(v_clip > 0.0f) || (Hp != 1 && Hp != cache->H)) return FQ_INVALID_ARG;
+    if (empty || (!k && !v)) return FQ_OK;
+    st = cache_rows(cache, batch, k, k_stride, v, v_stride, r);
+    if (st != FQ_OK) return st;
+    if ((reinterpret_cast<uintptr_t>(P_k) & 15) || (reinterpret_cast<uintptr_t>(P_v) & 15)) return FQ_MISALIGNED;
+    if (P_k || P_v) return FQ_UNSUPPORTED_SHAPE;
+    r.P[0] = static_cast<const _Float16*>(P_k); r.P[1] = static_cast<const _Float16*>(P_v);
+    r.Hp = Hp; r.clip[0] = k_clip; r.clip[1] = v_clip;
+    return fq::finish(fq::cache_write_launch(d, r, static_cast<hipStream_t>(stream)));
+}
+
+fq_status flatquant_cache_read(const fq_kv_cache* cache, const fq_kv_batch* batch, void* k, int64_t k_stride, void* v, int64_t v_stride, void* stream) {
+    fq::CacheDev d;
+    fq::CacheRows r;
+    bool empty;
+    fq_status st = cache_args(cache, batch, d, empty);
+    if (st != FQ_OK) return st;
+    if (empty || (!k && !v)) return FQ_OK;
+    st = cache_rows(cache, batch, k, k_stride, v, v_stride, r);
+    if (st != FQ_OK) return st;
+    const int64_t row = 128LL * cache->H;
+    if (k && v && fq::overlap(k, ((batch->T - 1) * k_stride + row) * 2, v, ((batch->T - 1) * v_stride + row) * 2)) return FQ_INVALID_ARG;
+    return fq::finish(fq::cache_read_launch(d, r, static_cast<hipStream_t>(stream)));
+}
+
+static fq_status cache_attention(const fq_kv_cache* cache, const fq_kv_batch* batch, const void* q, int64_t q_stride, int Hq, float scale,
+                                 int window, int sinks, const uint64_t* visible, bool tree, void* out, int64_t out_stride, void* workspace,
+                                 int64_t workspace_bytes, void* stream) {
+    fq::CacheDev d;
+    bool empty;
+    fq_status st = cache_args(cache, batch, d, empty);
+    if (st != FQ_OK) return st;
+    const int64_t row = 128LL * Hq;
+    if (Hq < 1 || Hq % cache->H != 0 || !std::isfinite(scale) || window < 0 || sinks < 0 || q_stride < row || out_stride < row || workspace_bytes < 0)
+        return FQ_INVALID_ARG;
+    if (Hq > (1 << 24) || batch->T > (1LL << 40) / Hq || q_stride > (1LL << 40) || out_stride > (1LL << 40) || (tree && batch->max_rows > 64)) return FQ_UNSUPPORTED_SHAPE;
+    if (empty) return FQ_OK;
+    if (!q || !out || (tree && !visible)) return FQ_INVALID_ARG;
+    const fq::AttnPlan plan = fq::attention_plan(batch->B, batch->T, cache->H, Hq, batch->max_rows, batch->max_length);
+    if (workspace_bytes < plan.workspace || (plan.workspace > 0 && !workspace)) return FQ_INVALID_ARG;
+    auto bad = [](const void* p, int a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; };
+    if (bad(q, 16) || bad(out, 16) || (q_stride & 7) || (out_stride & 7) || bad(workspace, 16) || bad(visible, 8)) return FQ_MISALIGNED;
+    const int64_t qbytes = ((batch->T - 1) * q_stride + row) * 2, obytes = ((batch->T - 1) * out_stride + row) * 2;
+    if (fq::overlap(q, qbytes, out, obytes) || in_cache(cache, batch, out, obytes) || (tree && fq::overlap(visible, batch->T * 8, out, obytes)))
+        return FQ_INVALID_ARG;
+    if (plan.workspace > 0 && (fq::overlap(workspace, plan.workspace, out, obytes) || fq::overlap(workspace, plan.workspace, q, qbytes) ||
+                               in_cache(cache, batch, workspace, plan.workspace) || (tree && fq::overlap(visible, batch->T * 8, workspace, plan.workspace))))
+        return FQ_INVALID_ARG;
+    fq::AttnArgs a;
+    a.q = static_cast<const _Float16*>(q); a.out = static_cast<_Float16*>(out); a.q_stride = q_stride; a.out_stride = out_stride;
+    a.Hq = Hq; a.scale = scale; a.window = window; a.sinks = sinks; a.visible = visible; a.workspace = static_cast<float*>(workspace);
+    a.max_rows = batch->max_rows; a.max_length = batch->max_length;
+    return fq::finish(fq::attention_launch(d, a, plan, static_cast<hipStream_t>(stream)));
+}
+
+fq_status flatquant_cache_attention(const fq_kv_cache* cache, const fq_kv_batch* batch, const void* q, int64_t q_stride, int Hq, float scale,
+                                    int window, int sinks, void* out, int64_t out_stride, void* workspace, int64_t workspace_bytes, void* stream) {
+    return cache_attention(cache, batch, q, q_stride, Hq, scale, window, sinks, nullptr, false, out, out_stride, workspace, workspace_bytes, stream);
+}
+
+fq_status flatquant_cache_tree_attention(const fq_kv_cache* cache, const fq_kv_batch* batch, const void* q, int64_t q_stride, int Hq, float scale,
+                                         const uint64_t* visible, void* out, int64_t out_stride, void* workspace, int64_t workspace_bytes,
+                                         void* stream) {
+    return cache_attention(cache, batch, q, q_stride, Hq, scale, 0, 0, visible, true, out, out_stride, workspace, workspace_bytes, stream);
+}
+
+int64_t fq_cache_attention_workspace(const fq_kv_cache* cache, const fq_kv_batch* batch, int Hq) {
+    if (!cache || !batch || cache->H < 1 || cache->H > 65535 || Hq < 1 || Hq % cache->H != 0 || Hq > (1 << 24)) return -1;
+    if (batch->B < 0 || batch->T < 0 || batch->max_rows < 0 || batch->max_length < 0 || batch->T > (1LL << 29) || batch->T > (1LL << 40) / Hq ||
+        batch->B > 0xffffff / cache->H)
+        return -1;
+    if (batch->B == 0 || batch->T == 0) return 0;
+    return fq::attention_plan(batch->B, batch->T, cache->H, Hq, batch->max_rows, batch->max_length).workspace;
+}
+
 fq_status flatquant_dequant_mxfp4(const uint8_t* codes, const uint8_t* scales, int64_t rows, int n, float* out, void* stream) {
     if (rows < 0 || n < 32 || (n & 31)) return FQ_INVALID_ARG;
     if (rows == 0) return FQ_OK;

@@ -145,6 +145,49 @@ struct KvArgs {
 };
 hipError_t kv_launch(const KvArgs& a, hipStream_t stream);
 
+// The paged key/value cache and a batch on it, as the kernels see them (flatquant.h says what the fields are).
+struct CacheDev {
+    uint8_t* codes[2];        // keys, values
+    uint32_t* params[2];
+    const int32_t* row_starts;
+    const int32_t* lengths;
+    const int32_t* page_table;
+    int64_t table_stride;
+    int64_t T;
+    int32_t B, pages, table_width, H;
+    int32_t page_shift;       // log2 of the tokens of a page
+    int32_t bits[2];
+};
+struct CacheRows {            // row tensors of a write or a read; a null pointer leaves that half out
+    void* rows[2];
+    int64_t stride[2];
+    const _Float16* P[2] = {nullptr, nullptr};
+    int Hp = 1;
+    float clip[2] = {1.0f, 1.0f};
+};
+hipError_t cache_write_launch(const CacheDev& c, const CacheRows& r, hipStream_t stream);
+hipError_t cache_read_launch(const CacheDev& c, const CacheRows& r, hipStream_t stream);
+struct AttnArgs {
+    const _Float16* q;
+    _Float16* out;
+    int64_t q_stride, out_stride;
+    int Hq;
+    float scale;
+    int window, sinks;
+    const uint64_t* visible;  // trees of drafted tokens; null: causal
+    float* workspace;
+    int64_t max_rows, max_length;
+};
+// How an attention launch is cut: column tiles of 16 rows per wave, tokens per split, splits.
+struct AttnPlan {
+    int col_tiles;
+    int chunk;
+    int splits;
+    int64_t workspace;        // bytes
+};
+AttnPlan attention_plan(int64_t B, int64_t T, int H, int Hq, int64_t max_rows, int64_t max_length);
+hipError_t attention_launch(const CacheDev& c, const AttnArgs& a, const AttnPlan& plan, hipStream_t stream);
+
 hipError_t dequant_mxfp4_launch(const uint8_t* codes, const uint8_t* exps, int64_t rows, int n, float* out, hipStream_t stream);
 hipError_t dequant_bits_launch(const uint8_t* codes, const _Float16* scales, const _Float16* zeros,
                                int64_t rows, int n, int bits, float* out, hipStream_t stream);

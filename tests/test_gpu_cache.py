@@ -1,0 +1,150 @@
+"""The paged key/value cache on the GPU: write and read bit by bit against the oracle, attention against fp64 within the bound of its
+arithmetic (oracle.cache_oracle.attention_bound)."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import cache_oracle as co
+from paper_2410_09426_amd import binding as fq
+from cache_util import Batch, check_attention, run_attention
+
+pytestmark = pytest.mark.gpu
+D = 128
+
+
+def _dev(a):
+    return torch.from_numpy(a.view(np.uint16).copy()).view(torch.float16).cuda()
+
+
+def _host(t):
+    return t.cpu().view(torch.int16).numpy().view(np.float16)
+
+
+def _write(c, k, v, k_clip=0.95, v_clip=0.9):
+    """On the device, and on the host by the oracle."""
+    dk, dv = (None if x is None else _dev(x) for x in (k, v))
+    fq.flatquant_cache_write(c.cache(), c.batch(), dk, 0 if k is None else k.shape[1], dv, 0 if v is None else v.shape[1], None, None, 1, k_clip, v_clip,
+                             stream=torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    for b in range(c.B):
+        for i in range(c.rows[b]):
+            t = c.starts[b] + i
+            for x, rows, clip in zip(c.host, (k, v), (k_clip, v_clip)):
+                if rows is not None:
+                    x.write(c.table[b, :c.width], c.lengths[b] - c.rows[b] + i, rows[t, :c.H * D].reshape(c.H, D), clip)
+
+
+def _same_pages(c):
+    for name, x in zip("kv", c.host):
+        assert np.array_equal(c.d[name + "c"].cpu().numpy(), x.codes), f"{name} codes"
+        assert np.array_equal(c.d[name + "p"].cpu().numpy().view(np.uint32), x.params), f"{name} parameters"
+
+
+def _read(c, pad=(0, 0), which="kv"):
+    out = [torch.full((c.T, c.H * D + p), -3.5, dtype=torch.float16, device="cuda") for p in pad]
+    a, b = (o if n in which else None for o, n in zip(out, "kv"))
+    fq.flatquant_cache_read(c.cache(), c.batch(), a, c.H * D + pad[0], b, c.H * D + pad[1], stream=torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    return [_host(o) for o in out]
+
+
+SHAPES = [  # rows, lengths, H, page
+    ((1,), (1,), 1, 16),
+    ((1,), (33,), 3, 16),
+    ((1, 1, 1, 1, 1), (7, 64, 65, 128, 1), 8, 64),
+    ((5, 0, 17, 1, 0), (5, 9, 100, 40, 0), 2, 32),
+    ((300, 1, 77), (300, 300, 513), 5, 128),
+    ((1100,), (1500,), 4, 1024),
+]
+
+
+@pytest.mark.parametrize("k_bits,v_bits", [(4, 4), (3, 2), (2, 3)])
+@pytest.mark.parametrize("rows,lengths,H,page", SHAPES)
+def test_write_and_read_bit_by_bit(rows, lengths, H, page, k_bits, v_bits):
+    print(f"[case] write {rows} of {lengths}, {H} heads, pages of {page}, {k_bits}/{v_bits} bits", flush=True)
+    c = Batch(11 + len(rows), rows, lengths, H, page, k_bits, v_bits, pad=3, filled=False).upload()
+    k, v = c.row_tensor(H, 8), c.row_tensor(H, 0, gain=3.0)
+    k[0, :D] = 0                                             # a group of zeros: step 0
+    if c.T > 2:
+        k[1, :D] = np.float16(6e-8)                          # a step that rounds to zero
+        v[1, :D] = np.arange(D) - 3.0                        # whole numbers
+        k[c.T - 4, -D - 8:-8] = 65504.0                      # one sign only, the largest number
+    _write(c, k, v)
+    _same_pages(c)
+    pk, pv = _read(c, (0, 16))
+    for x, got in zip(c.host, (pk, pv)):
+        for b in range(c.B):
+            n = rows[b]
+            if n:
+                y = x.values(c.table[b, :c.width], np.arange(lengths[b] - n, lengths[b])).transpose(1, 0, 2)
+                with np.errstate(over="ignore"):
+                    assert np.array_equal(got[c.starts[b]:c.starts[b] + n, :H * D].reshape(n, H, D), y.astype(np.float16))
+    assert np.all(pk[c.starts[-1]:] == -3.5) and np.all(pv[c.starts[-1]:] == -3.5) and np.all(pv[:, H * D:] == -3.5)
+
+
+@pytest.mark.parametrize("bits", [2, 3, 4])
+def test_steps_next_to_fp16_midpoints(bits):
+    """Many groups, so that some fp32 steps are fp16 midpoints that the unrounded quotient is not."""
+    rows, H = 1200, 32
+    print(f"[case] write {rows} rows of {H} heads, {bits} bits", flush=True)
+    c = Batch(77, (rows,), (rows,), H, 64, bits, bits, filled=False).upload()
+    k, v = c.row_tensor(H), c.row_tensor(H, gain=7.0)
+    k[0, 0], k[0, 1:D] = -7.6796875, 2.505859375          # 0.95 * 10.185546875 / 7 is one in fp32 and just below it
+    dk, dv = _dev(k), _dev(v)
+    fq.flatquant_cache_write(c.cache(), c.batch(), dk, H * D, dv, H * D, None, None, 1, 0.95, 0.95, stream=torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    pos = np.arange(rows)
+    for name, y in zip("kv", (k, v)):
+        q, s, z = co.grid32(y.reshape(rows, H, D), 0.95, bits)
+        at = (c.table[0, pos // 64], slice(None), pos % 64)
+        assert np.array_equal(c.d[name + "p"].cpu().numpy().view(np.uint32)[at], co.parameters(s, z))
+        assert np.array_equal(c.d[name + "c"].cpu().numpy()[at], co.pack(q, bits))
+
+
+ATTEND = [  # rows, lengths, H, G, page, bits, window, sinks
+    ((1,), (1,), 1, 1, 16, (4, 4), 0, 0),
+    ((1,), (31,), 2, 1, 16, (4, 4), 0, 0),
+    ((1,), (32,), 1, 4, 32, (4, 4), 0, 0),
+    ((1,), (33,), 1, 8, 16, (3, 3), 0, 0),
+    ((1, 1, 1), (129, 1, 700), 2, 4, 64, (4, 4), 0, 0),
+    ((1, 1), (1500, 1027), 1, 5, 16, (2, 4), 0, 0),
+    ((1, 1), (1500, 40), 3, 16, 128, (4, 2), 0, 0),
+    ((1, 0, 1), (1000, 300, 900), 2, 7, 16, (3, 4), 100, 0),
+    ((1, 1), (1000, 70), 2, 4, 16, (4, 3), 64, 4),
+    ((3, 1), (1000, 70), 2, 4, 16, (2, 2), 33, 40),
+    ((7, 2), (300, 2), 2, 4, 16, (4, 4), 0, 0),
+    ((64, 5), (64, 200), 2, 1, 16, (4, 4), 0, 0),
+    ((130, 33), (130, 400), 1, 3, 32, (3, 4), 0, 0),
+    ((200,), (777,), 1, 2, 64, (4, 2), 90, 5),
+    ((40,), (40,), 1, 32, 16, (2, 3), 1, 0),
+]
+
+
+@pytest.mark.parametrize("rows,lengths,H,G,page,bits,window,sinks", ATTEND)
+def test_attention(rows, lengths, H, G, page, bits, window, sinks):
+    print(f"[case] attention {rows} of {lengths}, {H} x {G} heads, pages of {page}, {bits} bits, window {window} + {sinks}", flush=True)
+    c = Batch(500 + sum(lengths), rows, lengths, H, page, *bits, pad=2).upload()
+    q = c.row_tensor(H * G, 8, gain=2.0)
+    got = run_attention(c, q, G, 0.09, window, sinks, pad=16)
+    check_attention(c, q, G, 0.09, got, window=window, sinks=sinks)
+
+
+TREES = [((1,), (1,), 1, 1, 16, (4, 4)), ((13, 5), (400, 5), 2, 4, 16, (4, 4)), ((64,), (1000,), 1, 8, 64, (4, 3)), ((64, 1, 33), (64, 90, 600), 2, 2, 32, (2, 2)),
+         ((9, 20), (50, 320), 2, 1, 16, (3, 4))]
+
+
+@pytest.mark.parametrize("rows,lengths,H,G,page,bits", TREES)
+def test_tree_attention(rows, lengths, H, G, page, bits):
+    print(f"[case] tree {rows} of {lengths}, {H} x {G} heads", flush=True)
+    c = Batch(900 + sum(lengths), rows, lengths, H, page, *bits, pad=1).upload()
+    masks = np.zeros(c.T, dtype=np.uint64)
+    for b in range(c.B):
+        for i in range(c.rows[b]):
+            up = int(masks[c.starts[b] + c.r.integers(0, i)]) if i else 0
+            masks[c.starts[b] + i] = up | 1 << i
+    masks[c.T - 1] = 0xFFFFFFFFFFFFFFFF
+    if c.rows[0] > 4:
+        masks[3] = 0                                          # sees the prefix alone, or nothing
+    q = c.row_tensor(H * G)
+    got = run_attention(c, q, G, 0.088, masks=masks)
+    check_attention(c, q, G, 0.088, got, masks=masks)
