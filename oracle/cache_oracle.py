@@ -84,13 +84,25 @@ class Pages:
                 out[:, k] = dequantize(unpack(self.codes[at[0], :, at[1]], self.bits), (w & 0xFFFF).astype(np.uint16).view(np.float16), w >> 16)
         return out
 
+    def steps(self, table, positions):
+        """fp64 [H, tokens]; zeros where the token has no place."""
+        out = np.zeros((self.codes.shape[1], len(positions)))
+        for k, pos in enumerate(positions):
+            at = self.place(table, int(pos))
+            if at is not None:
+                out[:, k] = (self.params[at[0], :, at[1]] & 0xFFFF).astype(np.uint16).view(np.float16).astype(np.float64)
+        return out
 
-def attention64(q, k, v, seen, scale):
-    """q [n, 128], k, v [L, 128], seen [n, L] -> (out fp64 [n, 128], A [n, 128] = sum_j w_j |v_j|, smax [n] = max_j scale sum |q| |k_j|);
-    zeros for a row that sees nothing."""
+
+def attention64(q, k, v, seen, scale, k_step, v_step, k_bits=4):
+    """q [n, 128], k, v [L, 128], seen [n, L], the tokens' steps [L].  Returns out fp64 [n, 128] (zeros for a row that sees nothing) and what the
+    bound needs: A [n, 128] = sum_j w_j |v_j|, S [n] = sum_j w_j v_step_j, and the error `delta` [n] of a score:
+    s_j (sum_d q_d c_d - z sum_d q_d), each sum fp32 over 128 exact products of at most (2^b - 1) |q_d|, 12 more roundings; and the matrix
+    instruction, four of which add a score's products, drops what lies 24 bits below the largest of 33 addends, which counts as max |q| 2^10
+    code units of 2^-4 (codes are subnormal numbers there): 4 * 33 * 2^-18 max |q| s_j."""
     q = np.asarray(q, dtype=np.float64)
     n = q.shape[0]
-    out, A, smax = np.zeros((n, D)), np.zeros((n, D)), np.zeros(n)
+    out, A, S, delta = np.zeros((n, D)), np.zeros((n, D)), np.zeros(n), np.zeros(n)
     for i in range(n):
         j = np.flatnonzero(seen[i])
         if len(j) == 0:
@@ -100,17 +112,23 @@ def attention64(q, k, v, seen, scale):
         w /= w.sum()
         out[i] = w @ v[j]
         A[i] = w @ np.abs(v[j])
-        smax[i] = abs(scale) * (np.abs(k[j]) @ np.abs(q[i])).max()
-    return out, A, smax
+        S[i] = w @ v_step[j]
+        a = np.abs(q[i])
+        delta[i] = abs(scale) * k_step[j].max() * (280 * 2.0 ** -24 * (2 ** k_bits - 1) * a.sum() + 132 * 2.0 ** -18 * a.max())
+    return out, A, S, delta
 
 
-def attention_bound(out, A, smax, tokens):
-    """How far an output may be from fp64, from the arithmetic alone:
-    scores   fp32 sums of 128 exact products and four more roundings, exp2 of a difference: relative error of a weight below
-             delta = 2^-24 (128 + 12) smax + 2^-21
-    products weight times step rounded to fp16 (2^-11 of it; in the subnormals 2^-25 of at least 2^-7 of the row's largest, below), sums over
-             `tokens` in fp32: at most tokens / 128 + 64 additions behind each other, each 2^-24 of the sum of magnitudes
-    output   one rounding to fp16."""
-    delta = 2.0 ** -24 * 140 * smax[:, None] + 2.0 ** -21
-    sums = 2.0 ** -24 * (tokens / 128 + 64) + tokens * 2.0 ** -32
-    return A * (2.0 ** -11 + 2 * delta + 2 * sums) * (1 + 2.0 ** -8) + np.abs(out) * 2.0 ** -11 + 2.0 ** -24
+def attention_bound(out, A, S, delta, tokens, v_bits=4):
+    """How far an output may be from fp64, from the arithmetic alone.
+    scores   off by delta, and 2^-21 from exp2 of a rounded difference: relative errors of the weights
+    weights  times the value's step, rounded to fp16: 2^-11 of it (in the subnormals 2^-25 of at least 2^-7 of the row's largest: 2^-32 per token)
+    sums     sum_j w_j s_j c_j - sum_j w_j s_j z_j in fp32: at most tokens / 128 + 64 additions behind each other, each 2^-24 of a sum of at most
+             (2^b - 1) S; and what the matrix instruction drops of its 33 addends: 33 * 2^-24 of 2^10 code units of 2^-4 of the largest weight
+             of its 32 tokens, which sum to S at most over all of them
+    output   one rounding to fp16.
+    The weights' sum has the relative errors of the scores and sums."""
+    top = 2 ** v_bits - 1
+    delta = delta[:, None] + 2.0 ** -21
+    sums = 2.0 ** -24 * (tokens / 128 + 64)
+    return (A * (2.0 ** -11 + 2 * delta + sums) + S[:, None] * (2 * top * sums + top * tokens * 2.0 ** -32 + 33 * 2.0 ** -18)) * (1 + 2.0 ** -8) + \
+        np.abs(out) * 2.0 ** -11 + 2.0 ** -24

@@ -47,7 +47,7 @@ hipError_t kernel_occupancy(const void* fn, int threads, int lds, OccCache& cach
 
 KnobState g_knobs[(int)Knob::COUNT];
 namespace {
-const char* const kKnobNames[] = {"FLATQUANT_MODE", "FLATQUANT_WG_PER_CU", "FLATQUANT_FORCE_GENERIC", "FLATQUANT_KV_WG_PER_CU", "FLATQUANT_GEMM_TILED", "FLATQUANT_GEMM_WIDE", "FLATQUANT_GEMM_DEPTH", "FLATQUANT_GEMM_WAVES", "FLATQUANT_GEMM_ROWS", "FLATQUANT_GEMM_TOKENS", "FLATQUANT_GEMM_RING_MAX_T", "FLATQUANT_KV_FOLD_HEADS", "FLATQUANT_KV_FEW", "FLATQUANT_WAVE_TPW", "FLATQUANT_PROBE_SHAPE"};
+const char* const kKnobNames[] = {"FLATQUANT_MODE", "FLATQUANT_WG_PER_CU", "FLATQUANT_FORCE_GENERIC", "FLATQUANT_KV_WG_PER_CU", "FLATQUANT_GEMM_TILED", "FLATQUANT_GEMM_WIDE", "FLATQUANT_GEMM_DEPTH", "FLATQUANT_GEMM_WAVES", "FLATQUANT_GEMM_ROWS", "FLATQUANT_GEMM_TOKENS", "FLATQUANT_GEMM_RING_MAX_T", "FLATQUANT_KV_FOLD_HEADS", "FLATQUANT_KV_FEW", "FLATQUANT_WAVE_TPW", "FLATQUANT_PROBE_SHAPE", "FLATQUANT_ATT_CHUNK", "FLATQUANT_ATT_WG_PER_CU", "FLATQUANT_ATT_WHOLE_MAX"};
 static_assert(sizeof(kKnobNames) / sizeof(kKnobNames[0]) == (size_t)Knob::COUNT, "a name for every override");
 }  // namespace
 
@@ -360,7 +360,7 @@ static fq_status cache_attention(const fq_kv_cache* cache, const fq_kv_batch* ba
     const int64_t row = 128LL * Hq;
     if (Hq < 1 || Hq % cache->H != 0 || !std::isfinite(scale) || window < 0 || sinks < 0 || q_stride < row || out_stride < row || workspace_bytes < 0)
         return FQ_INVALID_ARG;
-    if (Hq > (1 << 24) || batch->T > (1LL << 40) / Hq || q_stride > (1LL << 40) || out_stride > (1LL << 40) || (tree && batch->max_rows > 64)) return FQ_UNSUPPORTED_SHAPE;
+    if (Hq > (1 << 24) || batch->T > 0x7fffff00LL / Hq || q_stride > (1LL << 40) || out_stride > (1LL << 40) || (tree && batch->max_rows > 64)) return FQ_UNSUPPORTED_SHAPE;
     if (empty) return FQ_OK;
     if (!q || !out || (tree && !visible)) return FQ_INVALID_ARG;
     const fq::AttnPlan plan = fq::attention_plan(batch->B, batch->T, cache->H, Hq, batch->max_rows, batch->max_length);
@@ -393,7 +393,7 @@ fq_status flatquant_cache_tree_attention(const fq_kv_cache* cache, const fq_kv_b
 
 int64_t fq_cache_attention_workspace(const fq_kv_cache* cache, const fq_kv_batch* batch, int Hq) {
     if (!cache || !batch || cache->H < 1 || cache->H > 65535 || Hq < 1 || Hq % cache->H != 0 || Hq > (1 << 24)) return -1;
-    if (batch->B < 0 || batch->T < 0 || batch->max_rows < 0 || batch->max_length < 0 || batch->T > (1LL << 29) || batch->T > (1LL << 40) / Hq ||
+    if (batch->B < 0 || batch->T < 0 || batch->max_rows < 0 || batch->max_length < 0 || batch->T > (1LL << 29) || batch->T > 0x7fffff00LL / Hq ||
         batch->B > 0xffffff / cache->H)
         return -1;
     if (batch->B == 0 || batch->T == 0) return 0;

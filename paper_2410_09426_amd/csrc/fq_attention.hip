@@ -7,11 +7,13 @@
 //                                registers in the order in which those codes become fp16
 //   O^T[channel, row] += V^T P^T A: lane (i, g) has channels 8 i .. 8 i + 7 of eight tokens, 4 g .. 4 g + 3 of each half of the 32:
 //                                those whose weights the lane of S^T already holds, so the weights need no exchange
-// Codes become fp16 without a conversion: a code's bits in the mantissa of 1024 (or of 1024 at bit s: 1024 + 2^s code), then one packed
-// fma takes 1024 and the zero point off, exactly.  The keys' steps scale the scores, the values' steps the weights.
+// Codes become fp16 without a conversion.  Few rows: a code in its place, masked, is a subnormal fp16 number (2^(s - 24) code), which the
+// matrix instructions take as it is; the powers of two are taken out of the queries and of the results, and the zero points out of the sums
+// (sum_d q_d (c_d - z) = sum_d q_d c_d - z sum_d q_d).  Many rows share the work of taking the zero point off each code, in LDS.  The keys'
+// steps scale the scores, the values' steps the weights.
 //
 // Softmax in one pass: weights are 2^(score - M), M a reference per row that is raised only where a weight times its step would pass
-// 2^15 (fp16's range) or a weight 2^40: most steps neither reduce a maximum nor touch the accumulators.  When it is raised it is put
+// 2^15 (fp16's range) or the weights 2^40: most steps neither reduce a maximum nor touch the accumulators.  When it is raised it is put
 // 2^7 above the largest product, so that products below 2^-14 of it, in fp16's subnormals, lose no more than 2^-32 of that product.
 //
 // The waves of a workgroup take every fourth step and meet in LDS at the end; where the rows are few the axis is split further over
@@ -26,38 +28,62 @@ constexpr int ATT_WAVES = 4;
 constexpr int ATT_NT = 64 * ATT_WAVES;
 constexpr int ATT_STEP = 32;               // tokens per step of a wave
 constexpr int ATT_PITCH = ATT_D + 4;       // floats per row of partial channels in LDS
+constexpr int kMaxSplits = 128;
 constexpr float ATT_NONE = -1e30f;         // reference of a row that has seen nothing: below every finite score
 
 typedef _Float16 half2v __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+// Lists that no kernel writes, read at uniform addresses: by scalar loads, which do not stand in the queue of the codes' loads.
+typedef const __attribute__((address_space(4))) int32_t* list_t;
 
 struct AttnDev {
     CacheDev c;
     const _Float16* q;
     _Float16* out;
     const uint64_t* visible;
-    float* part;              // [T * Hq, splits, 128] channels, then [T * Hq, splits] pairs of M and sum
+    float* part;              // partial channels, 128 a row, and pairs of M and sum: [T * Hq, splits] rows, or two tiles a workgroup (balanced)
+    float* stats;
     int64_t q_stride, out_stride;
     float scale2;             // scale * log2(e)
-    int Hq, G, window, sinks, chunk, splits;
+    int Hq, G, window, sinks, chunk, splits, min_units;
 };
+
+template <int N, int K = 0, typename F>
+__device__ __forceinline__ void each(F&& f) {                                  // f(0) .. f(N - 1), constants
+    if constexpr (K < N) {
+        f(std::integral_constant<int, K>{});
+        each<N, K + 1>(f);
+    }
+}
 
 // ---- codes to fp16
 
 __device__ __forceinline__ half2v as_half2(uint32_t x) { return __builtin_bit_cast(half2v, x); }
 __device__ __forceinline__ uint32_t as_u32(half2v x) { return __builtin_bit_cast(uint32_t, x); }
 
-// Two codes in bits [S, S + QB) of the halves of x, minus the zero points in `z` (packed fp16 whole numbers).
+// Two codes in bits [S, S + QB) of the halves of x, S + QB <= 10: as fp16 bits that is 2^(S - 24) code, a subnormal number, which the matrix
+// instructions take at its value.  They align the products to the largest of them, though, by its exponent as if it were normalised, and drop what
+// lies 24 bits below (measured: one code unit beside others is off by up to 2^-13.4 of itself at S = 0, by nothing at 2 and above for weights within
+// a factor of 20): S is 4 at least.
 template <int QB, int S>
-__device__ __forceinline__ half2v code_pair(uint32_t x, half2v z) {
-    constexpr uint32_t mask = (((1u << QB) - 1u) << S) * 0x00010001u;
-    const half2v raised = as_half2((x & mask) | 0x64006400u);                  // 1024 + 2^S code
-    if constexpr (S == 0) return raised - (z + (half2v)(_Float16)1024.0f);
-    constexpr _Float16 down = (_Float16)(1.0f / (float)(1 << S)), off = (_Float16)(-1024.0f / (float)(1 << S));
+__device__ __forceinline__ uint32_t field(uint32_t x) {
+    static_assert(S >= 4 && S + QB <= 10, "mantissa bits");
+    return x & ((((1u << QB) - 1u) << S) * 0x00010001u);
+}
+// code - zero point of such a field; `z`: 1024 + the zero points, in fp16.  1024 in the exponent makes it 1024 + 2^S code; one packed fma takes
+// 1024 and the zero point off, exactly.
+template <int S>
+__device__ __forceinline__ half2v code_value(uint32_t f, half2v z) {
+    const half2v raised = as_half2(f | 0x64006400u);
+    constexpr _Float16 down = (_Float16)(1.0f / (float)(1 << S)), off = (_Float16)(1024.0f - 1024.0f / (float)(1 << S));
     return __builtin_elementwise_fma(raised, half2v{down, down}, half2v{off, off} - z);
 }
+__device__ __forceinline__ half2v raised_zeros(uint32_t low, uint32_t high) {  // of two tokens' parameters
+    return as_half2((__builtin_amdgcn_perm(high, low, 0x07060302u) & 0x000F000Fu) | 0x64006400u);
+}
 
-// The 32 codes of a lane's quarter of a key, as 16 pairs; pair p is (first(p), second(p)) of the 32.
+// The 32 codes of a lane's quarter of a key, as 16 pairs of fields; pair p is (first(p), second(p)) of the 32, at bit shift(p).
 template <int QB>
 struct KeyCodes;
 template <>
@@ -65,147 +91,166 @@ struct KeyCodes<4> {
     typedef u32x4 words;
     static constexpr int first(int p) { return 8 * (p >> 2) + (p & 3); }
     static constexpr int second(int p) { return first(p) + 4; }
-    static __device__ __forceinline__ void expand(const words& w, half2v z, half2v (&o)[16]) {
+    static constexpr int shift(int) { return 4; }
+    static __device__ __forceinline__ void fields(const words& w, uint32_t (&o)[16]) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const uint32_t hi = w[k] >> 8;
-            o[4 * k] = code_pair<4, 0>(w[k], z);
-            o[4 * k + 1] = code_pair<4, 4>(w[k], z);
-            o[4 * k + 2] = code_pair<4, 0>(hi, z);
-            o[4 * k + 3] = code_pair<4, 4>(hi, z);
+            o[4 * k] = field<4, 4>(w[k] << 4);
+            o[4 * k + 1] = field<4, 4>(w[k]);
+            o[4 * k + 2] = field<4, 4>(w[k] >> 4);
+            o[4 * k + 3] = field<4, 4>(w[k] >> 8);
         }
     }
 };
+__device__ __forceinline__ constexpr int shift2(int c) { return c < 3 ? 4 + 2 * c : c < 5 ? 2 * c : 2 * c - 6; }      // of the 2-bit codes of a half
 template <>
 struct KeyCodes<2> {
     typedef uint32_t words __attribute__((ext_vector_type(2)));
     static constexpr int first(int p) { return 16 * (p >> 3) + (p & 7); }
     static constexpr int second(int p) { return first(p) + 8; }
-    static __device__ __forceinline__ void expand(const words& w, half2v z, half2v (&o)[16]) {
+    static constexpr int shift(int p) { return shift2(p & 7); }
+    static __device__ __forceinline__ void fields(const words& w, uint32_t (&o)[16]) {
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-            const uint32_t hi = w[k] >> 10;
-            o[8 * k] = code_pair<2, 0>(w[k], z);
-            o[8 * k + 1] = code_pair<2, 2>(w[k], z);
-            o[8 * k + 2] = code_pair<2, 4>(w[k], z);
-            o[8 * k + 3] = code_pair<2, 6>(w[k], z);
-            o[8 * k + 4] = code_pair<2, 8>(w[k], z);
-            o[8 * k + 5] = code_pair<2, 0>(hi, z);
-            o[8 * k + 6] = code_pair<2, 2>(hi, z);
-            o[8 * k + 7] = code_pair<2, 4>(hi, z);
+            o[8 * k] = field<2, 4>(w[k] << 4);
+            o[8 * k + 1] = field<2, 6>(w[k] << 4);
+            o[8 * k + 2] = field<2, 8>(w[k] << 4);
+            o[8 * k + 3] = field<2, 6>(w[k]);
+            o[8 * k + 4] = field<2, 8>(w[k]);
+            o[8 * k + 5] = field<2, 4>(w[k] >> 6);
+            o[8 * k + 6] = field<2, 6>(w[k] >> 6);
+            o[8 * k + 7] = field<2, 8>(w[k] >> 6);
         }
     }
 };
-// Sixteen codes are 48 bits, three halves X0, X1, X2: codes 5 and 10 straddle two of them.
-__device__ __forceinline__ void expand48(uint32_t x0, uint32_t x1, uint32_t x2, half2v z, half2v (&o)[16]) {
-    const uint32_t y0 = x0 >> 9, y1 = x1 >> 8, y2 = x2 >> 10;
-    o[0] = code_pair<3, 0>(x0, z);
-    o[1] = code_pair<3, 3>(x0, z);
-    o[2] = code_pair<3, 6>(x0, z);
-    o[3] = code_pair<3, 0>(y0, z);
-    o[4] = code_pair<3, 3>(y0, z);
-    o[5] = code_pair<3, 6>((y0 & 0x00400040u) | (x1 << 7 & 0x01800180u), z);
-    o[6] = code_pair<3, 2>(x1, z);
-    o[7] = code_pair<3, 5>(x1, z);
-    o[8] = code_pair<3, 0>(y1, z);
-    o[9] = code_pair<3, 3>(y1, z);
-    o[10] = code_pair<3, 6>((y1 & 0x00C000C0u) | (x2 << 8 & 0x01000100u), z);
-    o[11] = code_pair<3, 1>(x2, z);
-    o[12] = code_pair<3, 4>(x2, z);
-    o[13] = code_pair<3, 7>(x2, z);
-    o[14] = code_pair<3, 0>(y2, z);
-    o[15] = code_pair<3, 3>(y2, z);
-}
 template <>
 struct KeyCodes<3> {
     typedef uint32_t words __attribute__((ext_vector_type(3)));
     static constexpr int first(int p) { return p; }
     static constexpr int second(int p) { return p + 16; }
-    static __device__ __forceinline__ void expand(const words& w, half2v z, half2v (&o)[16]) {
+    // sixteen codes are 48 bits, three halves x0, x1, x2: codes 5 and 10 straddle two of them
+    static constexpr int shift(int p) {
+        constexpr int at[16] = {4, 7, 6, 4, 7, 6, 5, 5, 4, 7, 6, 5, 4, 7, 4, 7};
+        return at[p];
+    }
+    static __device__ __forceinline__ void fields(const words& w, uint32_t (&o)[16]) {
         // bits 0 .. 47 in the low halves, 48 .. 95 in the high ones
-        expand48(__builtin_amdgcn_perm(w[1], w[0], 0x07060100u), __builtin_amdgcn_perm(w[2], w[0], 0x05040302u),
-                 __builtin_amdgcn_perm(w[2], w[1], 0x07060100u), z, o);
+        const uint32_t x0 = __builtin_amdgcn_perm(w[1], w[0], 0x07060100u), x1 = __builtin_amdgcn_perm(w[2], w[0], 0x05040302u),
+                       x2 = __builtin_amdgcn_perm(w[2], w[1], 0x07060100u);
+        o[0] = field<3, 4>(x0 << 4);
+        o[1] = field<3, 7>(x0 << 4);
+        o[2] = field<3, 6>(x0);
+        o[3] = field<3, 4>(x0 >> 5);
+        o[4] = field<3, 7>(x0 >> 5);
+        o[5] = (x0 >> 9 & 0x00400040u) | (x1 << 7 & 0x01800180u);
+        o[6] = field<3, 5>(x1 << 3);
+        o[7] = field<3, 5>(x1);
+        o[8] = field<3, 4>(x1 >> 4);
+        o[9] = field<3, 7>(x1 >> 4);
+        o[10] = (x1 >> 8 & 0x00C000C0u) | (x2 << 8 & 0x01000100u);
+        o[11] = field<3, 5>(x2 << 4);
+        o[12] = field<3, 4>(x2);
+        o[13] = field<3, 7>(x2);
+        o[14] = field<3, 4>(x2 >> 6);
+        o[15] = field<3, 7>(x2 >> 6);
     }
 };
 
-// A lane's eight channels of two tokens (low half, high half): o[channel].
+// Four of a lane's eight channels (HALF 0: 0 .. 3, 1: 4 .. 7) of two tokens (low half, high half), channel c of the eight at bit shift(c).
 template <int QB>
-__device__ __forceinline__ void value_pairs(uint32_t a, uint32_t b, half2v z, half2v (&o)[8]) {
-    const uint32_t x = __builtin_amdgcn_perm(b, a, 0x05040100u);
-    if constexpr (QB == 4) {
-        const uint32_t y = __builtin_amdgcn_perm(b, a, 0x07060302u), xh = x >> 8, yh = y >> 8;
-        o[0] = code_pair<4, 0>(x, z);
-        o[1] = code_pair<4, 4>(x, z);
-        o[2] = code_pair<4, 0>(xh, z);
-        o[3] = code_pair<4, 4>(xh, z);
-        o[4] = code_pair<4, 0>(y, z);
-        o[5] = code_pair<4, 4>(y, z);
-        o[6] = code_pair<4, 0>(yh, z);
-        o[7] = code_pair<4, 4>(yh, z);
-    } else if constexpr (QB == 2) {
-        const uint32_t xh = x >> 10;
-        o[0] = code_pair<2, 0>(x, z);
-        o[1] = code_pair<2, 2>(x, z);
-        o[2] = code_pair<2, 4>(x, z);
-        o[3] = code_pair<2, 6>(x, z);
-        o[4] = code_pair<2, 8>(x, z);
-        o[5] = code_pair<2, 0>(xh, z);
-        o[6] = code_pair<2, 2>(xh, z);
-        o[7] = code_pair<2, 4>(xh, z);
-    } else {
-        const uint32_t y = __builtin_amdgcn_perm(b, a, 0x07060302u), xh = x >> 9;
-        o[0] = code_pair<3, 0>(x, z);
-        o[1] = code_pair<3, 3>(x, z);
-        o[2] = code_pair<3, 6>(x, z);
-        o[3] = code_pair<3, 0>(xh, z);
-        o[4] = code_pair<3, 3>(xh, z);
-        o[5] = code_pair<3, 6>((xh & 0x00400040u) | (y << 7 & 0x01800180u), z);
-        o[6] = code_pair<3, 2>(y, z);
-        o[7] = code_pair<3, 5>(y, z);
+struct ValueCodes {
+    static constexpr int shift(int c) {
+        constexpr int at[8] = {4, 7, 6, 4, 7, 6, 5, 5};
+        return QB == 4 ? 4 : QB == 2 ? shift2(c) : at[c];
     }
-}
-
-// ---- one step's tokens
-
-template <int KB, int VB>
-struct StepCodes {
-    typename KeyCodes<KB>::words k[2];
-    uint32_t kz[2];                        // parameters of the token that is the lane's row of A
-    u32x4 ks[2];                           // parameters of the four tokens that are the lane's rows of S^T
-    uint32_t v[8];
-    u32x4 vs[2];
+    template <int HALF>
+    static __device__ __forceinline__ void fields(uint32_t a, uint32_t b, uint32_t (&o)[4]) {
+        const uint32_t x = __builtin_amdgcn_perm(b, a, 0x05040100u);
+        if constexpr (QB == 4) {
+            const uint32_t y = HALF ? __builtin_amdgcn_perm(b, a, 0x07060302u) : x;
+            o[0] = field<4, 4>(y << 4);
+            o[1] = field<4, 4>(y);
+            o[2] = field<4, 4>(y >> 4);
+            o[3] = field<4, 4>(y >> 8);
+        } else if constexpr (QB == 2 && HALF == 0) {
+            o[0] = field<2, 4>(x << 4);
+            o[1] = field<2, 6>(x << 4);
+            o[2] = field<2, 8>(x << 4);
+            o[3] = field<2, 6>(x);
+        } else if constexpr (QB == 2) {
+            o[0] = field<2, 8>(x);
+            o[1] = field<2, 4>(x >> 6);
+            o[2] = field<2, 6>(x >> 6);
+            o[3] = field<2, 8>(x >> 6);
+        } else if constexpr (HALF == 0) {
+            o[0] = field<3, 4>(x << 4);
+            o[1] = field<3, 7>(x << 4);
+            o[2] = field<3, 6>(x);
+            o[3] = field<3, 4>(x >> 5);
+        } else {
+            const uint32_t y = __builtin_amdgcn_perm(b, a, 0x07060302u);
+            o[0] = field<3, 7>(x >> 5);
+            o[1] = (x >> 9 & 0x00400040u) | (y << 7 & 0x01800180u);
+            o[2] = field<3, 5>(y << 3);
+            o[3] = field<3, 5>(y);
+        }
+    }
 };
-// Codes and parameters of tokens k0 .. k0 + 15 and k0 + 16 .. k0 + 31, in pages p[0] and p[1] (the caller has checked the numbers): whole
-// pages are memory that may be read, whatever of them has been written.
+
+// ---- a wave's ring of steps in LDS (few rows)
+//
+// A slot holds 32 tokens: two pieces of 16 keys' codes, two of values', and the 64 parameters.  Global-to-LDS loads fill it, one 16-byte
+// chunk a lane and one instruction a piece (4 bits; fewer lanes for fewer bits), so that a step costs five loads and no registers while
+// it is on its way.  At 4 bits the lanes fetch the chunks in the order that makes the reads free of bank conflicts: keys by quarters of all
+// 16 tokens, values by tokens 4 g + r of all four g.
 template <int KB, int VB>
-__device__ __forceinline__ void load_step(const CacheDev& c, int head, int k0, const int (&p)[2], int i, int g, StepCodes<KB, VB>& s) {
+struct Ring {
+    static constexpr int K_PIECE = 256 * KB, V_PIECE = 256 * VB;
+    static constexpr int V_AT = 2 * K_PIECE, P_AT = V_AT + 2 * V_PIECE, SLOT = P_AT + 256;
+    static constexpr int LOADS = 5;
+};
+typedef const __attribute__((address_space(1))) void* att_gptr;
+typedef __attribute__((address_space(3))) void* att_lptr;
+template <int BITS, bool VALUES>
+__device__ __forceinline__ void load_piece(const uint8_t* src, unsigned char* dst, int l) {
+    // byte of the piece that lane l fetches
+    const int from = BITS != 4 ? 16 * l : VALUES ? 64 * (4 * (l >> 2 & 3) + (l >> 4)) + 16 * (l & 3) : 64 * (l & 15) + 16 * (l >> 4);
+    if (BITS == 4 || l < 16 * BITS) __builtin_amdgcn_global_load_lds((att_gptr)(src + from), (att_lptr)dst, 16, 0, 0);
+}
+// Tokens k0 .. k0 + 15 and k0 + 16 .. k0 + 31 in pages pg[0] and pg[1] (the caller has checked the numbers): whole pages are memory that may be
+// read, whatever of them has been written.
+template <int KB, int VB>
+__device__ __forceinline__ void load_step(const CacheDev& c, int head, int k0, const int (&pg)[2], int l, unsigned char* slot) {
+    typedef Ring<KB, VB> R;
+    int64_t at[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-        const int64_t at = (((int64_t)p[t] * c.H + head) << c.page_shift) + ((k0 + 16 * t) & ((1 << c.page_shift) - 1));
-        const uint8_t* kc = c.codes[0] + at * (16 * KB);
-        const uint8_t* vc = c.codes[1] + at * (16 * VB);
-        const uint32_t* kp = c.params[0] + at;
-        const uint32_t* vp = c.params[1] + at;
-        __builtin_memcpy(&s.k[t], __builtin_assume_aligned(kc + i * (16 * KB) + g * (4 * KB), 4), 4 * KB);
-        s.kz[t] = kp[i];
-        s.ks[t] = *reinterpret_cast<const u32x4*>(kp + 4 * g);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const uint8_t* row = vc + (4 * g + r) * (16 * VB);
-            if constexpr (VB == 4) {
-                s.v[4 * t + r] = reinterpret_cast<const uint32_t*>(row)[i];
-            } else if constexpr (VB == 2) {
-                s.v[4 * t + r] = reinterpret_cast<const uint16_t*>(row)[i];
-            } else {                       // three bytes at 3 i, as four that do not leave the row (shifted where they are used)
-                uint32_t w;
-                __builtin_memcpy(&w, row + (i < 15 ? 3 * i : 44), 4);
-                s.v[4 * t + r] = w;
-            }
-        }
-        s.vs[t] = *reinterpret_cast<const u32x4*>(vp + 4 * g);
+        at[t] = (((int64_t)pg[t] * c.H + head) << c.page_shift) + ((k0 + 16 * t) & ((1 << c.page_shift) - 1));
+        load_piece<KB, false>(c.codes[0] + at[t] * (16 * KB), slot + t * R::K_PIECE, l);
+        load_piece<VB, true>(c.codes[1] + at[t] * (16 * VB), slot + R::V_AT + t * R::V_PIECE, l);
     }
+    const uint32_t* params = (l < 32 ? c.params[0] : c.params[1]) + (l & 16 ? at[1] : at[0]) + (l & 15);
+    __builtin_amdgcn_global_load_lds((att_gptr)params, (att_lptr)(slot + R::P_AT), 4, 0, 0);
+}
+// The lane's quarter of token i's key in piece t; its four values' codes (tokens 4 g + r, r = 0 .. 3, channels 8 i .. 8 i + 7) in piece t.
+template <int KB>
+__device__ __forceinline__ typename KeyCodes<KB>::words ring_key(const unsigned char* piece, int i, int g) {
+    typename KeyCodes<KB>::words w;
+    if constexpr (KB == 4) w = *reinterpret_cast<const u32x4*>(piece + 16 * (16 * g + i));
+    else
+#pragma unroll
+        for (int k = 0; k < KB; ++k) w[k] = reinterpret_cast<const uint32_t*>(piece)[4 * KB * i + KB * g + k];
+    return w;
+}
+template <int VB>
+__device__ __forceinline__ uint32_t ring_value(const unsigned char* piece, int i, int g, int r) {
+    if constexpr (VB == 4) return reinterpret_cast<const uint32_t*>(piece)[64 * r + 16 * g + i];
+    if constexpr (VB == 2) return reinterpret_cast<const uint16_t*>(piece)[16 * (4 * g + r) + i];
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(piece) + 12 * (4 * g + r) + (3 * i >> 2);      // (the last lane's second word is never used)
+    return __builtin_amdgcn_alignbit(w[(3 * i & 3) > 1 ? 1 : 0], w[0], 8 * (3 * i & 3));
 }
 
+__device__ __forceinline__ float zero_of(uint32_t params) { return (float)(params >> 16 & 255u); }
 __device__ __forceinline__ float step_of(uint32_t params) { return (float)__builtin_bit_cast(_Float16, (uint16_t)params); }
 
 template <typename T>
@@ -249,312 +294,864 @@ struct Sequence {
     int first, rows, length;
 };
 __device__ __forceinline__ Sequence sequence_of(const CacheDev& c, int b) {
-    const int last = c.row_starts[b + 1], T = (int)c.T;
+    const list_t starts = (list_t)c.row_starts;
+    const int first = starts[b], last = starts[b + 1], T = (int)c.T;
     Sequence s;
-    s.first = c.row_starts[b] > 0 ? c.row_starts[b] : 0;
+    s.length = ((list_t)c.lengths)[b];
+    s.first = first > 0 ? first : 0;
     s.rows = (last < T ? last : T) - s.first;
-    s.length = c.lengths[b];
     return s;
 }
 
-// blockIdx: (sequence and head, tile of rows, split).
-template <int KB, int VB, int NT>
-__global__ __launch_bounds__(ATT_NT) void attention_kernel(AttnDev p) {
-    __shared__ __attribute__((aligned(16))) float sums[ATT_WAVES][16][ATT_PITCH];
-    __shared__ float refs[ATT_WAVES][16 * NT], totals[ATT_WAVES][16 * NT];
+// Whether a row at position `pos` (in a tree: the last token before the draft, and `seen`) sees token k.
+__device__ __forceinline__ bool sees(const AttnDev& p, int k, int pos, int before, uint64_t seen) {
+    bool ok = k <= pos;
+    if (p.visible) {
+        const int bit = k - before;
+        ok = ok || (bit >= 0 && bit < 64 && (seen >> (bit & 63) & 1));
+    } else if (p.window > 0) {
+        ok = ok && ((int64_t)k > (int64_t)pos - p.window || k < p.sinks);
+    }
+    return ok;
+}
+// The step of a value that not every row sees: a number, so that a weight of zero makes a product of zero whatever the page holds.
+__device__ __forceinline__ float finite_step(float s) { return __builtin_fminf(s, 65504.0f); }
+// Weights 2^(factor score - ref), their products with the values' steps and the weights' sum; true if a lane of the wave needs a higher reference.
+template <int N, typename Scores, typename Factor>
+__device__ __forceinline__ bool weigh(const Scores& score, Factor factor, const float (&step)[N], float ref, float (&prod)[N], float& sum) {
+    float big = 0.0f;
+    sum = 0.0f;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(score[k], factor(k), -ref));
+        sum += e;
+        prod[k] = e * step[k];
+        big = __builtin_fmaxf(big, prod[k]);
+    }
+    return __any(big > 32768.0f || sum > 0x1p40f);
+}
+// Raises the reference so that the row's largest product here is at most 2^7 (a step below 2^-25 counts as that); returns the factor for what has been summed.
+template <int N, typename Scores, typename Factor, typename Row>
+__device__ __forceinline__ float raise_reference(const Scores& score, Factor factor, const float (&step)[N], float& ref, Row row_max) {
+    float top = ATT_NONE;
+#pragma unroll
+    for (int k = 0; k < N; ++k) top = __builtin_fmaxf(top, score[k] * factor(k) + __builtin_fmaxf(__builtin_amdgcn_logf(step[k]), -25.0f));
+    const float to = __builtin_fmaxf(ref, row_max(top) - 7.0f), f = __builtin_amdgcn_exp2f(ref - to);
+    ref = to;
+    return f;
+}
+
+// ---- few rows: a wave has 16 NT of them and every NW-th step of a stretch of the sequence
+template <int KB, int VB, int NT, int NW>
+struct FewRows {
+    static constexpr int DEPTH = 2;                                            // slots of a wave's ring
+    static constexpr int RING = NW * DEPTH * Ring<KB, VB>::SLOT, SUMS = NW * 16 * ATT_PITCH * 4;
+    static constexpr int STATS = RING > SUMS ? RING : SUMS;                    // references and sums of the rows, behind what the ring and the join share
+    static constexpr int LDS = STATS + 2 * NW * 16 * NT * 4;
+};
+// Rows row0 .. row_end - 1 (16 NT at most) of head `head` of sequence b over steps [x_begin, x_end) of their span.  The result is the output, or (partial) what
+// the join needs, rows from partial_at on.
+template <int KB, int VB, int NT, int NW>
+__device__ __forceinline__ void few_rows(const AttnDev& p, unsigned char* smem, int b, int head, const Sequence& seq, int row0, int row_end, const Span& span,
+                                         int x_begin, int x_end, bool partial, int64_t partial_at) {
+    typedef Ring<KB, VB> R;
+    typedef FewRows<KB, VB, NT, NW> F;
+    constexpr int DEPTH = F::DEPTH;
     const int l = threadIdx.x & 63, i = l & 15, g = l >> 4;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int b = blockIdx.x / p.c.H, head = blockIdx.x - b * p.c.H;
-    const Sequence seq = sequence_of(p.c, b);
-    const int64_t all_rows = (int64_t)seq.rows * p.G;
-    const int tiles = (int)((all_rows + 16 * NT - 1) / (16 * NT));
-    const int32_t* table = p.c.page_table + b * p.c.table_stride;
-    for (int tile_no = blockIdx.y; tile_no < tiles; tile_no += gridDim.y) {
-        const int64_t row0 = (int64_t)(tiles - 1 - tile_no) * (16 * NT);      // the last rows, which see most, first
-        const int64_t row_end = row0 + 16 * NT < all_rows ? row0 + 16 * NT : all_rows;
-        const int before = seq.length - seq.rows;                              // position of row 0's token
-        const int pos_lo = before + (int)(row0 / p.G), pos_hi = before + (int)((row_end - 1) / p.G);
-        const Span span = span_of(p, seq.length, pos_lo, pos_hi);
-        const int used = splits_used(p, span.steps);
-        if ((int)blockIdx.z >= used) continue;
-        const int per = p.chunk / ATT_STEP;
-        const int x_end = (int)blockIdx.z == p.splits - 1 ? span.steps : min(span.steps, ((int)blockIdx.z + 1) * per);
+    unsigned char* ring = smem + w * DEPTH * R::SLOT;
+    float (*sums)[16][ATT_PITCH] = reinterpret_cast<float (*)[16][ATT_PITCH]>(smem);
+    float (*refs)[16 * NT] = reinterpret_cast<float (*)[16 * NT]>(smem + F::STATS);
+    float (*totals)[16 * NT] = refs + NW;
+    const list_t table = (list_t)p.c.page_table + b * p.c.table_stride;
+    const int before = seq.length - seq.rows;                                  // position of row 0's token
+    const int pos_lo = before + row0 / p.G, pos_hi = before + (row_end - 1) / p.G;
 
-        // rows: queries in the order of the codes, positions
-        half8 q[NT][4];
-        int pos[NT];
-        uint64_t seen[NT];
+    // (a step behind the last one: no harm, what its table entries say is checked before it is followed)
+    auto pages_of = [&](int x, int (&pg)[2]) {
+        const int k0 = span.token(x);
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            int64_t r = row0 + 16 * n + i;
-            r = r < row_end ? r : row_end - 1;
-            const int token = (int)(r / p.G), sub = (int)(r - (int64_t)token * p.G);
-            const _Float16* src = p.q + (seq.first + token) * p.q_stride + (head * p.G + sub) * ATT_D + 32 * g;
-            half8 raw[4];
-#pragma unroll
-            for (int m = 0; m < 4; ++m) raw[m] = *reinterpret_cast<const half8*>(src + 8 * m);
-#pragma unroll
-            for (int m = 0; m < 4; ++m)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int a = KeyCodes<KB>::first(4 * m + e), z = KeyCodes<KB>::second(4 * m + e);
-                    q[n][m][2 * e] = raw[a >> 3][a & 7];
-                    q[n][m][2 * e + 1] = raw[z >> 3][z & 7];
-                }
-            pos[n] = p.visible ? before - 1 : before + token;
-            seen[n] = p.visible ? p.visible[seq.first + token] : 0;
+        for (int t = 0; t < 2; ++t) {
+            const unsigned j = (unsigned)(k0 + 16 * t) >> p.c.page_shift;
+            pg[t] = table[j < (unsigned)p.c.table_width ? j : p.c.table_width - 1];        // (behind the width is behind the end)
         }
+    };
+    auto load = [&](int x, const int (&pg)[2], int slot) {
+        const int ok[2] = {(unsigned)pg[0] < (unsigned)p.c.pages ? pg[0] : 0, (unsigned)pg[1] < (unsigned)p.c.pages ? pg[1] : 0};
+        load_step<KB, VB>(p.c, head, span.token(x), ok, l, ring + slot * R::SLOT);
+    };
+    int x = x_begin + w;
+    int pg[DEPTH + 1][2];
+    const bool any = x < x_end;
+    if (any)
+#pragma unroll
+        for (int k = 0; k <= DEPTH; ++k) pages_of(x + NW * k, pg[k]);
 
-        f32x4 acc[NT][8];
-        float ref[NT], total[NT];
+    // Rows: queries in the order of the codes, brought up to 2^9 and down by the codes' shifts (a power of two each, and back in `factor`, where the
+    // sign of the scale goes the other way), their sums, positions.  Asked for before the first steps: loads return in order.
+    half8 raw[NT][4];
+    int pos[NT];
+    uint64_t seen[NT];
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            ref[n] = ATT_NONE;
-            total[n] = 0.0f;
+    for (int n = 0; n < NT; ++n) {
+        int r = row0 + 16 * n + i;
+        r = r < row_end ? r : row_end - 1;
+        const int token = r / p.G, sub = r - token * p.G;
+        const _Float16* src = p.q + (seq.first + token) * p.q_stride + (head * p.G + sub) * ATT_D + 32 * g;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) acc[n][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        }
-
-        auto pages_of = [&](int x, int (&pg)[2]) {
-            x = x < span.steps ? x : span.steps - 1;
-            const int k0 = span.token(x);
+        for (int m = 0; m < 4; ++m) raw[n][m] = *reinterpret_cast<const half8*>(src + 8 * m);
+        pos[n] = p.visible ? before - 1 : before + token;
+        seen[n] = p.visible ? p.visible[seq.first + token] : 0;
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (any)
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                int j = (k0 + 16 * t) >> p.c.page_shift;
-                j = j < p.c.table_width ? j : p.c.table_width - 1;             // only tokens behind the end: masked
-                pg[t] = table[j];
+        for (int k = 0; k < DEPTH; ++k) load(x + NW * k, pg[k], k);
+    __builtin_amdgcn_sched_barrier(0);
+    half8 q[NT][4];
+    float q_sum[NT], factor[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        float sum = 0.0f, top = 0.0f;
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                sum += (float)raw[n][m][e];
+                top = __builtin_fmaxf(top, __builtin_fabsf((float)raw[n][m][e]));
             }
-        };
-        auto load = [&](int x, const int (&pg)[2], StepCodes<KB, VB>& s) {
-            x = x < span.steps ? x : span.steps - 1;
-            const int ok[2] = {(unsigned)pg[0] < (unsigned)p.c.pages ? pg[0] : 0, (unsigned)pg[1] < (unsigned)p.c.pages ? pg[1] : 0};
-            load_step<KB, VB>(p.c, head, span.token(x), ok, i, g, s);
-        };
-        auto work = [&](int x, const int (&pg)[2], const StepCodes<KB, VB>& s) {
-            const int k0 = span.token(x);
-            f32x4 sc[NT][2];
+        const int up = 10 - __builtin_amdgcn_frexp_expf(across_groups(top, fmax_op));
+        const float scaled = __builtin_ldexpf(p.scale2 < 0.0f ? -1.0f : 1.0f, up);
+        q_sum[n] = across_groups(sum, fadd_op) * __builtin_ldexpf(scaled, -24);
+        // never zero: what is not visible scores -infinity before this factor
+        factor[n] = __builtin_amdgcn_fmed3f(__builtin_ldexpf(__builtin_fabsf(p.scale2), 24 - up), 0x1p-120f, 0x1p100f);
+        each<16>([&](auto pp) {
+            constexpr int pair = decltype(pp)::value, a = KeyCodes<KB>::first(pair), z = KeyCodes<KB>::second(pair);
+            const float by = scaled * (1.0f / (float)(1 << KeyCodes<KB>::shift(pair)));
+            q[n][pair >> 2][2 * (pair & 3)] = (_Float16)((float)raw[n][a >> 3][a & 7] * by);
+            q[n][pair >> 2][2 * (pair & 3) + 1] = (_Float16)((float)raw[n][z >> 3][z & 7] * by);
+        });
+    }
+
+    f32x4 acc[NT][8];
+    float ref[NT], total[NT], zeros[NT];                                   // zeros: sum of the products times their tokens' zero points
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        ref[n] = ATT_NONE;
+        total[n] = zeros[n] = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[n][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+
+    auto work = [&](int x, const int (&pg)[2], const unsigned char* slot) {
+        const int k0 = span.token(x);
+        f32x4 sc[NT][2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            __builtin_amdgcn_sched_barrier(0);
+            uint32_t kk[16];
+            KeyCodes<KB>::fields(ring_key<KB>(slot + t * R::K_PIECE, i, g), kk);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) sc[n][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int m = 0; m < 4; ++m) {
+                const u32x4 a = {kk[4 * m], kk[4 * m + 1], kk[4 * m + 2], kk[4 * m + 3]};
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+                    sc[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, a), q[n][m], sc[n][t], 0, 0, 0);
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        // sum_d q_d (c_d - z) = (sum_d q_d c_d) - z sum_d q_d
+        float vs[8], vz[8];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const u32x4 kp = *reinterpret_cast<const u32x4*>(slot + R::P_AT + 64 * t + 16 * g), vp = *reinterpret_cast<const u32x4*>(slot + R::P_AT + 128 + 64 * t + 16 * g);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const float z = zero_of(kp[r]), f = step_of(kp[r]);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) sc[n][t][r] = __builtin_fmaf(-z, q_sum[n], sc[n][t][r]) * f;
+                vs[4 * t + r] = step_of(vp[r]);
+                vz[4 * t + r] = zero_of(vp[r]);
+            }
+        }
+        const bool pages_ok = (unsigned)pg[0] < (unsigned)p.c.pages && (unsigned)pg[1] < (unsigned)p.c.pages;
+        const int all_see = p.visible ? before - 1 : pos_lo;               // every row sees the tokens up to here, but for the window
+        if (!(pages_ok && k0 + ATT_STEP - 1 <= all_see && k0 + ATT_STEP <= span.end && (p.window <= 0 || p.visible || k0 > pos_hi - p.window))) {
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                const half2v z = as_half2((s.kz[t] >> 16 & 15u) * 0x00010001u | 0x64006400u) - (half2v)(_Float16)1024.0f;
-                half2v kk[16];
-                KeyCodes<KB>::expand(s.k[t], z, kk);
+                const bool page_ok = (unsigned)pg[t] < (unsigned)p.c.pages;
 #pragma unroll
-                for (int n = 0; n < NT; ++n) sc[n][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                for (int m = 0; m < 4; ++m) {
-                    const u32x4 a = {as_u32(kk[4 * m]), as_u32(kk[4 * m + 1]), as_u32(kk[4 * m + 2]), as_u32(kk[4 * m + 3])};
+                for (int r = 0; r < 4; ++r) {
+                    const int k = k0 + 16 * t + 4 * g + r;
+                    vs[4 * t + r] = finite_step(vs[4 * t + r]);
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
-                        sc[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, a), q[n][m], sc[n][t], 0, 0, 0);
+                        sc[n][t][r] = sees(p, k, pos[n], before, seen[n]) && page_ok && k < span.end ? sc[n][t][r] : -__builtin_inff();
                 }
             }
+        }
+        half8 pw[NT];
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+        for (int n = 0; n < NT; ++n) {
+            float s8[8], prod[8], sum;
+            auto by = [&](int) { return factor[n]; };
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
+            for (int k = 0; k < 8; ++k) s8[k] = sc[n][k >> 2][k & 3];
+            if (weigh<8>(s8, by, vs, ref[n], prod, sum)) {
+                const float f = raise_reference<8>(s8, by, vs, ref[n], [](float top) { return across_groups(top, fmax_op); });
+                total[n] *= f;
+                zeros[n] *= f;
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) sc[n][t][r] *= step_of(s.ks[t][r]) * p.scale2;
-            const bool pages_ok = (unsigned)pg[0] < (unsigned)p.c.pages && (unsigned)pg[1] < (unsigned)p.c.pages;
-            const int all_see = p.visible ? before - 1 : pos_lo;               // every row sees the tokens up to here, but for the window
-            if (!(pages_ok && k0 + ATT_STEP - 1 <= all_see && k0 + ATT_STEP <= span.end && (p.window <= 0 || p.visible || k0 > pos_hi - p.window))) {
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    const bool page_ok = (unsigned)pg[t] < (unsigned)p.c.pages;
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int k = k0 + 16 * t + 4 * g + r;
-#pragma unroll
-                        for (int n = 0; n < NT; ++n) {
-                            bool ok = k <= pos[n];
-                            if (p.visible) {
-                                const int bit = k - before;
-                                ok = ok || (bit >= 0 && bit < 64 && (seen[n] >> (bit & 63) & 1));
-                            } else if (p.window > 0) {
-                                ok = ok && ((int64_t)k > (int64_t)pos[n] - p.window || k < p.sinks);
-                            }
-                            sc[n][t][r] = ok && page_ok && k < span.end ? sc[n][t][r] : -__builtin_inff();
-                        }
-                    }
-                }
+                for (int j = 0; j < 8; ++j) acc[n][j] *= f;
+                weigh<8>(s8, by, vs, ref[n], prod, sum);
             }
-            float vs[8];
-            half2v vz[4];
+            total[n] += sum;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) vs[k] = step_of(s.vs[k >> 2][k & 3]);
+            for (int k = 0; k < 8; ++k) {
+                pw[n][k] = (_Float16)prod[k];
+                zeros[n] = __builtin_fmaf((float)pw[n][k], vz[k], zeros[n]);
+            }
+        }
+        auto values = [&](auto part) {
+            constexpr int HALF = decltype(part)::value;
+            uint32_t vv[4][4];
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-                vz[k] = as_half2((__builtin_amdgcn_perm(s.vs[k >> 1][2 * (k & 1) + 1], s.vs[k >> 1][2 * (k & 1)], 0x07060302u) & 0x000F000Fu) | 0x64006400u) -
-                        (half2v)(_Float16)1024.0f;
-            half8 pw[NT];
+                ValueCodes<VB>::template fields<HALF>(ring_value<VB>(slot + R::V_AT + (k >> 1) * R::V_PIECE, i, g, 2 * (k & 1)),
+                                                      ring_value<VB>(slot + R::V_AT + (k >> 1) * R::V_PIECE, i, g, 2 * (k & 1) + 1), vv[k]);
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                float e[8], prod[8];
-                auto weigh = [&]() {
+            for (int j = 0; j < 4; ++j) {
+                const u32x4 a = {vv[0][j], vv[1][j], vv[2][j], vv[3][j]};
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        const float x = sc[n][k >> 2][k & 3];
-                        e[k] = __builtin_amdgcn_exp2f(x - ref[n]);
-                        prod[k] = x == -__builtin_inff() ? 0.0f : e[k] * vs[k];   // what is not visible may have any step
-                    }
-                };
-                weigh();
-                float big = 0.0f, bigp = 0.0f;
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    big = __builtin_fmaxf(big, e[k]);
-                    bigp = __builtin_fmaxf(bigp, prod[k]);
-                }
-                if (__any(bigp > 32768.0f || big > 0x1p40f)) {
-                    float top = ATT_NONE;
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) top = __builtin_fmaxf(top, sc[n][k >> 2][k & 3] + __builtin_fmaxf(__builtin_amdgcn_logf(vs[k]), -25.0f));
-                    top = across_groups(top, fmax_op) - 7.0f;
-                    const float to = __builtin_fmaxf(ref[n], top), f = __builtin_amdgcn_exp2f(ref[n] - to);
-                    ref[n] = to;
-                    total[n] *= f;
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) acc[n][j] *= f;
-                    weigh();
-                }
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    total[n] += e[k];
-                    pw[n][k] = (_Float16)prod[k];
-                }
-            }
-            half2v vv[4][8];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                uint32_t a = s.v[2 * k], z = s.v[2 * k + 1];
-                if constexpr (VB == 3) {
-                    const int sh = i < 15 ? 0 : 8;
-                    a >>= sh;
-                    z >>= sh;
-                }
-                value_pairs<VB>(a, z, vz[k], vv[k]);
-            }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const u32x4 a = {as_u32(vv[0][j]), as_u32(vv[1][j]), as_u32(vv[2][j]), as_u32(vv[3][j])};
-#pragma unroll
-                for (int n = 0; n < NT; ++n) acc[n][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, a), pw[n], acc[n][j], 0, 0, 0);
+                for (int n = 0; n < NT; ++n)
+                    acc[n][4 * HALF + j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, a), pw[n], acc[n][4 * HALF + j], 0, 0, 0);
             }
         };
-
-        int x = (int)blockIdx.z * per + w;
-        if (x < x_end) {
-            StepCodes<KB, VB> cur, nxt;
-            int pc[2], pn[2], pf[2];
-            pages_of(x, pc);
-            pages_of(x + ATT_WAVES, pn);
-            load(x, pc, cur);
-            while (x < x_end) {
-                pages_of(x + 2 * ATT_WAVES, pf);
-                load(x + ATT_WAVES, pn, nxt);
-                work(x, pc, cur);
-                cur = nxt;
-                pc[0] = pn[0]; pc[1] = pn[1];
-                pn[0] = pf[0]; pn[1] = pf[1];
-                x += ATT_WAVES;
-            }
-        }
-
-        // ---- the waves meet
-        __syncthreads();                                                       // of an earlier tile's reads
+        values(std::integral_constant<int, 0>{});
+        __builtin_amdgcn_sched_barrier(0);                                 // (four channels' fragments at a time: registers)
+        values(std::integral_constant<int, 1>{});
+    };
+    if (any) {
+        int slot = 0;
+        for (; x < x_end; x += NW) {
+            wait_vm_pending<(DEPTH - 1) * R::LOADS>();
+            int next[2];
+            pages_of(x + NW * (DEPTH + 1), next);
+            work(x, pg[0], ring + slot * R::SLOT);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");                 // the slot has been read: it may take another step
+            load(x + NW * DEPTH, pg[DEPTH], slot);
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            total[n] = across_groups(total[n], fadd_op);
-            if (g == 0) {
-                refs[w][16 * n + i] = ref[n];
-                totals[w][16 * n + i] = total[n];
+            for (int k = 0; k < DEPTH; ++k) {
+                pg[k][0] = pg[k + 1][0];
+                pg[k][1] = pg[k + 1][1];
             }
+            pg[DEPTH][0] = next[0];
+            pg[DEPTH][1] = next[1];
+            slot = slot + 1 == DEPTH ? 0 : slot + 1;
         }
+        wait_vm_pending<0>();                                                  // nothing may still be on its way into LDS
+    }
+
+    // ---- the waves meet
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        total[n] = across_groups(total[n], fadd_op);
+        zeros[n] = across_groups(zeros[n], fadd_op);
+        if (g == 0) {
+            refs[w][16 * n + i] = ref[n];
+            totals[w][16 * n + i] = total[n];
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        float top = refs[0][16 * n + i];
+#pragma unroll
+        for (int k = 1; k < NW; ++k) top = __builtin_fmaxf(top, refs[k][16 * n + i]);
+        const float f = __builtin_amdgcn_exp2f(ref[n] - top);
+        if (n > 0) __syncthreads();
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                f32x4 o;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    o[j] = __builtin_fmaf(acc[n][4 * half + j][r], (float)(1 << (24 - ValueCodes<VB>::shift(4 * half + j))), -zeros[n]) * f;
+                *reinterpret_cast<f32x4*>(&sums[w][i][8 * (4 * g + r) + 4 * half]) = o;
+            }
         __syncthreads();
-        for (int n = 0; n < NT; ++n) {
-            float top = refs[0][16 * n + i];
+        // 16 rows of 128 channels: 2048 / (64 NW) channels a thread
+        constexpr int CH = 32 / NW;
+        const int rr = threadIdx.x / (ATT_D / CH), d = CH * (threadIdx.x % (ATT_D / CH));
+        float ref_all = refs[0][16 * n + rr], sum = 0.0f, o[CH] = {};
 #pragma unroll
-            for (int k = 1; k < ATT_WAVES; ++k) top = __builtin_fmaxf(top, refs[k][16 * n + i]);
-            const float f = __builtin_amdgcn_exp2f(ref[n] - top);
-            if (n > 0) __syncthreads();
+        for (int k = 1; k < NW; ++k) ref_all = __builtin_fmaxf(ref_all, refs[k][16 * n + rr]);
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
+        for (int k = 0; k < NW; ++k) {
+            sum += totals[k][16 * n + rr] * __builtin_amdgcn_exp2f(refs[k][16 * n + rr] - ref_all);
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    f32x4 o;
+            for (int e = 0; e < CH; ++e) o[e] += sums[k][rr][d + e];
+        }
+        const int r = row0 + 16 * n + rr;
+        if (r < row_end) {
+            const int64_t token = seq.first + r / p.G;
+            const int hq = head * p.G + r % p.G;
+            if (!partial) {
+                const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+                typedef _Float16 halves __attribute__((ext_vector_type(CH)));
+                halves y;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) o[j] = acc[n][4 * half + j][r] * f;
-                    *reinterpret_cast<f32x4*>(&sums[w][i][8 * (4 * g + r) + 4 * half]) = o;
-                }
-            __syncthreads();
-            const int rr = threadIdx.x >> 4, d = 8 * (threadIdx.x & 15);
-            float ref_all = refs[0][16 * n + rr], sum = 0.0f, o[8] = {};
+                for (int e = 0; e < CH; ++e) y[e] = (_Float16)(o[e] * inv);
+                *reinterpret_cast<halves*>(p.out + token * p.out_stride + hq * ATT_D + d) = y;
+            } else {
+                typedef float floats __attribute__((ext_vector_type(CH)));
+                const int64_t at = partial_at + 16 * n + rr;
+                floats y;
 #pragma unroll
-            for (int k = 1; k < ATT_WAVES; ++k) ref_all = __builtin_fmaxf(ref_all, refs[k][16 * n + rr]);
-#pragma unroll
-            for (int k = 0; k < ATT_WAVES; ++k) {
-                sum += totals[k][16 * n + rr] * __builtin_amdgcn_exp2f(refs[k][16 * n + rr] - ref_all);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) o[e] += sums[k][rr][d + e];
+                for (int e = 0; e < CH; ++e) y[e] = o[e];
+                *reinterpret_cast<floats*>(p.part + at * ATT_D + d) = y;
+                if (d == 0) reinterpret_cast<float2*>(p.stats)[at] = float2{ref_all, sum};
             }
-            const int64_t r = row0 + 16 * n + rr;
-            if (r < row_end) {
-                const int64_t token = seq.first + r / p.G;
-                const int hq = head * p.G + (int)(r % p.G);
-                if (used == 1) {
-                    const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
-                    half8 y;
+        }
+    }
+    __syncthreads();                                                           // what follows fills the ring again
+}
+
+// A tile of rows, and the steps of the rows' span, of a sequence of few rows.
+struct Tile {
+    int row0, row_end;
+    Span span;
+};
+template <int ROWS>
+__device__ __forceinline__ Tile tile_of(const AttnDev& p, const Sequence& seq, int tile) {
+    Tile t;
+    const int all = seq.rows * p.G, before = seq.length - seq.rows;
+    t.row0 = tile * ROWS;
+    t.row_end = t.row0 + ROWS < all ? t.row0 + ROWS : all;
+    t.span = span_of(p, seq.length, before + t.row0 / p.G, before + (t.row_end - 1) / p.G);
+    return t;
+}
+
+// blockIdx: (sequence and head, tile of rows).
+template <int KB, int VB, int NT, int NW>
+__global__ __launch_bounds__(64 * NW, NW == 16 ? 4 : NT == 1 ? 3 : 2) void whole_attention_kernel(AttnDev p) {
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    const int b = blockIdx.x / p.c.H, head = blockIdx.x - b * p.c.H;
+    const Sequence seq = sequence_of(p.c, b);
+    const int tiles = (seq.rows * p.G + 16 * NT - 1) / (16 * NT);
+    for (int tile = blockIdx.y; tile < tiles; tile += gridDim.y) {
+        const Tile t = tile_of<16 * NT>(p, seq, tiles - 1 - tile);             // the last rows, which see most, first
+        few_rows<KB, VB, NT, NW>(p, smem, b, head, seq, t.row0, t.row_end, t.span, 0, t.span.steps, false, 0);
+    }
+}
+
+// The balanced launch: the steps of all sequences and heads behind each other, in units of 4 (128 tokens), are cut into gridDim.x equal stretches, whatever
+// the lengths.  A workgroup goes through the (sequence, head) pairs of its stretch; the first and the last may be shared with its neighbours, and leave
+// partial results in the workgroup's two places.  Every wave works the cut out for itself: a lane holds four sequences.
+// A sequence that has none of the units is gone through whole, a head a workgroup.
+constexpr int kBalancedSequences = 256;
+struct Cut {
+    int units[4], sum;        // of the lane's four sequences, all heads; of the sequences of the lanes before
+    int all, per;             // of all; of a workgroup
+};
+// Units of one head of a sequence (one for rows that see nothing: they still have an output); 0: not among the units, because it has no rows, more of them
+// than a tile, or so many tokens that the units of all sequences would pass 32 bits.
+template <int ROWS>
+__device__ __forceinline__ int share_of(const AttnDev& p, const Sequence& seq) {
+    if (seq.rows <= 0 || seq.rows * p.G > ROWS) return 0;
+    const int n = (tile_of<ROWS>(p, seq, 0).span.steps + 3) >> 2;
+    return n > 0x7fffffff / kBalancedSequences / p.c.H ? 0 : n > 1 ? n : 1;
+}
+template <int ROWS>
+__device__ __forceinline__ Cut cut_of(const AttnDev& p, int workgroups) {
+    const int l = threadIdx.x & 63;
+    Cut c;
+    int mine = 0;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) y[e] = (_Float16)(o[e] * inv);
-                    *reinterpret_cast<half8*>(p.out + token * p.out_stride + hq * ATT_D + d) = y;
-                } else {
-                    const int64_t at = (token * p.Hq + hq) * p.splits + blockIdx.z;
-                    float* dst = p.part + at * ATT_D + d;
-                    *reinterpret_cast<f32x4*>(dst) = f32x4{o[0], o[1], o[2], o[3]};
-                    *reinterpret_cast<f32x4*>(dst + 4) = f32x4{o[4], o[5], o[6], o[7]};
-                    if (d == 0) {
-                        float* pair = p.part + p.c.T * p.Hq * p.splits * ATT_D + 2 * at;
-                        pair[0] = ref_all;
-                        pair[1] = sum;
-                    }
-                }
-            }
+    for (int k = 0; k < 4; ++k) {
+        const int b = 4 * l + k;
+        c.units[k] = 0;
+        if (b < p.c.B) {
+            Sequence seq;
+            const int first = p.c.row_starts[b], last = p.c.row_starts[b + 1], T = (int)p.c.T;
+            seq.length = p.c.lengths[b];
+            seq.first = first > 0 ? first : 0;
+            seq.rows = (last < T ? last : T) - seq.first;
+            c.units[k] = share_of<ROWS>(p, seq) * p.c.H;
+        }
+        mine += c.units[k];
+    }
+    int sum = mine;
+#pragma unroll
+    for (int m = 1; m < 64; m *= 2) {
+        const int other = __shfl_up(sum, m);
+        sum += l >= m ? other : 0;
+    }
+    c.sum = sum - mine;
+    c.all = __builtin_amdgcn_readlane(sum, 63);
+    c.per = (c.all + workgroups - 1) / workgroups;
+    c.per = c.per > p.min_units ? c.per : p.min_units;
+    return c;
+}
+// First unit of sequence b (uniform), and the sequence that has unit u.
+__device__ __forceinline__ int first_unit(const Cut& c, int b) {
+    int at = c.sum;
+#pragma unroll
+    for (int k = 0; k < 3; ++k) at += (b & 3) > k ? c.units[k] : 0;
+    return __builtin_amdgcn_readlane(at, b >> 2);
+}
+__device__ __forceinline__ int sequence_at(const Cut& c, int u) {
+    const int lane = __builtin_popcountll(__ballot(c.sum <= u)) - 1;          // the last lane whose sequences begin at u or before
+    int at = __builtin_amdgcn_readlane(c.sum, lane), b = 4 * lane;
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+        at += __builtin_amdgcn_readlane(c.units[k], lane);
+        if (at <= u) b = 4 * lane + k + 1;
+    }
+    return b;
+}
+
+template <int KB, int VB, int NT, int NW>
+__global__ __launch_bounds__(64 * NW, NT == 1 ? 3 : 2) void balanced_attention_kernel(AttnDev p) {
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    constexpr int ROWS = 16 * NT;
+    const Cut cut = cut_of<ROWS>(p, gridDim.x);
+    const int wg = blockIdx.x, begin = wg * cut.per, end = min(begin + cut.per, cut.all);
+    for (int u = begin; u < end;) {
+        const int b = sequence_at(cut, u), first = first_unit(cut, b);
+        const Sequence seq = sequence_of(p.c, b);
+        const Tile t = tile_of<ROWS>(p, seq, 0);
+        const int n = share_of<ROWS>(p, seq), head = (u - first) / n, from = u - first - head * n;
+        const int to = min(n, from + end - u);
+        const bool partial = from > 0 || to < n;
+        few_rows<KB, VB, NT, NW>(p, smem, b, head, seq, t.row0, t.row_end, t.span, 4 * from, min(t.span.steps, 4 * to), partial,
+                                 ((int64_t)2 * wg + (u == begin ? 0 : 1)) * ROWS);
+        u += to - from;
+    }
+    for (int bh = wg; bh < p.c.B * p.c.H; bh += gridDim.x) {                   // what is not among the units
+        const int b = bh / p.c.H;
+        const Sequence seq = sequence_of(p.c, b);
+        const int tiles = (seq.rows * p.G + ROWS - 1) / ROWS;
+        if (tiles < 1 || share_of<ROWS>(p, seq)) continue;
+        for (int tile = 0; tile < tiles; ++tile) {
+            const Tile t = tile_of<ROWS>(p, seq, tile);
+            few_rows<KB, VB, NT, NW>(p, smem, b, bh - b * p.c.H, seq, t.row0, t.row_end, t.span, 0, t.span.steps, false, 0);
         }
     }
 }
 
-// Joins the splits of every (row, query head) that has more than one: one wave each, two channels a lane.
+// Joins the partial results of row r of every (sequence, head) pair that more than one workgroup had: blockIdx (pair, row).  The waves take the workgroups in turn.
+template <int NT>
+__global__ __launch_bounds__(ATT_NT) void balanced_join_kernel(AttnDev p, int workgroups) {
+    __shared__ float tops[ATT_WAVES], totals[ATT_WAVES], sums[ATT_WAVES][ATT_D];
+    constexpr int ROWS = 16 * NT;
+    const int l = threadIdx.x & 63;
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int b = blockIdx.x / p.c.H, head = blockIdx.x - b * p.c.H;
+    const Sequence seq = sequence_of(p.c, b);
+    const Cut cut = cut_of<ROWS>(p, workgroups);
+    const int n = share_of<ROWS>(p, seq), u = first_unit(cut, b) + head * n;
+    const int first = u / cut.per, last = (u + n - 1) / cut.per;
+    if (n == 0 || first == last) return;
+    for (int r = blockIdx.y; r < seq.rows * p.G; r += gridDim.y) {
+        auto place = [&](int wg) { return ((int64_t)2 * wg + (wg > first || u == first * cut.per ? 0 : 1)) * ROWS + r; };
+        // each wave its workgroups, eight at a time, with a reference of its own
+        float top = ATT_NONE, sum = 0.0f, o0 = 0.0f, o1 = 0.0f;
+        for (int k = first + w; k <= last; k += 8 * ATT_WAVES) {
+            float2 s[8], v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int64_t at = place(min(k + ATT_WAVES * e, last));
+                s[e] = reinterpret_cast<const float2*>(p.stats)[at];
+                v[e] = reinterpret_cast<const float2*>(p.part + at * ATT_D)[l];
+            }
+            float to = top;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) to = __builtin_fmaxf(to, s[e].x);
+            const float f = __builtin_amdgcn_exp2f(top - to);
+            top = to;
+            sum *= f;
+            o0 *= f;
+            o1 *= f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float g = k + ATT_WAVES * e <= last ? __builtin_amdgcn_exp2f(s[e].x - to) : 0.0f;
+                sum += s[e].y * g;
+                o0 += v[e].x * g;
+                o1 += v[e].y * g;
+            }
+        }
+        if (l == 0) {
+            tops[w] = top;
+            totals[w] = sum;
+        }
+        reinterpret_cast<float2*>(sums[w])[l] = float2{o0, o1};
+        __syncthreads();
+        if (w == 0) {
+            float all = tops[0];
+#pragma unroll
+            for (int k = 1; k < ATT_WAVES; ++k) all = __builtin_fmaxf(all, tops[k]);
+            sum = o0 = o1 = 0.0f;
+#pragma unroll
+            for (int k = 0; k < ATT_WAVES; ++k) {
+                const float f = __builtin_amdgcn_exp2f(tops[k] - all);
+                const float2 v = reinterpret_cast<const float2*>(sums[k])[l];
+                sum += totals[k] * f;
+                o0 += v.x * f;
+                o1 += v.y * f;
+            }
+            const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+            const int64_t token = seq.first + r / p.G;
+            reinterpret_cast<half2v*>(p.out + token * p.out_stride + (head * p.G + r % p.G) * ATT_D)[l] = half2v{(_Float16)(o0 * inv), (_Float16)(o1 * inv)};
+        }
+        __syncthreads();
+    }
+}
+
+// ---- many rows: the tokens' codes become fp16 once per workgroup
+//
+// Four waves of 32 rows each on v_mfma_f32_32x32x16_f16, 64 tokens a step: waves 0 and 1 turn the keys of one half of them into fp16,
+// waves 2 and 3 the values, into the LDS buffer of the next step.  Keys lie row by row in the order of their codes, values channel by
+// channel with the eight tokens of a fragment (those whose weights a lane holds) in 16 bytes; 16-byte chunks are exchanged by row so that
+// the reads of a fragment spread over all banks.
+
+constexpr int SH_ROWS = 32;                // rows per wave
+constexpr int SH_K_BYTES = 64 * ATT_D * 2, SH_V_BYTES = ATT_D * 64 * 2, SH_STEP_BYTES = 2 * 64 * 4;
+constexpr int SH_BUFFER = SH_K_BYTES + SH_V_BYTES + SH_STEP_BYTES;
+constexpr int SH_LDS = 2 * SH_BUFFER;
+
+// A thread's share of 64 tokens: two quarters of a key, or eight channels of eight values, and which of the four pages of 16 tokens are pages.
+struct ShareCodes {
+    uint32_t w[8], params[8];
+    int pages;                             // (uniform) bit k: tokens 16 k .. of the 64
+};
+
+template <int KB, int VB>
+__global__ __launch_bounds__(ATT_NT, 2) void shared_attention_kernel(AttnDev p) {
+    extern __shared__ __attribute__((aligned(16))) unsigned char sh_smem[];
+    const int l = threadIdx.x & 63, c = l & 31, h = l >> 5;
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int b = blockIdx.x / p.c.H, head = blockIdx.x - b * p.c.H;
+    const Sequence seq = sequence_of(p.c, b);
+    const int all_rows = seq.rows * p.G;
+    constexpr int TILE = SH_ROWS * ATT_WAVES;
+    const int tiles = (all_rows + TILE - 1) / TILE;
+    const list_t table = (list_t)p.c.page_table + b * p.c.table_stride;
+    for (int tile_no = blockIdx.y; tile_no < tiles; tile_no += gridDim.y) {
+        const int row0 = (tiles - 1 - tile_no) * TILE;
+        const int row_end = row0 + TILE < all_rows ? row0 + TILE : all_rows;
+        const int before = seq.length - seq.rows;
+        const Span span = span_of(p, seq.length, before + row0 / p.G, before + (row_end - 1) / p.G);
+        const int used = splits_used(p, span.steps);
+        if ((int)blockIdx.z >= used) continue;
+        const int per = p.chunk / ATT_STEP;
+        const int x_begin = (int)blockIdx.z * per;
+        const int x_end = (int)blockIdx.z == p.splits - 1 ? span.steps : min(span.steps, x_begin + per);
+
+        // this wave's rows
+        const int wrow0 = row0 + SH_ROWS * w, wrow_end = wrow0 + SH_ROWS < row_end ? wrow0 + SH_ROWS : row_end;
+        const bool busy = wrow0 < wrow_end;
+        const int pos_lo = before + wrow0 / p.G, pos_hi = before + (wrow_end - 1) / p.G;
+        int r = wrow0 + c;
+        r = r < row_end ? r : row_end - 1;
+        const int token = r / p.G, sub = r - token * p.G;
+        const int pos = p.visible ? before - 1 : before + token;
+        const uint64_t seen = p.visible ? p.visible[seq.first + token] : 0;
+        half8 q[8];                                                            // fragment k: chunk 2 k + h of the key rows
+        {
+            const _Float16* src = p.q + (seq.first + token) * p.q_stride + (head * p.G + sub) * ATT_D;
+#pragma unroll
+            for (int quarter = 0; quarter < 4; ++quarter) {
+                half8 raw[4];
+#pragma unroll
+                for (int m = 0; m < 4; ++m) raw[m] = *reinterpret_cast<const half8*>(src + 32 * quarter + 8 * m);
+                auto pick = [&](int at) { return raw[at >> 3][at & 7]; };
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int lo = 8 * k + e, hi = lo + 4;                 // pairs of chunk 2 k and of chunk 2 k + 1
+                        q[2 * quarter + k][2 * e] = h ? pick(KeyCodes<KB>::first(hi)) : pick(KeyCodes<KB>::first(lo));
+                        q[2 * quarter + k][2 * e + 1] = h ? pick(KeyCodes<KB>::second(hi)) : pick(KeyCodes<KB>::second(lo));
+                    }
+            }
+        }
+        f32x16 acc[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int k = 0; k < 16; ++k) acc[t][k] = 0.0f;
+        float ref = ATT_NONE, total = 0.0f;
+
+        // codes of steps x and x + 1 of the span, 32 tokens each, which need not follow each other
+        auto load = [&](int x, ShareCodes& s) {
+            int pg[4], k0[2];
+            s.pages = 0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int xx = x + (k >> 1) < span.steps ? x + (k >> 1) : span.steps - 1;
+                k0[k >> 1] = span.token(xx);
+                const int j = (k0[k >> 1] + 16 * (k & 1)) >> p.c.page_shift;
+                pg[k] = table[j < p.c.table_width ? j : p.c.table_width - 1];  // (behind the width: behind the end)
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const bool ok = (unsigned)pg[k] < (unsigned)p.c.pages;
+                s.pages |= (int)ok << k;
+                pg[k] = ok ? pg[k] : 0;
+            }
+            const int mine = w & 1, mask = (1 << p.c.page_shift) - 1;
+            if (w < 2) {                                                       // token c of the half, quarters 2 h and 2 h + 1
+                const int64_t at = (((int64_t)(c < 16 ? pg[2 * mine] : pg[2 * mine + 1]) * p.c.H + head) << p.c.page_shift) + ((k0[mine] + c) & mask);
+                __builtin_memcpy(s.w, __builtin_assume_aligned(p.c.codes[0] + at * (16 * KB) + h * (8 * KB), 8), 8 * KB);
+                s.params[0] = p.c.params[0][at];
+            } else {                                                           // channels 8 i .. 8 i + 7 of tokens 16 (g >> 1) + 4 (g & 1) + {0 .. 3, 8 .. 11}
+                const int i = l & 15, g = l >> 4;
+                const int64_t at = (((int64_t)(g < 2 ? pg[2 * mine] : pg[2 * mine + 1]) * p.c.H + head) << p.c.page_shift) +
+                                   ((k0[mine] + 16 * (g >> 1) + 4 * (g & 1)) & mask);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const uint8_t* row = p.c.codes[1] + (at + (k & 3) + 8 * (k >> 2)) * (16 * VB);
+                    if constexpr (VB == 4) s.w[k] = reinterpret_cast<const uint32_t*>(row)[i];
+                    else if constexpr (VB == 2) s.w[k] = reinterpret_cast<const uint16_t*>(row)[i];
+                    else __builtin_memcpy(&s.w[k], row + (i < 15 ? 3 * i : 44), 4);
+                }
+                const u32x4 lo = *reinterpret_cast<const u32x4*>(p.c.params[1] + at), hi = *reinterpret_cast<const u32x4*>(p.c.params[1] + at + 8);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    s.params[k] = lo[k];
+                    s.params[4 + k] = hi[k];
+                }
+            }
+        };
+        auto convert = [&](const ShareCodes& s, int buf) {
+            unsigned char* base = sh_smem + buf * SH_BUFFER;
+            float* steps = reinterpret_cast<float*>(base + SH_K_BYTES + SH_V_BYTES);
+            if (w < 2) {
+                const half2v z = raised_zeros(s.params[0], s.params[0]);
+                const int tok = 32 * w + c;
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    typename KeyCodes<KB>::words cw;
+#pragma unroll
+                    for (int k = 0; k < KB; ++k) cw[k] = s.w[KB * half + k];
+                    uint32_t kk[16];
+                    KeyCodes<KB>::fields(cw, kk);
+                    each<4>([&](auto mm) {
+                        constexpr int m = decltype(mm)::value;
+                        const int chunk = 4 * (2 * h + half) + m;
+                        u32x4 o;
+                        each<4>([&](auto ee) {
+                            constexpr int e = decltype(ee)::value;
+                            o[e] = as_u32(code_value<KeyCodes<KB>::shift(4 * m + e)>(kk[4 * m + e], z));
+                        });
+                        *reinterpret_cast<u32x4*>(base + tok * 256 + ((chunk ^ (tok & 15)) << 4)) = o;
+                    });
+                }
+                if (h == 0) steps[tok] = step_of(s.params[0]) * p.scale2;
+            } else {
+                const int i = l & 15, g = l >> 4, chunk = 4 * (w - 2) + g;
+                auto values = [&](auto part) {
+                    constexpr int HALF = decltype(part)::value;
+                    uint32_t vv[4][4];
+                    half2v z[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        z[k] = raised_zeros(s.params[2 * k], s.params[2 * k + 1]);
+                        const int down = VB == 3 && i == 15 ? 8 : 0;
+                        ValueCodes<VB>::template fields<HALF>(s.w[2 * k] >> down, s.w[2 * k + 1] >> down, vv[k]);
+                    }
+                    each<4>([&](auto jj) {
+                        constexpr int j = decltype(jj)::value;
+                        const int d = 8 * i + 4 * HALF + j;
+                        u32x4 o;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) o[k] = as_u32(code_value<ValueCodes<VB>::shift(4 * HALF + j)>(vv[k][j], z[k]));
+                        *reinterpret_cast<u32x4*>(base + SH_K_BYTES + d * 128 + ((chunk ^ ((d >> 3 ^ d) & 7)) << 4)) = o;
+                    });
+                };
+                values(std::integral_constant<int, 0>{});
+                values(std::integral_constant<int, 1>{});
+                if (i < 8) {
+                    float st = 0.0f;
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) st = i == k ? step_of(s.params[k]) : st;
+                    steps[64 + 32 * (w - 2) + 16 * (g >> 1) + 4 * (g & 1) + (i & 3) + 8 * (i >> 2)] = st;
+                }
+            }
+        };
+        auto work = [&](int x, int buf, int pages) {
+            const unsigned char* base = sh_smem + buf * SH_BUFFER;
+            const float* steps = reinterpret_cast<const float*>(base + SH_K_BYTES + SH_V_BYTES) + 4 * h;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                if (x + t >= x_end) break;
+                const int k0 = span.token(x + t);
+                if (!p.visible && k0 > pos_hi) break;                          // (the first tokens lie before everything else)
+                f32x16 sc;
+#pragma unroll
+                for (int k = 0; k < 16; ++k) sc[k] = 0.0f;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const half8 a = *reinterpret_cast<const half8*>(base + (32 * t + c) * 256 + (((2 * k + h) ^ (c & 15)) << 4));
+                    sc = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, q[k], sc, 0, 0, 0);
+                }
+                float vs[16], fk[16];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const f32x4 a = *reinterpret_cast<const f32x4*>(steps + 32 * t + 8 * k), z = *reinterpret_cast<const f32x4*>(steps + 64 + 32 * t + 8 * k);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        fk[4 * k + e] = a[e];
+                        vs[4 * k + e] = z[e];
+                    }
+                }
+                const int pages_ok = pages >> (2 * t) & 3, all_see = p.visible ? before - 1 : pos_lo;
+                if (!(pages_ok == 3 && k0 + 31 <= all_see && k0 + 32 <= span.end && (p.window <= 0 || p.visible || k0 > pos_hi - p.window))) {
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) {
+                        const int kk = k0 + 8 * (k >> 2) + 4 * h + (k & 3);
+                        const bool ok = sees(p, kk, pos, before, seen) && (pages_ok >> (k >> 3) & 1) && kk < span.end;
+                        sc[k] = ok ? sc[k] * fk[k] : -__builtin_inff();
+                        fk[k] = 1.0f;
+                        vs[k] = finite_step(vs[k]);
+                    }
+                }
+                float prod[16], sum;
+                auto by = [&](int k) { return fk[k]; };
+                if (weigh<16>(sc, by, vs, ref, prod, sum)) {
+                    const float f = raise_reference<16>(sc, by, vs, ref, [](float top) { return __builtin_fmaxf(top, __shfl_xor(top, 32)); });
+                    total *= f;
+#pragma unroll
+                    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) acc[dt][k] *= f;
+                    weigh<16>(sc, by, vs, ref, prod, sum);
+                }
+                total += sum;
+                half8 pw[2];
+#pragma unroll
+                for (int k = 0; k < 16; ++k) pw[k >> 3][k & 7] = (_Float16)prod[k];
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int dt = 0; dt < 4; ++dt) {
+                        const int d = 32 * dt + c;
+                        const half8 a = *reinterpret_cast<const half8*>(base + SH_K_BYTES + d * 128 + (((4 * t + 2 * s + h) ^ ((d >> 3 ^ d) & 7)) << 4));
+                        acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, pw[s], acc[dt], 0, 0, 0);
+                    }
+            }
+        };
+
+        if (x_begin < x_end) {
+            ShareCodes s;
+            load(x_begin, s);
+            convert(s, 0);
+            int pages = s.pages;
+            load(x_begin + 2, s);
+            __syncthreads();
+            int buf = 0;
+            for (int x = x_begin; x < x_end; x += 2) {
+                if (busy) work(x, buf, pages);
+                convert(s, buf ^ 1);
+                pages = s.pages;
+                load(x + 4, s);
+                __syncthreads();
+                buf ^= 1;
+            }
+        }
+        total += __shfl_xor(total, 32);
+        if (wrow0 + c < wrow_end) {
+            const int64_t row_token = seq.first + token;
+            const int hq = head * p.G + sub;
+            if (used == 1) {
+                const float inv = total > 0.0f ? 1.0f / total : 0.0f;
+                _Float16* dst = p.out + row_token * p.out_stride + hq * ATT_D;
+#pragma unroll
+                for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        typedef _Float16 half4 __attribute__((ext_vector_type(4)));
+                        half4 y;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) y[e] = (_Float16)(acc[dt][4 * k + e] * inv);
+                        *reinterpret_cast<half4*>(dst + 32 * dt + 8 * k + 4 * h) = y;
+                    }
+            } else {
+                const int64_t at = (row_token * p.Hq + hq) * p.splits + blockIdx.z;
+                float* dst = p.part + at * ATT_D;
+#pragma unroll
+                for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        *reinterpret_cast<f32x4*>(dst + 32 * dt + 8 * k + 4 * h) = f32x4{acc[dt][4 * k], acc[dt][4 * k + 1], acc[dt][4 * k + 2], acc[dt][4 * k + 3]};
+                if (h == 0) {
+                    reinterpret_cast<float2*>(p.stats)[at] = float2{ref, total};
+                }
+            }
+        }
+        __syncthreads();                                                       // the next tile writes buffer 0
+    }
+}
+
+// Joins the splits of every (row, query head) that has more than one: one wave each, two channels a lane.  ROWS: of the tiles that were split.
 template <int ROWS>
 __global__ __launch_bounds__(ATT_NT) void attention_join_kernel(AttnDev p) {
     const int l = threadIdx.x & 63;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int b = blockIdx.x / p.c.H, head = blockIdx.x - b * p.c.H;
     const Sequence seq = sequence_of(p.c, b);
-    const int64_t all_rows = (int64_t)seq.rows * p.G;
-    const int tiles = (int)((all_rows + ROWS - 1) / ROWS);
-    for (int tile = blockIdx.y; tile < tiles; tile += gridDim.y) {
-        const int64_t row0 = (int64_t)tile * ROWS, row_end = row0 + ROWS < all_rows ? row0 + ROWS : all_rows;
+    const int all_rows = seq.rows * p.G;
+    for (int r = (int)blockIdx.y * ATT_WAVES + w; r < all_rows; r += (int)gridDim.y * ATT_WAVES) {
+        const int row0 = r / ROWS * ROWS, row_end = row0 + ROWS < all_rows ? row0 + ROWS : all_rows;
         const int before = seq.length - seq.rows;
-        const Span span = span_of(p, seq.length, before + (int)(row0 / p.G), before + (int)((row_end - 1) / p.G));
+        const Span span = span_of(p, seq.length, before + row0 / p.G, before + (row_end - 1) / p.G);
         const int used = splits_used(p, span.steps);
         if (used == 1) continue;
-        for (int64_t r = row0 + w + (int64_t)ATT_WAVES * blockIdx.z; r < row_end; r += ATT_WAVES * gridDim.z) {
-            const int64_t token = seq.first + r / p.G;
-            const int hq = head * p.G + (int)(r % p.G);
-            const int64_t at = (token * p.Hq + hq) * p.splits;
-            const float2* pair = reinterpret_cast<const float2*>(p.part + p.c.T * p.Hq * p.splits * ATT_D) + at;
-            float top = ATT_NONE;
-            for (int k = 0; k < used; ++k) top = __builtin_fmaxf(top, pair[k].x);
-            float sum = 0.0f, o0 = 0.0f, o1 = 0.0f;
-            for (int k = 0; k < used; ++k) {
-                const float2 e = pair[k], v = reinterpret_cast<const float2*>(p.part + (at + k) * ATT_D)[l];
-                const float f = __builtin_amdgcn_exp2f(e.x - top);
-                sum += e.y * f;
-                o0 += v.x * f;
-                o1 += v.y * f;
-            }
-            const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
-            reinterpret_cast<half2v*>(p.out + token * p.out_stride + hq * ATT_D)[l] = half2v{(_Float16)(o0 * inv), (_Float16)(o1 * inv)};
+        const int64_t token = seq.first + r / p.G;
+        const int hq = head * p.G + r % p.G;
+        const int64_t at = (token * p.Hq + hq) * p.splits;
+        const float2* pair = reinterpret_cast<const float2*>(p.stats) + at;
+        const float2* part = reinterpret_cast<const float2*>(p.part + at * ATT_D) + l;
+        // the splits' references and sums, a split a lane (kMaxSplits of them at most), and their factors
+        float2 mine[kMaxSplits / 64];
+        float top = ATT_NONE, sum = 0.0f, f[kMaxSplits / 64];
+#pragma unroll
+        for (int k = 0; k < kMaxSplits / 64; ++k) {
+            mine[k] = 64 * k + l < used ? pair[64 * k + l] : float2{ATT_NONE, 0.0f};
+            top = __builtin_fmaxf(top, mine[k].x);
         }
+        top = wave_max(top);
+#pragma unroll
+        for (int k = 0; k < kMaxSplits / 64; ++k) {
+            f[k] = __builtin_amdgcn_exp2f(mine[k].x - top);
+            sum += mine[k].y * f[k];
+        }
+#pragma unroll
+        for (int m = 1; m < 64; m *= 2) sum += __shfl_xor(sum, m);
+        float o0 = 0.0f, o1 = 0.0f;
+#pragma unroll
+        for (int k = 0; k < kMaxSplits / 64; ++k)
+            for (int m = 0; 64 * k + m < used && m < 64; m += 8) {
+                float2 v[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int x = 64 * k + m + e;
+                    v[e] = part[(int64_t)(x < used ? x : used - 1) * (ATT_D / 2)];
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    // (a lane behind the last split holds a factor of 2^(none - top): zero, or one of an empty row's zeros)
+                    const float g = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f[k]), m + e));
+                    o0 += 64 * k + m + e < used ? v[e].x * g : 0.0f;
+                    o1 += 64 * k + m + e < used ? v[e].y * g : 0.0f;
+                }
+            }
+        const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+        reinterpret_cast<half2v*>(p.out + token * p.out_stride + hq * ATT_D)[l] = half2v{(_Float16)(o0 * inv), (_Float16)(o1 * inv)};
     }
 }
 
@@ -566,47 +1163,78 @@ AttnPlan attention_plan(int64_t B, int64_t T, int H, int Hq, int64_t max_rows, i
     max_rows = max_rows < T ? max_rows : T;                                    // positions and rows are 32-bit numbers
     max_length = max_length < 0x7fffffff ? max_length : 0x7fffffff;
     const int64_t rows = max_rows * (Hq / H);
-    plan.col_tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-    const int64_t tiles = (rows + 16 * plan.col_tiles - 1) / (16 * plan.col_tiles), groups = B * H * (tiles > 0 ? tiles : 1);
-    // workgroups for three per CU, of no less than 256 tokens each
-    int64_t splits = (3 * kPlanCus + groups - 1) / groups;
-    const int64_t most = (max_length + 255) / 256;
-    splits = splits < most ? splits : most;
-    splits = splits < 1 ? 1 : splits > 128 ? 128 : splits;
-    const int64_t per = ((max_length + splits - 1) / splits + 127) / 128 * 128;
-    plan.chunk = per < 128 ? 128 : per > (1 << 30) ? 1 << 30 : (int)per;
-    splits = splits > 1 ? (max_length + plan.chunk - 1) / plan.chunk : 1;
-    plan.splits = (int)(splits < 1 ? 1 : splits);
-    plan.workspace = plan.splits > 1 ? T * Hq * plan.splits * (ATT_D + 2) * 4 : 0;
+    plan.tile_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : SH_ROWS * ATT_WAVES;
+    plan.splits = 1;
+    plan.chunk = 1 << 30;
+    plan.waves = ATT_WAVES;
+    plan.workgroups = 0;
+    int64_t partials = 0;
+    if (plan.tile_rows <= 32) {
+        const int64_t most = tuned(Knob::ATT_WHOLE_MAX, 2048);
+        if (B * H <= kPlanCus && max_length <= most) {
+            plan.waves = plan.tile_rows == 16 ? 16 : ATT_WAVES;
+        } else if (B <= kBalancedSequences && max_length > (most < 256 ? most : 256)) {
+            plan.workgroups = (int)(kPlanCus * tuned(Knob::ATT_WG_PER_CU, plan.tile_rows == 16 ? 3 : 2));
+            partials = (int64_t)plan.workgroups * 2 * plan.tile_rows;
+        }
+    } else {
+        const int64_t tiles = (rows + plan.tile_rows - 1) / plan.tile_rows, groups = B * H * (tiles > 0 ? tiles : 1);
+        int64_t splits = (2 * kPlanCus + groups - 1) / groups;
+        const int64_t most = (max_length + 255) / 256;                         // of no less than 256 tokens each
+        splits = splits < most ? splits : most;
+        splits = splits < 1 ? 1 : splits > kMaxSplits ? kMaxSplits : splits;
+        const int64_t per = ((max_length + splits - 1) / splits + 127) / 128 * 128;
+        plan.chunk = per < 128 ? 128 : per > (1 << 30) ? 1 << 30 : (int)per;
+        const int chunk = tuned(Knob::ATT_CHUNK, 0);
+        if (chunk > 0) plan.chunk = (chunk + 127) / 128 * 128;
+        splits = chunk > 0 || splits > 1 ? (max_length + plan.chunk - 1) / plan.chunk : 1;
+        plan.splits = (int)(splits < 1 ? 1 : splits > kMaxSplits ? kMaxSplits : splits);
+        if (plan.splits > 1) partials = T * Hq * plan.splits;
+    }
+    plan.stats_at = partials * ATT_D;
+    plan.workspace = partials * (ATT_D + 2) * 4;
     return plan;
-}
-
-template <int KB, int VB, int NT>
-static hipError_t attention_launch_as(const AttnDev& d, int64_t max_rows, hipStream_t stream) {
-    const int64_t tiles = (max_rows * d.G + 16 * NT - 1) / (16 * NT);
-    const dim3 grid((unsigned)(d.c.B * d.c.H), (unsigned)(tiles < 1 ? 1 : tiles > 65535 ? 65535 : tiles), (unsigned)d.splits);
-    hipError_t e = launch(attention_kernel<KB, VB, NT>, grid, dim3(ATT_NT), 0, stream, d);
-    if (e != hipSuccess || d.splits == 1) return e;
-    return launch(attention_join_kernel<16 * NT>, dim3(grid.x, grid.y, NT), dim3(ATT_NT), 0, stream, d);
 }
 
 template <int KB, int VB>
 static hipError_t attention_launch_bits(const AttnDev& d, const AttnPlan& plan, int64_t max_rows, hipStream_t stream) {
-    switch (plan.col_tiles) {
-        case 1: return attention_launch_as<KB, VB, 1>(d, max_rows, stream);
-        case 2: return attention_launch_as<KB, VB, 2>(d, max_rows, stream);
-        default: return attention_launch_as<KB, VB, 4>(d, max_rows, stream);
+    const int64_t tiles = (max_rows * d.G + plan.tile_rows - 1) / plan.tile_rows;
+    const dim3 pairs((unsigned)(d.c.B * d.c.H), (unsigned)(tiles < 1 ? 1 : tiles > 65535 ? 65535 : tiles), (unsigned)d.splits);
+    auto go = [&](auto kernel, dim3 grid, int threads, int lds, OccCache& cache) {
+        int occ = 0;
+        const hipError_t e = kernel_occupancy(reinterpret_cast<const void*>(kernel), threads, lds, cache, occ);
+        return e == hipSuccess ? launch(kernel, grid, dim3((unsigned)threads), lds, stream, d) : e;
+    };
+    static OccCache caches[6];
+    hipError_t e;
+    if (plan.workgroups > 0) {
+        const dim3 grid((unsigned)plan.workgroups);
+        if (plan.tile_rows == 16) e = go(balanced_attention_kernel<KB, VB, 1, 4>, grid, 256, FewRows<KB, VB, 1, 4>::LDS, caches[0]);
+        else e = go(balanced_attention_kernel<KB, VB, 2, 4>, grid, 256, FewRows<KB, VB, 2, 4>::LDS, caches[1]);
+        if (e != hipSuccess) return e;
+        const int64_t rows = max_rows * d.G;
+        const dim3 join(pairs.x, (unsigned)(rows < 1 ? 1 : rows < plan.tile_rows ? rows : plan.tile_rows));
+        if (plan.tile_rows == 16) return launch(balanced_join_kernel<1>, join, dim3(ATT_NT), 0, stream, d, plan.workgroups);
+        return launch(balanced_join_kernel<2>, join, dim3(ATT_NT), 0, stream, d, plan.workgroups);
     }
+    if (plan.tile_rows == 16 && plan.waves == 16) return go(whole_attention_kernel<KB, VB, 1, 16>, pairs, 1024, FewRows<KB, VB, 1, 16>::LDS, caches[2]);
+    if (plan.tile_rows == 16) return go(whole_attention_kernel<KB, VB, 1, 4>, pairs, 256, FewRows<KB, VB, 1, 4>::LDS, caches[3]);
+    if (plan.tile_rows == 32) return go(whole_attention_kernel<KB, VB, 2, 4>, pairs, 256, FewRows<KB, VB, 2, 4>::LDS, caches[4]);
+    e = go(shared_attention_kernel<KB, VB>, pairs, ATT_NT, SH_LDS, caches[5]);
+    if (e != hipSuccess || d.splits == 1) return e;
+    const int64_t rows = (max_rows * d.G + ATT_WAVES - 1) / ATT_WAVES;
+    return launch(attention_join_kernel<SH_ROWS * ATT_WAVES>, dim3(pairs.x, (unsigned)(rows < 1 ? 1 : rows > 65535 ? 65535 : rows)), dim3(ATT_NT), 0, stream, d);
 }
 
 hipError_t attention_launch(const CacheDev& c, const AttnArgs& a, const AttnPlan& plan, hipStream_t stream) {
     AttnDev d;
     d.c = c;
-    d.q = a.q; d.out = a.out; d.visible = a.visible; d.part = a.workspace;
+    d.q = a.q; d.out = a.out; d.visible = a.visible; d.part = a.workspace; d.stats = a.workspace + plan.stats_at;
     d.q_stride = a.q_stride; d.out_stride = a.out_stride;
     d.scale2 = a.scale * 1.44269504088896340736f;
     d.Hq = a.Hq; d.G = a.Hq / c.H; d.window = a.window; d.sinks = a.sinks;
-    d.chunk = plan.chunk; d.splits = plan.splits;
+    d.chunk = plan.chunk; d.splits = plan.splits; d.min_units = tuned(Knob::ATT_CHUNK, 512) / 128;
+    if (d.min_units < 1) d.min_units = 1;
     switch (c.bits[0] * 8 + c.bits[1]) {
         case 2 * 8 + 2: return attention_launch_bits<2, 2>(d, plan, a.max_rows, stream);
         case 2 * 8 + 3: return attention_launch_bits<2, 3>(d, plan, a.max_rows, stream);

@@ -178,11 +178,11 @@ struct AttnArgs {
     float* workspace;
     int64_t max_rows, max_length;
 };
-// How an attention launch is cut: column tiles of 16 rows per wave, tokens per split, splits.
+// How an attention launch is cut: rows and waves of a workgroup, tokens per split and splits, or the workgroups of a balanced launch (0: none).
 struct AttnPlan {
-    int col_tiles;
-    int chunk;
-    int splits;
+    int tile_rows, waves, workgroups;
+    int chunk, splits;
+    int64_t stats_at;         // floats of partial channels in the workspace
     int64_t workspace;        // bytes
 };
 AttnPlan attention_plan(int64_t B, int64_t T, int H, int Hq, int64_t max_rows, int64_t max_length);
@@ -322,7 +322,7 @@ int cu_count();
 // Tuning overrides (kernel flavour, workgroups per CU, ...), for measurements and for the tests that must reach every code
 // path; kKnobNames (fq_api.hip) has their names in the same order.  Each starts from the environment variable of that name, read
 // once per process, and can be changed with fq_set_tuning.
-enum class Knob { MODE, WG_PER_CU, FORCE_GENERIC, KV_WG_PER_CU, GEMM_TILED, GEMM_WIDE, GEMM_DEPTH, GEMM_WAVES, GEMM_ROWS, GEMM_TOKENS, GEMM_RING_MAX_T, KV_FOLD_HEADS, KV_FEW, WAVE_TPW, PROBE_SHAPE, COUNT };
+enum class Knob { MODE, WG_PER_CU, FORCE_GENERIC, KV_WG_PER_CU, GEMM_TILED, GEMM_WIDE, GEMM_DEPTH, GEMM_WAVES, GEMM_ROWS, GEMM_TOKENS, GEMM_RING_MAX_T, KV_FOLD_HEADS, KV_FEW, WAVE_TPW, PROBE_SHAPE, ATT_CHUNK, ATT_WG_PER_CU, ATT_WHOLE_MAX, COUNT };
 struct KnobState {
     std::atomic<int> state{0};   // 0: environment not read yet, 1: unset (callers use their default), 2: set
     std::atomic<int> value{0};

@@ -89,12 +89,13 @@ class Batch:
             if self.rows[b] == 0:
                 continue
             L = max(0, self.lengths[b])
-            k, v = (x.values(self.table[b, :self.width], np.arange(L)) for x in self.host)
+            k, v = (np.nan_to_num(x.values(self.table[b, :self.width], np.arange(L))) for x in self.host)
+            ks, vs = (np.nan_to_num(x.steps(self.table[b, :self.width], np.arange(L))) for x in self.host)
             seen = self.visible(b, window, sinks, masks)
             t = slice(self.starts[b], self.starts[b + 1])
             for h in range(self.H * G):
-                o, A, smax = co.attention64(q[t, h], np.nan_to_num(k[h // G]), np.nan_to_num(v[h // G]), seen, scale)
-                out[t, h], tol[t, h] = o, co.attention_bound(o, A, smax, L)
+                o, *size = co.attention64(q[t, h], k[h // G], v[h // G], seen, scale, ks[h // G], vs[h // G], self.bits[0])
+                out[t, h], tol[t, h] = o, co.attention_bound(o, *size, L, self.bits[1])
         return out, tol
 
 

@@ -121,8 +121,8 @@ def test_what_attention_refuses(call):
 def test_workspace_follows_from_the_host_figures():
     size = lambda H=4, Hq=8, **b: fq.fq_cache_attention_workspace(_cache(H=H), _batch(**b), Hq)      # noqa: E731
     assert size(T=0) == 0 and size(T=5, B=0) == 0 and size(T=2, max_length=64) == 0
-    one = size(T=1, B=1, max_length=131072)
-    assert one > 0 and one % (8 * 130 * 4) == 0 and size(T=2, B=1, max_length=131072) == 2 * one
+    assert size(T=1, B=1, max_length=131072) > 0 and size(T=1, B=1, max_length=131072) % 16 == 0
+    assert size(T=300, B=3, max_rows=100, max_length=131072) > size(T=100, B=1, max_rows=100, max_length=1000)
     for bad in (dict(Hq=0), dict(Hq=6), dict(T=-1), dict(T=2 ** 29 + 1), dict(B=2 ** 22)):
         with pytest.raises(fq.FlatQuantError):
             size(**{**dict(T=1), **bad})
@@ -130,7 +130,7 @@ def test_workspace_follows_from_the_host_figures():
         for length in (0, 1, 31, 4096, 10 ** 6, 2 ** 30):
             for B in (1, 7, 300):
                 n = size(T=B * rows, B=B, max_rows=rows, max_length=length)
-                assert 0 <= n <= B * rows * 8 * 128 * 130 * 4
+                assert 0 <= n <= max(2 * 4 * 256 * 32, B * rows * 8 * 128) * 130 * 4 and n % 16 == 0
 
 
 class _Buffer:
@@ -207,22 +207,26 @@ def test_oracle_attention_closed_forms():
     r = np.random.Generator(np.random.PCG64(9))
     k, v, q = r.standard_normal((7, 128)), r.standard_normal((7, 128)), r.standard_normal((3, 128))
     seen = np.array([[1, 0, 0, 0, 0, 0, 0], [0] * 7, [0, 1, 1, 0, 0, 0, 1]], dtype=bool)
-    out, A, _ = co.attention64(q, k, v, seen, 0.3)
-    assert np.allclose(out[0], v[0]) and not out[1].any() and np.allclose(A[0], np.abs(v[0]))
-    assert np.allclose(co.attention64(q, k, v, seen, 0.0)[0][2], v[[1, 2, 6]].mean(0))
+    one = np.ones(7)
+    out, A, S, delta = co.attention64(q, k, v, seen, 0.3, one, 2 * one)
+    assert np.allclose(out[0], v[0]) and not out[1].any() and np.allclose(A[0], np.abs(v[0])) and S[1] == 0 and np.isclose(S[2], 2)
+    assert delta[1] == 0 and np.isclose(delta[2], 0.3 * (280 * 15 * np.abs(q[2]).sum() / 2 ** 24 + 132 * np.abs(q[2]).max() / 2 ** 18))
+    assert np.allclose(co.attention64(q, k, v, seen, 0.0, one, one)[0][2], v[[1, 2, 6]].mean(0))
 
 
 def test_oracle_bound_rejects_planted_mistakes():
-    """A token too many, a token too few, a step left out, two query heads exchanged: each is far outside the bound."""
+    """A token too many, a token too few, a token of every 32 left out, two query heads exchanged, a step halved: each is far outside the bound."""
     r = np.random.Generator(np.random.PCG64(10))
     L = 200
-    k, v, q = r.standard_normal((L, 128)), r.standard_normal((L, 128)), r.standard_normal((2, 128))
+    grids = [co.grid32(r.standard_normal((L, 128)), 1.0, 4) for _ in range(2)]
+    (k, v), (ks, vs) = [co.dequantize(*g) for g in grids], [g[1].astype(np.float64) for g in grids]
+    q = r.standard_normal((2, 128))
     seen = np.ones((2, L), dtype=bool)
     seen[0, -1] = False
-    out, A, smax = co.attention64(q, k, v, seen, 0.09)
-    tol = co.attention_bound(out, A, smax, L)
-    worse = [co.attention64(q, k, v, m, 0.09)[0] for m in (np.ones_like(seen), seen & (np.arange(L) > 0), seen & (np.arange(L) % 32 != 5))]
-    worse += [out[::-1], co.attention64(q, k, v * np.where(np.arange(L) == 3, 0.5, 1.0)[:, None], seen, 0.09)[0], out * 1.003]
+    out, *size = co.attention64(q, k, v, seen, 0.09, ks, vs)
+    tol = co.attention_bound(out, *size, L)
+    worse = [co.attention64(q, k, v, m, 0.09, ks, vs)[0] for m in (np.ones_like(seen), seen & (np.arange(L) > 0), seen & (np.arange(L) % 32 != 5))]
+    worse += [out[::-1], co.attention64(q, k, v * np.where(np.arange(L) == 3, 0.5, 1.0)[:, None], seen, 0.09, ks, vs)[0], out * 1.02]
     for x in worse:
         assert (np.abs(x - out) / tol).max() > 1.0
     assert (np.abs(out.astype(np.float16) - out) / tol).max() < 1.0

@@ -120,8 +120,14 @@ ATTEND = [  # rows, lengths, H, G, page, bits, window, sinks
 ]
 
 
+LAUNCHES = {"chosen": {}, "balanced": {"FLATQUANT_ATT_WHOLE_MAX": 0, "FLATQUANT_ATT_CHUNK": 128}, "balanced, few": {"FLATQUANT_ATT_WHOLE_MAX": 0, "FLATQUANT_ATT_WG_PER_CU": 1}}
+
+
+@pytest.mark.parametrize("launch", LAUNCHES)
 @pytest.mark.parametrize("rows,lengths,H,G,page,bits,window,sinks", ATTEND)
-def test_attention(rows, lengths, H, G, page, bits, window, sinks):
+def test_attention(rows, lengths, H, G, page, bits, window, sinks, launch, tuning):
+    for name, value in LAUNCHES[launch].items():
+        tuning(name, value)
     print(f"[case] attention {rows} of {lengths}, {H} x {G} heads, pages of {page}, {bits} bits, window {window} + {sinks}", flush=True)
     c = Batch(500 + sum(lengths), rows, lengths, H, page, *bits, pad=2).upload()
     q = c.row_tensor(H * G, 8, gain=2.0)
@@ -133,8 +139,11 @@ TREES = [((1,), (1,), 1, 1, 16, (4, 4)), ((13, 5), (400, 5), 2, 4, 16, (4, 4)), 
          ((9, 20), (50, 320), 2, 1, 16, (3, 4))]
 
 
+@pytest.mark.parametrize("launch", LAUNCHES)
 @pytest.mark.parametrize("rows,lengths,H,G,page,bits", TREES)
-def test_tree_attention(rows, lengths, H, G, page, bits):
+def test_tree_attention(rows, lengths, H, G, page, bits, launch, tuning):
+    for name, value in LAUNCHES[launch].items():
+        tuning(name, value)
     print(f"[case] tree {rows} of {lengths}, {H} x {G} heads", flush=True)
     c = Batch(900 + sum(lengths), rows, lengths, H, page, *bits, pad=1).upload()
     masks = np.zeros(c.T, dtype=np.uint64)
