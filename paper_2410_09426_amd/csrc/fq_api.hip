@@ -47,7 +47,7 @@ hipError_t kernel_occupancy(const void* fn, int threads, int lds, OccCache& cach
 
 KnobState g_knobs[(int)Knob::COUNT];
 namespace {
-const char* const kKnobNames[] = {"FLATQUANT_MODE", "FLATQUANT_WG_PER_CU", "FLATQUANT_FORCE_GENERIC", "FLATQUANT_KV_WG_PER_CU", "FLATQUANT_GEMM_TILED", "FLATQUANT_GEMM_WIDE", "FLATQUANT_GEMM_DEPTH", "FLATQUANT_GEMM_WAVES", "FLATQUANT_GEMM_ROWS", "FLATQUANT_GEMM_TOKENS", "FLATQUANT_GEMM_RING_MAX_T", "FLATQUANT_KV_FOLD_HEADS", "FLATQUANT_KV_FEW", "FLATQUANT_WAVE_TPW", "FLATQUANT_PROBE_SHAPE", "FLATQUANT_ATT_CHUNK", "FLATQUANT_ATT_WG_PER_CU", "FLATQUANT_ATT_WHOLE_MAX"};
+const char* const kKnobNames[] = {"FLATQUANT_MODE", "FLATQUANT_WG_PER_CU", "FLATQUANT_FORCE_GENERIC", "FLATQUANT_KV_WG_PER_CU", "FLATQUANT_GEMM_TILED", "FLATQUANT_GEMM_WIDE", "FLATQUANT_GEMM_DEPTH", "FLATQUANT_GEMM_WAVES", "FLATQUANT_GEMM_ROWS", "FLATQUANT_GEMM_TOKENS", "FLATQUANT_GEMM_RING_MAX_T", "FLATQUANT_KV_FOLD_HEADS", "FLATQUANT_KV_FEW", "FLATQUANT_WAVE_TPW", "FLATQUANT_PROBE_SHAPE", "FLATQUANT_ATT_CHUNK", "FLATQUANT_ATT_WG_PER_CU", "FLATQUANT_ATT_WAVES"};
 static_assert(sizeof(kKnobNames) / sizeof(kKnobNames[0]) == (size_t)Knob::COUNT, "a name for every override");
 }  // namespace
 
@@ -363,8 +363,13 @@ static fq_status cache_attention(const fq_kv_cache* cache, const fq_kv_batch* ba
     if (Hq > (1 << 24) || batch->T > 0x7fffff00LL / Hq || q_stride > (1LL << 40) || out_stride > (1LL << 40) || (tree && batch->max_rows > 64)) return FQ_UNSUPPORTED_SHAPE;
     if (empty) return FQ_OK;
     if (!q || !out || (tree && !visible)) return FQ_INVALID_ARG;
-    const fq::AttnPlan plan = fq::attention_plan(batch->B, batch->T, cache->H, Hq, batch->max_rows, batch->max_length);
+    fq::AttnPlan plan = fq::attention_plan(batch->B, batch->T, cache->H, Hq, batch->max_rows, batch->max_length, batch->max_length);
     if (workspace_bytes < plan.workspace || (plan.workspace > 0 && !workspace)) return FQ_INVALID_ARG;
+    if (window > 0) {   // steps of 32 tokens around a tile's windows, and the first tokens
+        const fq::AttnPlan fewer = fq::attention_plan(batch->B, batch->T, cache->H, Hq, batch->max_rows, batch->max_length,
+                                                      (int64_t)window + sinks + batch->max_rows + 64);
+        if (fewer.workspace <= plan.workspace) plan = fewer;
+    }
     auto bad = [](const void* p, int a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; };
     if (bad(q, 16) || bad(out, 16) || (q_stride & 7) || (out_stride & 7) || bad(workspace, 16) || bad(visible, 8)) return FQ_MISALIGNED;
     const int64_t qbytes = ((batch->T - 1) * q_stride + row) * 2, obytes = ((batch->T - 1) * out_stride + row) * 2;
@@ -376,7 +381,7 @@ static fq_status cache_attention(const fq_kv_cache* cache, const fq_kv_batch* ba
     fq::AttnArgs a;
     a.q = static_cast<const _Float16*>(q); a.out = static_cast<_Float16*>(out); a.q_stride = q_stride; a.out_stride = out_stride;
     a.Hq = Hq; a.scale = scale; a.window = window; a.sinks = sinks; a.visible = visible; a.workspace = static_cast<float*>(workspace);
-    a.max_rows = batch->max_rows; a.max_length = batch->max_length;
+    a.max_rows = batch->max_rows;
     return fq::finish(fq::attention_launch(d, a, plan, static_cast<hipStream_t>(stream)));
 }
 
@@ -397,7 +402,7 @@ int64_t fq_cache_attention_workspace(const fq_kv_cache* cache, const fq_kv_batch
         batch->B > 0xffffff / cache->H)
         return -1;
     if (batch->B == 0 || batch->T == 0) return 0;
-    return fq::attention_plan(batch->B, batch->T, cache->H, Hq, batch->max_rows, batch->max_length).workspace;
+    return fq::attention_plan(batch->B, batch->T, cache->H, Hq, batch->max_rows, batch->max_length, batch->max_length).workspace;
 }
 
 fq_status flatquant_dequant_mxfp4(const uint8_t* codes, const uint8_t* scales, int64_t rows, int n, float* out, void* stream) {

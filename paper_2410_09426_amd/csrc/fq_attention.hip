@@ -65,10 +65,10 @@ __device__ __forceinline__ uint32_t as_u32(half2v x) { return __builtin_bit_cast
 // Two codes in bits [S, S + QB) of the halves of x, S + QB <= 10: as fp16 bits that is 2^(S - 24) code, a subnormal number, which the matrix
 // instructions take at its value.  They align the products to the largest of them, though, by its exponent as if it were normalised, and drop what
 // lies 24 bits below (measured: one code unit beside others is off by up to 2^-13.4 of itself at S = 0, by nothing at 2 and above for weights within
-// a factor of 20): S is 4 at least.
+// a factor of 20): S is 2 at least.
 template <int QB, int S>
 __device__ __forceinline__ uint32_t field(uint32_t x) {
-    static_assert(S >= 4 && S + QB <= 10, "mantissa bits");
+    static_assert(S >= 2 && S + QB <= 10, "mantissa bits");
     return x & ((((1u << QB) - 1u) << S) * 0x00010001u);
 }
 // code - zero point of such a field; `z`: 1024 + the zero points, in fp16.  1024 in the exponent makes it 1024 + 2^S code; one packed fma takes
@@ -91,14 +91,14 @@ struct KeyCodes<4> {
     typedef u32x4 words;
     static constexpr int first(int p) { return 8 * (p >> 2) + (p & 3); }
     static constexpr int second(int p) { return first(p) + 4; }
-    static constexpr int shift(int) { return 4; }
+    static constexpr int shift(int p) { return p & 1 ? 6 : 2; }
     static __device__ __forceinline__ void fields(const words& w, uint32_t (&o)[16]) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            o[4 * k] = field<4, 4>(w[k] << 4);
-            o[4 * k + 1] = field<4, 4>(w[k]);
-            o[4 * k + 2] = field<4, 4>(w[k] >> 4);
-            o[4 * k + 3] = field<4, 4>(w[k] >> 8);
+            o[4 * k] = field<4, 2>(w[k] << 2);
+            o[4 * k + 1] = field<4, 6>(w[k] << 2);
+            o[4 * k + 2] = field<4, 2>(w[k] >> 6);
+            o[4 * k + 3] = field<4, 6>(w[k] >> 6);
         }
     }
 };
@@ -161,17 +161,17 @@ template <int QB>
 struct ValueCodes {
     static constexpr int shift(int c) {
         constexpr int at[8] = {4, 7, 6, 4, 7, 6, 5, 5};
-        return QB == 4 ? 4 : QB == 2 ? shift2(c) : at[c];
+        return QB == 4 ? (c & 1 ? 6 : 2) : QB == 2 ? shift2(c) : at[c];
     }
     template <int HALF>
     static __device__ __forceinline__ void fields(uint32_t a, uint32_t b, uint32_t (&o)[4]) {
         const uint32_t x = __builtin_amdgcn_perm(b, a, 0x05040100u);
         if constexpr (QB == 4) {
             const uint32_t y = HALF ? __builtin_amdgcn_perm(b, a, 0x07060302u) : x;
-            o[0] = field<4, 4>(y << 4);
-            o[1] = field<4, 4>(y);
-            o[2] = field<4, 4>(y >> 4);
-            o[3] = field<4, 4>(y >> 8);
+            o[0] = field<4, 2>(y << 2);
+            o[1] = field<4, 6>(y << 2);
+            o[2] = field<4, 2>(y >> 6);
+            o[3] = field<4, 6>(y >> 6);
         } else if constexpr (QB == 2 && HALF == 0) {
             o[0] = field<2, 4>(x << 4);
             o[1] = field<2, 6>(x << 4);
@@ -250,7 +250,9 @@ __device__ __forceinline__ uint32_t ring_value(const unsigned char* piece, int i
     return __builtin_amdgcn_alignbit(w[(3 * i & 3) > 1 ? 1 : 0], w[0], 8 * (3 * i & 3));
 }
 
-__device__ __forceinline__ float zero_of(uint32_t params) { return (float)(params >> 16 & 255u); }
+// The zero point as it stands in a token's parameters: 2^-24 of it, a subnormal fp16 number, as is what the mixed-precision fma reads in place.
+__device__ __forceinline__ _Float16 zero_bits(uint32_t params) { return as_half2(params)[1]; }
+__device__ __forceinline__ _Float16 step_bits(uint32_t params) { return as_half2(params)[0]; }
 __device__ __forceinline__ float step_of(uint32_t params) { return (float)__builtin_bit_cast(_Float16, (uint16_t)params); }
 
 template <typename T>
@@ -316,26 +318,40 @@ __device__ __forceinline__ bool sees(const AttnDev& p, int k, int pos, int befor
 }
 // The step of a value that not every row sees: a number, so that a weight of zero makes a product of zero whatever the page holds.
 __device__ __forceinline__ float finite_step(float s) { return __builtin_fminf(s, 65504.0f); }
+// ... and its parameters: a step that is a number, a zero point of four bits.
+__device__ __forceinline__ uint32_t usable_parameters(uint32_t w) { return (w & 0x7C00u) == 0x7C00u ? 0u : w & 0x000FFFFFu; }
+__device__ __forceinline__ float times_step(uint32_t params, float x) {
+    float r;
+    asm("v_fma_mix_f32 %0, %1, %2, 0 op_sel_hi:[1,0,0]" : "=v"(r) : "v"(params), "v"(x));
+    return r;
+}
+// sum + product (a half of `pair`) times the zero point in a token's parameters, both read where they are.
+template <int HI>
+__device__ __forceinline__ float zero_sum(uint32_t pair, uint32_t params, float sum) {
+    if constexpr (HI) asm("v_fma_mix_f32 %0, %1, %2, %0 op_sel:[1,1,0] op_sel_hi:[1,1,0]" : "+v"(sum) : "v"(pair), "v"(params));
+    else asm("v_fma_mix_f32 %0, %1, %2, %0 op_sel:[0,1,0] op_sel_hi:[1,1,0]" : "+v"(sum) : "v"(pair), "v"(params));
+    return sum;
+}
 // Weights 2^(factor score - ref), their products with the values' steps and the weights' sum; true if a lane of the wave needs a higher reference.
-template <int N, typename Scores, typename Factor>
-__device__ __forceinline__ bool weigh(const Scores& score, Factor factor, const float (&step)[N], float ref, float (&prod)[N], float& sum) {
+template <int N, typename Scores, typename Factor, typename Step>
+__device__ __forceinline__ bool weigh(const Scores& score, Factor factor, Step step, float ref, float (&prod)[N], float& sum) {
     float big = 0.0f;
     sum = 0.0f;
 #pragma unroll
     for (int k = 0; k < N; ++k) {
         const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(score[k], factor(k), -ref));
         sum += e;
-        prod[k] = e * step[k];
+        prod[k] = e * step(k);
         big = __builtin_fmaxf(big, prod[k]);
     }
     return __any(big > 32768.0f || sum > 0x1p40f);
 }
 // Raises the reference so that the row's largest product here is at most 2^7 (a step below 2^-25 counts as that); returns the factor for what has been summed.
-template <int N, typename Scores, typename Factor, typename Row>
-__device__ __forceinline__ float raise_reference(const Scores& score, Factor factor, const float (&step)[N], float& ref, Row row_max) {
+template <int N, typename Scores, typename Factor, typename Step, typename Row>
+__device__ __forceinline__ float raise_reference(const Scores& score, Factor factor, Step step, float& ref, Row row_max) {
     float top = ATT_NONE;
 #pragma unroll
-    for (int k = 0; k < N; ++k) top = __builtin_fmaxf(top, score[k] * factor(k) + __builtin_fmaxf(__builtin_amdgcn_logf(step[k]), -25.0f));
+    for (int k = 0; k < N; ++k) top = __builtin_fmaxf(top, score[k] * factor(k) + __builtin_fmaxf(__builtin_amdgcn_logf(step(k)), -25.0f));
     const float to = __builtin_fmaxf(ref, row_max(top) - 7.0f), f = __builtin_amdgcn_exp2f(ref - to);
     ref = to;
     return f;
@@ -344,7 +360,7 @@ __device__ __forceinline__ float raise_reference(const Scores& score, Factor fac
 // ---- few rows: a wave has 16 NT of them and every NW-th step of a stretch of the sequence
 template <int KB, int VB, int NT, int NW>
 struct FewRows {
-    static constexpr int DEPTH = 2;                                            // slots of a wave's ring
+    static constexpr int DEPTH = 2;                                            // slots of a wave's ring (the waits in the loop are for two)
     static constexpr int RING = NW * DEPTH * Ring<KB, VB>::SLOT, SUMS = NW * 16 * ATT_PITCH * 4;
     static constexpr int STATS = RING > SUMS ? RING : SUMS;                    // references and sums of the rows, behind what the ring and the join share
     static constexpr int LDS = STATS + 2 * NW * 16 * NT * 4;
@@ -387,8 +403,8 @@ __device__ __forceinline__ void few_rows(const AttnDev& p, unsigned char* smem, 
 #pragma unroll
         for (int k = 0; k <= DEPTH; ++k) pages_of(x + NW * k, pg[k]);
 
-    // Rows: queries in the order of the codes, brought up to 2^9 and down by the codes' shifts (a power of two each, and back in `factor`, where the
-    // sign of the scale goes the other way), their sums, positions.  Asked for before the first steps: loads return in order.
+    // Rows: queries in the order of the codes, brought up to 2^9 and down by the codes' shifts (a power of two each, and back in `factor`; the sign of the
+    // scale is in the queries), their sums, positions.  Asked for before the first steps: loads return in order.
     half8 raw[NT][4];
     int pos[NT];
     uint64_t seen[NT];
@@ -406,31 +422,39 @@ __device__ __forceinline__ void few_rows(const AttnDev& p, unsigned char* smem, 
     __builtin_amdgcn_sched_barrier(0);
     if (any)
 #pragma unroll
-        for (int k = 0; k < DEPTH; ++k) load(x + NW * k, pg[k], k);
+        for (int k = 0; k < DEPTH; ++k)
+            if (x + NW * k < x_end) load(x + NW * k, pg[k], k);
     __builtin_amdgcn_sched_barrier(0);
     half8 q[NT][4];
-    float q_sum[NT], factor[NT];
+    float q_sum[NT], factor[NT];                                               // q_sum: minus the sum, as the instruction adds it up
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        float sum = 0.0f, top = 0.0f;
+        float squares = 0.0f;
 #pragma unroll
-        for (int m = 0; m < 4; ++m)
+        for (int m = 0; m < 4; ++m) {
+            const u32x4 r = __builtin_bit_cast(u32x4, raw[n][m]);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                sum += (float)raw[n][m][e];
-                top = __builtin_fmaxf(top, __builtin_fabsf((float)raw[n][m][e]));
-            }
-        const int up = 10 - __builtin_amdgcn_frexp_expf(across_groups(top, fmax_op));
-        const float scaled = __builtin_ldexpf(p.scale2 < 0.0f ? -1.0f : 1.0f, up);
-        q_sum[n] = across_groups(sum, fadd_op) * __builtin_ldexpf(scaled, -24);
+            for (int k = 0; k < 4; ++k) squares = __builtin_amdgcn_fdot2(as_half2(r[k]), as_half2(r[k]), squares, false);
+        }
+        int up = 9 - ((__builtin_amdgcn_frexp_expf(across_groups(squares, fadd_op)) + 1) >> 1);
+        up = up < 17 ? up : 17;                                                // (what is that small is exact all the same: multiples of 2^-24)
         // never zero: what is not visible scores -infinity before this factor
         factor[n] = __builtin_amdgcn_fmed3f(__builtin_ldexpf(__builtin_fabsf(p.scale2), 24 - up), 0x1p-120f, 0x1p100f);
-        each<16>([&](auto pp) {
-            constexpr int pair = decltype(pp)::value, a = KeyCodes<KB>::first(pair), z = KeyCodes<KB>::second(pair);
-            const float by = scaled * (1.0f / (float)(1 << KeyCodes<KB>::shift(pair)));
-            q[n][pair >> 2][2 * (pair & 3)] = (_Float16)((float)raw[n][a >> 3][a & 7] * by);
-            q[n][pair >> 2][2 * (pair & 3) + 1] = (_Float16)((float)raw[n][z >> 3][z & 7] * by);
+        const float sign = p.scale2 < 0.0f ? -1.0f : 1.0f;
+        f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+        each<4>([&](auto mm) {
+            constexpr int m = decltype(mm)::value;
+            u32x4 o, back;
+            each<4>([&](auto ee) {
+                constexpr int e = decltype(ee)::value, pair = 4 * m + e, a = KeyCodes<KB>::first(pair), z = KeyCodes<KB>::second(pair), S = KeyCodes<KB>::shift(pair);
+                const _Float16 by = (_Float16)__builtin_ldexpf(sign, up - S), off = (_Float16)(-(float)(1 << S));
+                o[e] = as_u32(half2v{raw[n][a >> 3][a & 7], raw[n][z >> 3][z & 7]} * half2v{by, by});
+                back[e] = as_u32(half2v{off, off});
+            });
+            q[n][m] = __builtin_bit_cast(half8, o);
+            sum = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, back), q[n][m], sum, 0, 0, 0);
         });
+        q_sum[n] = sum[0];
     }
 
     f32x4 acc[NT][8];
@@ -463,21 +487,20 @@ __device__ __forceinline__ void few_rows(const AttnDev& p, unsigned char* smem, 
         }
         __builtin_amdgcn_sched_barrier(0);
         // sum_d q_d (c_d - z) = (sum_d q_d c_d) - z sum_d q_d
-        float vs[8], vz[8];
+        uint32_t vp[8];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            const u32x4 kp = *reinterpret_cast<const u32x4*>(slot + R::P_AT + 64 * t + 16 * g), vp = *reinterpret_cast<const u32x4*>(slot + R::P_AT + 128 + 64 * t + 16 * g);
+            const u32x4 kp = *reinterpret_cast<const u32x4*>(slot + R::P_AT + 64 * t + 16 * g), v4 = *reinterpret_cast<const u32x4*>(slot + R::P_AT + 128 + 64 * t + 16 * g);
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const float z = zero_of(kp[r]), f = step_of(kp[r]);
 #pragma unroll
-                for (int n = 0; n < NT; ++n) sc[n][t][r] = __builtin_fmaf(-z, q_sum[n], sc[n][t][r]) * f;
-                vs[4 * t + r] = step_of(vp[r]);
-                vz[4 * t + r] = zero_of(vp[r]);
+                for (int n = 0; n < NT; ++n)
+                    sc[n][t][r] = times_step(kp[r], __builtin_fmaf((float)zero_bits(kp[r]), q_sum[n], sc[n][t][r]));
+                vp[4 * t + r] = v4[r];
             }
         }
         const bool pages_ok = (unsigned)pg[0] < (unsigned)p.c.pages && (unsigned)pg[1] < (unsigned)p.c.pages;
-        const int all_see = p.visible ? before - 1 : pos_lo;               // every row sees the tokens up to here, but for the window
+        const int all_see = p.visible ? before - 1 : pos_lo;                   // every row sees the tokens up to here, but for the window
         if (!(pages_ok && k0 + ATT_STEP - 1 <= all_see && k0 + ATT_STEP <= span.end && (p.window <= 0 || p.visible || k0 > pos_hi - p.window))) {
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
@@ -485,7 +508,7 @@ __device__ __forceinline__ void few_rows(const AttnDev& p, unsigned char* smem, 
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int k = k0 + 16 * t + 4 * g + r;
-                    vs[4 * t + r] = finite_step(vs[4 * t + r]);
+                    vp[4 * t + r] = usable_parameters(vp[4 * t + r]);
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
                         sc[n][t][r] = sees(p, k, pos[n], before, seen[n]) && page_ok && k < span.end ? sc[n][t][r] : -__builtin_inff();
@@ -497,30 +520,35 @@ __device__ __forceinline__ void few_rows(const AttnDev& p, unsigned char* smem, 
         for (int n = 0; n < NT; ++n) {
             float s8[8], prod[8], sum;
             auto by = [&](int) { return factor[n]; };
+            auto step = [&](int k) { return (float)step_bits(vp[k]); };
 #pragma unroll
             for (int k = 0; k < 8; ++k) s8[k] = sc[n][k >> 2][k & 3];
-            if (weigh<8>(s8, by, vs, ref[n], prod, sum)) {
-                const float f = raise_reference<8>(s8, by, vs, ref[n], [](float top) { return across_groups(top, fmax_op); });
+            if (weigh<8>(s8, by, step, ref[n], prod, sum)) {
+                const float f = raise_reference<8>(s8, by, step, ref[n], [](float top) { return across_groups(top, fmax_op); });
                 total[n] *= f;
                 zeros[n] *= f;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) acc[n][j] *= f;
-                weigh<8>(s8, by, vs, ref[n], prod, sum);
+                weigh<8>(s8, by, step, ref[n], prod, sum);
             }
             total[n] += sum;
+            u32x4 pp;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                pw[n][k] = (_Float16)prod[k];
-                zeros[n] = __builtin_fmaf((float)pw[n][k], vz[k], zeros[n]);
+            for (int k = 0; k < 4; ++k) {
+                pp[k] = as_u32(half2v{(_Float16)prod[2 * k], (_Float16)prod[2 * k + 1]});
+                zeros[n] = zero_sum<0>(pp[k], vp[2 * k], zeros[n]);
+                zeros[n] = zero_sum<1>(pp[k], vp[2 * k + 1], zeros[n]);
             }
+            pw[n] = __builtin_bit_cast(half8, pp);
         }
+        uint32_t vc[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) vc[k] = ring_value<VB>(slot + R::V_AT + (k >> 2) * R::V_PIECE, i, g, k & 3);
         auto values = [&](auto part) {
             constexpr int HALF = decltype(part)::value;
             uint32_t vv[4][4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                ValueCodes<VB>::template fields<HALF>(ring_value<VB>(slot + R::V_AT + (k >> 1) * R::V_PIECE, i, g, 2 * (k & 1)),
-                                                      ring_value<VB>(slot + R::V_AT + (k >> 1) * R::V_PIECE, i, g, 2 * (k & 1) + 1), vv[k]);
+            for (int k = 0; k < 4; ++k) ValueCodes<VB>::template fields<HALF>(vc[2 * k], vc[2 * k + 1], vv[k]);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const u32x4 a = {vv[0][j], vv[1][j], vv[2][j], vv[3][j]};
@@ -536,12 +564,13 @@ __device__ __forceinline__ void few_rows(const AttnDev& p, unsigned char* smem, 
     if (any) {
         int slot = 0;
         for (; x < x_end; x += NW) {
-            wait_vm_pending<(DEPTH - 1) * R::LOADS>();
+            if (x + NW < x_end) wait_vm_pending<R::LOADS>();                   // the next step alone may still be on its way
+            else wait_vm_pending<0>();
             int next[2];
             pages_of(x + NW * (DEPTH + 1), next);
             work(x, pg[0], ring + slot * R::SLOT);
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");                 // the slot has been read: it may take another step
-            load(x + NW * DEPTH, pg[DEPTH], slot);
+            if (x + NW * DEPTH < x_end) load(x + NW * DEPTH, pg[DEPTH], slot);
 #pragma unroll
             for (int k = 0; k < DEPTH; ++k) {
                 pg[k][0] = pg[k + 1][0];
@@ -551,14 +580,13 @@ __device__ __forceinline__ void few_rows(const AttnDev& p, unsigned char* smem, 
             pg[DEPTH][1] = next[1];
             slot = slot + 1 == DEPTH ? 0 : slot + 1;
         }
-        wait_vm_pending<0>();                                                  // nothing may still be on its way into LDS
     }
 
     // ---- the waves meet
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         total[n] = across_groups(total[n], fadd_op);
-        zeros[n] = across_groups(zeros[n], fadd_op);
+        zeros[n] = across_groups(zeros[n], fadd_op) * 0x1p24f;
         if (g == 0) {
             refs[w][16 * n + i] = ref[n];
             totals[w][16 * n + i] = total[n];
@@ -579,24 +607,24 @@ __device__ __forceinline__ void few_rows(const AttnDev& p, unsigned char* smem, 
                 f32x4 o;
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    o[j] = __builtin_fmaf(acc[n][4 * half + j][r], (float)(1 << (24 - ValueCodes<VB>::shift(4 * half + j))), -zeros[n]) * f;
+                    o[j] = __builtin_fmaf(acc[n][4 * half + j][r], f * (float)(1 << (24 - ValueCodes<VB>::shift(4 * half + j))), -zeros[n] * f);
                 *reinterpret_cast<f32x4*>(&sums[w][i][8 * (4 * g + r) + 4 * half]) = o;
             }
         __syncthreads();
         // 16 rows of 128 channels: 2048 / (64 NW) channels a thread
         constexpr int CH = 32 / NW;
         const int rr = threadIdx.x / (ATT_D / CH), d = CH * (threadIdx.x % (ATT_D / CH));
-        float ref_all = refs[0][16 * n + rr], sum = 0.0f, o[CH] = {};
-#pragma unroll
-        for (int k = 1; k < NW; ++k) ref_all = __builtin_fmaxf(ref_all, refs[k][16 * n + rr]);
-#pragma unroll
-        for (int k = 0; k < NW; ++k) {
-            sum += totals[k][16 * n + rr] * __builtin_amdgcn_exp2f(refs[k][16 * n + rr] - ref_all);
-#pragma unroll
-            for (int e = 0; e < CH; ++e) o[e] += sums[k][rr][d + e];
-        }
         const int r = row0 + 16 * n + rr;
         if (r < row_end) {
+            float ref_all = refs[0][16 * n + rr], sum = 0.0f, o[CH] = {};
+#pragma unroll
+            for (int k = 1; k < NW; ++k) ref_all = __builtin_fmaxf(ref_all, refs[k][16 * n + rr]);
+#pragma unroll
+            for (int k = 0; k < NW; ++k) {
+                sum += totals[k][16 * n + rr] * __builtin_amdgcn_exp2f(refs[k][16 * n + rr] - ref_all);
+#pragma unroll
+                for (int e = 0; e < CH; ++e) o[e] += sums[k][rr][d + e];
+            }
             const int64_t token = seq.first + r / p.G;
             const int hq = head * p.G + r % p.G;
             if (!partial) {
@@ -637,7 +665,7 @@ __device__ __forceinline__ Tile tile_of(const AttnDev& p, const Sequence& seq, i
 
 // blockIdx: (sequence and head, tile of rows).
 template <int KB, int VB, int NT, int NW>
-__global__ __launch_bounds__(64 * NW, NW == 16 ? 4 : NT == 1 ? 3 : 2) void whole_attention_kernel(AttnDev p) {
+__global__ __launch_bounds__(64 * NW, NW > 4 ? 4 : NT == 1 ? 3 : 2) void whole_attention_kernel(AttnDev p) {
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     const int b = blockIdx.x / p.c.H, head = blockIdx.x - b * p.c.H;
     const Sequence seq = sequence_of(p.c, b);
@@ -650,13 +678,9 @@ __global__ __launch_bounds__(64 * NW, NW == 16 ? 4 : NT == 1 ? 3 : 2) void whole
 
 // The balanced launch: the steps of all sequences and heads behind each other, in units of 4 (128 tokens), are cut into gridDim.x equal stretches, whatever
 // the lengths.  A workgroup goes through the (sequence, head) pairs of its stretch; the first and the last may be shared with its neighbours, and leave
-// partial results in the workgroup's two places.  Every wave works the cut out for itself: a lane holds four sequences.
+// partial results in the workgroup's two places.
 // A sequence that has none of the units is gone through whole, a head a workgroup.
 constexpr int kBalancedSequences = 256;
-struct Cut {
-    int units[4], sum;        // of the lane's four sequences, all heads; of the sequences of the lanes before
-    int all, per;             // of all; of a workgroup
-};
 // Units of one head of a sequence (one for rows that see nothing: they still have an output); 0: not among the units, because it has no rows, more of them
 // than a tile, or so many tokens that the units of all sequences would pass 32 bits.
 template <int ROWS>
@@ -665,85 +689,106 @@ __device__ __forceinline__ int share_of(const AttnDev& p, const Sequence& seq) {
     const int n = (tile_of<ROWS>(p, seq, 0).span.steps + 3) >> 2;
     return n > 0x7fffffff / kBalancedSequences / p.c.H ? 0 : n > 1 ? n : 1;
 }
+struct Cut {                  // in LDS
+    int first[kBalancedSequences], rows[kBalancedSequences], length[kBalancedSequences];
+    int share[kBalancedSequences], begin[kBalancedSequences];                 // units of a head, first unit
+    int all, per;             // units of all, of a workgroup
+};
+// The first wave works the cut out, a lane four sequences, for the workgroup.
 template <int ROWS>
-__device__ __forceinline__ Cut cut_of(const AttnDev& p, int workgroups) {
-    const int l = threadIdx.x & 63;
-    Cut c;
-    int mine = 0;
+__device__ __forceinline__ void make_cut(const AttnDev& p, int workgroups, Cut& cut) {
+    if (threadIdx.x < 64) {
+        const int l = threadIdx.x;
+        int share[4], mine = 0;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const int b = 4 * l + k;
-        c.units[k] = 0;
-        if (b < p.c.B) {
-            Sequence seq;
-            const int first = p.c.row_starts[b], last = p.c.row_starts[b + 1], T = (int)p.c.T;
-            seq.length = p.c.lengths[b];
-            seq.first = first > 0 ? first : 0;
-            seq.rows = (last < T ? last : T) - seq.first;
-            c.units[k] = share_of<ROWS>(p, seq) * p.c.H;
+        for (int k = 0; k < 4; ++k) {
+            const int b = l + 64 * k;
+            Sequence seq{0, 0, 0};
+            if (b < p.c.B) {
+                const int first = p.c.row_starts[b], last = p.c.row_starts[b + 1], T = (int)p.c.T;
+                seq.length = p.c.lengths[b];
+                seq.first = first > 0 ? first : 0;
+                seq.rows = (last < T ? last : T) - seq.first;
+            }
+            cut.first[b] = seq.first;
+            cut.rows[b] = seq.rows;
+            cut.length[b] = seq.length;
+            cut.share[b] = share[k] = share_of<ROWS>(p, seq);
         }
-        mine += c.units[k];
-    }
-    int sum = mine;
+        // the order of the units is that of (k, lane): sequences in their order
 #pragma unroll
-    for (int m = 1; m < 64; m *= 2) {
-        const int other = __shfl_up(sum, m);
-        sum += l >= m ? other : 0;
+        for (int k = 0; k < 4; ++k) {
+            int sum = share[k] * p.c.H;
+            if (64 * k < p.c.B) {
+#pragma unroll
+                for (int m = 1; m < 64; m *= 2) {
+                    const int other = __shfl_up(sum, m);
+                    sum += l >= m ? other : 0;
+                }
+            }
+            cut.begin[l + 64 * k] = mine + sum - share[k] * p.c.H;
+            mine += __builtin_amdgcn_readlane(sum, 63);
+        }
+        if (l == 0) {
+            cut.all = mine;
+            const int per = (mine + workgroups - 1) / workgroups;
+            cut.per = per > p.min_units ? per : p.min_units;
+        }
     }
-    c.sum = sum - mine;
-    c.all = __builtin_amdgcn_readlane(sum, 63);
-    c.per = (c.all + workgroups - 1) / workgroups;
-    c.per = c.per > p.min_units ? c.per : p.min_units;
-    return c;
+    __syncthreads();
 }
-// First unit of sequence b (uniform), and the sequence that has unit u.
-__device__ __forceinline__ int first_unit(const Cut& c, int b) {
-    int at = c.sum;
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ Sequence sequence_of(const Cut& c, int b) { return Sequence{uniform(c.first[b]), uniform(c.rows[b]), uniform(c.length[b])}; }
+// The sequence that has unit u: the last that begins at u or before (those without units begin where the next one does).
+__device__ __forceinline__ int sequence_at(const Cut& c, int B, int u) {
+    const int l = threadIdx.x & 63;
+    int n = 0;
 #pragma unroll
-    for (int k = 0; k < 3; ++k) at += (b & 3) > k ? c.units[k] : 0;
-    return __builtin_amdgcn_readlane(at, b >> 2);
-}
-__device__ __forceinline__ int sequence_at(const Cut& c, int u) {
-    const int lane = __builtin_popcountll(__ballot(c.sum <= u)) - 1;          // the last lane whose sequences begin at u or before
-    int at = __builtin_amdgcn_readlane(c.sum, lane), b = 4 * lane;
-#pragma unroll
-    for (int k = 0; k < 3; ++k) {
-        at += __builtin_amdgcn_readlane(c.units[k], lane);
-        if (at <= u) b = 4 * lane + k + 1;
-    }
-    return b;
+    for (int k = 0; k < 4; ++k) n += __builtin_popcountll(__ballot(l + 64 * k < B && c.begin[l + 64 * k] <= u));
+    return n - 1;
 }
 
 template <int KB, int VB, int NT, int NW>
 __global__ __launch_bounds__(64 * NW, NT == 1 ? 3 : 2) void balanced_attention_kernel(AttnDev p) {
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     constexpr int ROWS = 16 * NT;
-    const Cut cut = cut_of<ROWS>(p, gridDim.x);
-    const int wg = blockIdx.x, begin = wg * cut.per, end = min(begin + cut.per, cut.all);
-    for (int u = begin; u < end;) {
-        const int b = sequence_at(cut, u), first = first_unit(cut, b);
-        const Sequence seq = sequence_of(p.c, b);
-        const Tile t = tile_of<ROWS>(p, seq, 0);
-        const int n = share_of<ROWS>(p, seq), head = (u - first) / n, from = u - first - head * n;
-        const int to = min(n, from + end - u);
-        const bool partial = from > 0 || to < n;
-        few_rows<KB, VB, NT, NW>(p, smem, b, head, seq, t.row0, t.row_end, t.span, 4 * from, min(t.span.steps, 4 * to), partial,
-                                 ((int64_t)2 * wg + (u == begin ? 0 : 1)) * ROWS);
-        u += to - from;
-    }
-    for (int bh = wg; bh < p.c.B * p.c.H; bh += gridDim.x) {                   // what is not among the units
-        const int b = bh / p.c.H;
-        const Sequence seq = sequence_of(p.c, b);
-        const int tiles = (seq.rows * p.G + ROWS - 1) / ROWS;
-        if (tiles < 1 || share_of<ROWS>(p, seq)) continue;
-        for (int tile = 0; tile < tiles; ++tile) {
-            const Tile t = tile_of<ROWS>(p, seq, tile);
-            few_rows<KB, VB, NT, NW>(p, smem, b, bh - b * p.c.H, seq, t.row0, t.row_end, t.span, 0, t.span.steps, false, 0);
+    Cut& cut = *reinterpret_cast<Cut*>(smem + FewRows<KB, VB, NT, NW>::LDS);
+    make_cut<ROWS>(p, gridDim.x, cut);
+    const int wg = blockIdx.x, per = uniform(cut.per), begin = wg * per, end = min(begin + per, uniform(cut.all));
+    int u = begin, bh = wg, tile = 0;                                          // then, pair by pair and tile by tile, what is not among the units
+    for (;;) {
+        const bool units = u < end;
+        int b, head, from = 0, to = 0x7fffffff / 4;
+        bool partial = false;
+        int64_t at = 0;
+        if (units) {
+            b = sequence_at(cut, p.c.B, u);
+            const int n = uniform(cut.share[b]), in = u - uniform(cut.begin[b]);
+            head = in / n;
+            from = in - head * n;
+            to = min(n, from + end - u);
+            partial = from > 0 || to < n;
+            at = ((int64_t)2 * wg + (u == begin ? 0 : 1)) * ROWS;
+            u += to - from;
+        } else {
+            if (bh >= p.c.B * p.c.H) break;
+            b = bh / p.c.H;
+            head = bh - b * p.c.H;
+            if (uniform(cut.share[b]) || tile * ROWS >= uniform(cut.rows[b]) * p.G) {
+                bh += gridDim.x;
+                tile = 0;
+                continue;
+            }
         }
+        const Sequence seq = sequence_of(cut, b);
+        const Tile t = tile_of<ROWS>(p, seq, tile);
+        tile += !units;
+        few_rows<KB, VB, NT, NW>(p, smem, b, head, seq, t.row0, t.row_end, t.span, 4 * from, min(t.span.steps, 4 * to), partial, at);
     }
 }
 
-// Joins the partial results of row r of every (sequence, head) pair that more than one workgroup had: blockIdx (pair, row).  The waves take the workgroups in turn.
+// Joins the partial results of the (sequence, head) pairs that more than one workgroup had: blockIdx (pair, part of its rows).  Up to 16 workgroups: a wave a row;
+// more: a row at a time, its workgroups dealt out to the waves.
 template <int NT>
 __global__ __launch_bounds__(ATT_NT) void balanced_join_kernel(AttnDev p, int workgroups) {
     __shared__ float tops[ATT_WAVES], totals[ATT_WAVES], sums[ATT_WAVES][ATT_D];
@@ -751,46 +796,49 @@ __global__ __launch_bounds__(ATT_NT) void balanced_join_kernel(AttnDev p, int wo
     const int l = threadIdx.x & 63;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int b = blockIdx.x / p.c.H, head = blockIdx.x - b * p.c.H;
-    const Sequence seq = sequence_of(p.c, b);
-    const Cut cut = cut_of<ROWS>(p, workgroups);
-    const int n = share_of<ROWS>(p, seq), u = first_unit(cut, b) + head * n;
-    const int first = u / cut.per, last = (u + n - 1) / cut.per;
+    __shared__ Cut cut;
+    make_cut<ROWS>(p, workgroups, cut);
+    const Sequence seq = sequence_of(cut, b);
+    const int n = uniform(cut.share[b]), per = uniform(cut.per), u = uniform(cut.begin[b]) + head * n;
+    const int first = u / per, last = (u + n - 1) / per;
     if (n == 0 || first == last) return;
-    for (int r = blockIdx.y; r < seq.rows * p.G; r += gridDim.y) {
-        auto place = [&](int wg) { return ((int64_t)2 * wg + (wg > first || u == first * cut.per ? 0 : 1)) * ROWS + r; };
-        // each wave its workgroups, eight at a time, with a reference of its own
+    constexpr int AT_ONCE = 16;
+    const bool together = last - first >= AT_ONCE;
+    for (int r = together ? blockIdx.y : ATT_WAVES * blockIdx.y + w; r < seq.rows * p.G; r += together ? gridDim.y : ATT_WAVES * gridDim.y) {
+        auto place = [&](int wg) { return ((int64_t)2 * wg + (wg > first || u == first * per ? 0 : 1)) * ROWS + r; };
+        const int from = together ? first + w : first, by = together ? ATT_WAVES : 1;
         float top = ATT_NONE, sum = 0.0f, o0 = 0.0f, o1 = 0.0f;
-        for (int k = first + w; k <= last; k += 8 * ATT_WAVES) {
-            float2 s[8], v[8];
+        for (int k = from; k <= last; k += AT_ONCE * by) {
+            float2 s[AT_ONCE], v[AT_ONCE];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int64_t at = place(min(k + ATT_WAVES * e, last));
+            for (int e = 0; e < AT_ONCE; ++e) {
+                const int64_t at = place(min(k + by * e, last));
                 s[e] = reinterpret_cast<const float2*>(p.stats)[at];
                 v[e] = reinterpret_cast<const float2*>(p.part + at * ATT_D)[l];
             }
             float to = top;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) to = __builtin_fmaxf(to, s[e].x);
+            for (int e = 0; e < AT_ONCE; ++e) to = __builtin_fmaxf(to, s[e].x);
             const float f = __builtin_amdgcn_exp2f(top - to);
             top = to;
             sum *= f;
             o0 *= f;
             o1 *= f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float g = k + ATT_WAVES * e <= last ? __builtin_amdgcn_exp2f(s[e].x - to) : 0.0f;
+            for (int e = 0; e < AT_ONCE; ++e) {
+                const float g = k + by * e <= last ? __builtin_amdgcn_exp2f(s[e].x - to) : 0.0f;
                 sum += s[e].y * g;
                 o0 += v[e].x * g;
                 o1 += v[e].y * g;
             }
         }
-        if (l == 0) {
-            tops[w] = top;
-            totals[w] = sum;
-        }
-        reinterpret_cast<float2*>(sums[w])[l] = float2{o0, o1};
-        __syncthreads();
-        if (w == 0) {
+        if (together) {
+            if (l == 0) {
+                tops[w] = top;
+                totals[w] = sum;
+            }
+            reinterpret_cast<float2*>(sums[w])[l] = float2{o0, o1};
+            __syncthreads();
             float all = tops[0];
 #pragma unroll
             for (int k = 1; k < ATT_WAVES; ++k) all = __builtin_fmaxf(all, tops[k]);
@@ -803,11 +851,12 @@ __global__ __launch_bounds__(ATT_NT) void balanced_join_kernel(AttnDev p, int wo
                 o0 += v.x * f;
                 o1 += v.y * f;
             }
-            const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
-            const int64_t token = seq.first + r / p.G;
-            reinterpret_cast<half2v*>(p.out + token * p.out_stride + (head * p.G + r % p.G) * ATT_D)[l] = half2v{(_Float16)(o0 * inv), (_Float16)(o1 * inv)};
+            __syncthreads();
         }
-        __syncthreads();
+        const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+        const int64_t token = seq.first + r / p.G;
+        if (!together || w == 0)
+            reinterpret_cast<half2v*>(p.out + token * p.out_stride + (head * p.G + r % p.G) * ATT_D)[l] = half2v{(_Float16)(o0 * inv), (_Float16)(o1 * inv)};
     }
 }
 
@@ -1022,14 +1071,15 @@ __global__ __launch_bounds__(ATT_NT, 2) void shared_attention_kernel(AttnDev p) 
                 }
                 float prod[16], sum;
                 auto by = [&](int k) { return fk[k]; };
-                if (weigh<16>(sc, by, vs, ref, prod, sum)) {
-                    const float f = raise_reference<16>(sc, by, vs, ref, [](float top) { return __builtin_fmaxf(top, __shfl_xor(top, 32)); });
+                auto step = [&](int k) { return vs[k]; };
+                if (weigh<16>(sc, by, step, ref, prod, sum)) {
+                    const float f = raise_reference<16>(sc, by, step, ref, [](float top) { return __builtin_fmaxf(top, __shfl_xor(top, 32)); });
                     total *= f;
 #pragma unroll
                     for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
                         for (int k = 0; k < 16; ++k) acc[dt][k] *= f;
-                    weigh<16>(sc, by, vs, ref, prod, sum);
+                    weigh<16>(sc, by, step, ref, prod, sum);
                 }
                 total += sum;
                 half8 pw[2];
@@ -1158,11 +1208,14 @@ __global__ __launch_bounds__(ATT_NT) void attention_join_kernel(AttnDev p) {
 // Compute units of the card: the plan (and with it the workspace) follows from the host's figures alone.
 constexpr int64_t kPlanCus = 256;
 
-AttnPlan attention_plan(int64_t B, int64_t T, int H, int Hq, int64_t max_rows, int64_t max_length) {
+// `length`: of the longest sequence, `seen` of its tokens at most by a row's tile (fewer with a window).  The workspace is that of seen == length: with fewer the
+// launch needs as much or less.
+AttnPlan attention_plan(int64_t B, int64_t T, int H, int Hq, int64_t max_rows, int64_t length, int64_t seen) {
     AttnPlan plan;
     max_rows = max_rows < T ? max_rows : T;                                    // positions and rows are 32-bit numbers
-    max_length = max_length < 0x7fffffff ? max_length : 0x7fffffff;
-    const int64_t rows = max_rows * (Hq / H);
+    length = length < 0x7fffffff ? length : 0x7fffffff;
+    seen = seen < length ? seen : length;
+    const int64_t rows = max_rows * (Hq / H), pairs = B * H;
     plan.tile_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : SH_ROWS * ATT_WAVES;
     plan.splits = 1;
     plan.chunk = 1 << 30;
@@ -1170,24 +1223,30 @@ AttnPlan attention_plan(int64_t B, int64_t T, int H, int Hq, int64_t max_rows, i
     plan.workgroups = 0;
     int64_t partials = 0;
     if (plan.tile_rows <= 32) {
-        const int64_t most = tuned(Knob::ATT_WHOLE_MAX, 2048);
-        if (B * H <= kPlanCus && max_length <= most) {
-            plan.waves = plan.tile_rows == 16 ? 16 : ATT_WAVES;
-        } else if (B <= kBalancedSequences && max_length > (most < 256 ? most : 256)) {
+        // A workgroup a pair, or balanced?  us, measured at 16 rows, u = units of 128 tokens: a pair of 8 waves takes 6 + 0.58 u, of 16 waves 8 + 0.44 u (up to one a CU),
+        // the balanced launch 14 (two kernels and the cut) and what its bytes take, 0.94 u of a pair on every CU, of three quarters of the longest.
+        // 1 x 32 pairs of 1000 tokens 10.7 (8 waves) / 14.6, of 4000 22.0 (16) / 14.8; 128 of 4096 22.7 / 24.7, of 16000 66 / 51; 512 of 4096 46.9 (8) / 52.
+        const double u = (double)(seen + 127) / 128, pair8 = 6 + 0.58 * u, pair16 = 8 + 0.44 * u;
+        int waves = pairs > 2 * kPlanCus ? 4 : pairs > kPlanCus || pair8 < pair16 ? 8 : 16;
+        if (B <= kBalancedSequences && pairs <= kPlanCus && 14 + 0.7 * u * (double)pairs / kPlanCus < (pair8 < pair16 ? pair8 : pair16)) waves = 0;
+        waves = tuned(Knob::ATT_WAVES, waves);
+        if (waves == 0 && B > kBalancedSequences) waves = 4;
+        plan.waves = waves > 4 && plan.tile_rows == 16 ? (waves > 8 ? 16 : 8) : 4;
+        if (waves == 0) {
             plan.workgroups = (int)(kPlanCus * tuned(Knob::ATT_WG_PER_CU, plan.tile_rows == 16 ? 3 : 2));
             partials = (int64_t)plan.workgroups * 2 * plan.tile_rows;
         }
     } else {
-        const int64_t tiles = (rows + plan.tile_rows - 1) / plan.tile_rows, groups = B * H * (tiles > 0 ? tiles : 1);
+        const int64_t tiles = (rows + plan.tile_rows - 1) / plan.tile_rows, groups = pairs * (tiles > 0 ? tiles : 1);
         int64_t splits = (2 * kPlanCus + groups - 1) / groups;
-        const int64_t most = (max_length + 255) / 256;                         // of no less than 256 tokens each
+        const int64_t most = (seen + 255) / 256;                               // of no less than 256 tokens each
         splits = splits < most ? splits : most;
         splits = splits < 1 ? 1 : splits > kMaxSplits ? kMaxSplits : splits;
-        const int64_t per = ((max_length + splits - 1) / splits + 127) / 128 * 128;
+        const int64_t per = ((seen + splits - 1) / splits + 127) / 128 * 128;
         plan.chunk = per < 128 ? 128 : per > (1 << 30) ? 1 << 30 : (int)per;
         const int chunk = tuned(Knob::ATT_CHUNK, 0);
         if (chunk > 0) plan.chunk = (chunk + 127) / 128 * 128;
-        splits = chunk > 0 || splits > 1 ? (max_length + plan.chunk - 1) / plan.chunk : 1;
+        splits = chunk > 0 || splits > 1 ? (seen + plan.chunk - 1) / plan.chunk : 1;
         plan.splits = (int)(splits < 1 ? 1 : splits > kMaxSplits ? kMaxSplits : splits);
         if (plan.splits > 1) partials = T * Hq * plan.splits;
     }
@@ -1205,19 +1264,22 @@ static hipError_t attention_launch_bits(const AttnDev& d, const AttnPlan& plan, 
         const hipError_t e = kernel_occupancy(reinterpret_cast<const void*>(kernel), threads, lds, cache, occ);
         return e == hipSuccess ? launch(kernel, grid, dim3((unsigned)threads), lds, stream, d) : e;
     };
-    static OccCache caches[6];
+    static OccCache caches[7];
     hipError_t e;
     if (plan.workgroups > 0) {
         const dim3 grid((unsigned)plan.workgroups);
-        if (plan.tile_rows == 16) e = go(balanced_attention_kernel<KB, VB, 1, 4>, grid, 256, FewRows<KB, VB, 1, 4>::LDS, caches[0]);
-        else e = go(balanced_attention_kernel<KB, VB, 2, 4>, grid, 256, FewRows<KB, VB, 2, 4>::LDS, caches[1]);
+        if (plan.tile_rows == 16) e = go(balanced_attention_kernel<KB, VB, 1, 4>, grid, 256, FewRows<KB, VB, 1, 4>::LDS + (int)sizeof(Cut), caches[0]);
+        else e = go(balanced_attention_kernel<KB, VB, 2, 4>, grid, 256, FewRows<KB, VB, 2, 4>::LDS + (int)sizeof(Cut), caches[1]);
         if (e != hipSuccess) return e;
         const int64_t rows = max_rows * d.G;
-        const dim3 join(pairs.x, (unsigned)(rows < 1 ? 1 : rows < plan.tile_rows ? rows : plan.tile_rows));
+        // a workgroup a row where there are few pairs and so many partial results of each, else one for four rows
+        const int64_t parts = pairs.x < kPlanCus ? rows : (rows + ATT_WAVES - 1) / ATT_WAVES;
+        const dim3 join(pairs.x, (unsigned)(parts < 1 ? 1 : parts < plan.tile_rows ? parts : plan.tile_rows));
         if (plan.tile_rows == 16) return launch(balanced_join_kernel<1>, join, dim3(ATT_NT), 0, stream, d, plan.workgroups);
         return launch(balanced_join_kernel<2>, join, dim3(ATT_NT), 0, stream, d, plan.workgroups);
     }
     if (plan.tile_rows == 16 && plan.waves == 16) return go(whole_attention_kernel<KB, VB, 1, 16>, pairs, 1024, FewRows<KB, VB, 1, 16>::LDS, caches[2]);
+    if (plan.tile_rows == 16 && plan.waves == 8) return go(whole_attention_kernel<KB, VB, 1, 8>, pairs, 512, FewRows<KB, VB, 1, 8>::LDS, caches[6]);
     if (plan.tile_rows == 16) return go(whole_attention_kernel<KB, VB, 1, 4>, pairs, 256, FewRows<KB, VB, 1, 4>::LDS, caches[3]);
     if (plan.tile_rows == 32) return go(whole_attention_kernel<KB, VB, 2, 4>, pairs, 256, FewRows<KB, VB, 2, 4>::LDS, caches[4]);
     e = go(shared_attention_kernel<KB, VB>, pairs, ATT_NT, SH_LDS, caches[5]);

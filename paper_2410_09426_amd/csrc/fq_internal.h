@@ -176,7 +176,7 @@ struct AttnArgs {
     int window, sinks;
     const uint64_t* visible;  // trees of drafted tokens; null: causal
     float* workspace;
-    int64_t max_rows, max_length;
+    int64_t max_rows;
 };
 // How an attention launch is cut: rows and waves of a workgroup, tokens per split and splits, or the workgroups of a balanced launch (0: none).
 struct AttnPlan {
@@ -185,7 +185,7 @@ struct AttnPlan {
     int64_t stats_at;         // floats of partial channels in the workspace
     int64_t workspace;        // bytes
 };
-AttnPlan attention_plan(int64_t B, int64_t T, int H, int Hq, int64_t max_rows, int64_t max_length);
+AttnPlan attention_plan(int64_t B, int64_t T, int H, int Hq, int64_t max_rows, int64_t length, int64_t seen);
 hipError_t attention_launch(const CacheDev& c, const AttnArgs& a, const AttnPlan& plan, hipStream_t stream);
 
 hipError_t dequant_mxfp4_launch(const uint8_t* codes, const uint8_t* exps, int64_t rows, int n, float* out, hipStream_t stream);
@@ -322,7 +322,7 @@ int cu_count();
 // Tuning overrides (kernel flavour, workgroups per CU, ...), for measurements and for the tests that must reach every code
 // path; kKnobNames (fq_api.hip) has their names in the same order.  Each starts from the environment variable of that name, read
 // once per process, and can be changed with fq_set_tuning.
-enum class Knob { MODE, WG_PER_CU, FORCE_GENERIC, KV_WG_PER_CU, GEMM_TILED, GEMM_WIDE, GEMM_DEPTH, GEMM_WAVES, GEMM_ROWS, GEMM_TOKENS, GEMM_RING_MAX_T, KV_FOLD_HEADS, KV_FEW, WAVE_TPW, PROBE_SHAPE, ATT_CHUNK, ATT_WG_PER_CU, ATT_WHOLE_MAX, COUNT };
+enum class Knob { MODE, WG_PER_CU, FORCE_GENERIC, KV_WG_PER_CU, GEMM_TILED, GEMM_WIDE, GEMM_DEPTH, GEMM_WAVES, GEMM_ROWS, GEMM_TOKENS, GEMM_RING_MAX_T, KV_FOLD_HEADS, KV_FEW, WAVE_TPW, PROBE_SHAPE, ATT_CHUNK, ATT_WG_PER_CU, ATT_WAVES, COUNT };
 struct KnobState {
     std::atomic<int> state{0};   // 0: environment not read yet, 1: unset (callers use their default), 2: set
     std::atomic<int> value{0};

@@ -120,7 +120,8 @@ ATTEND = [  # rows, lengths, H, G, page, bits, window, sinks
 ]
 
 
-LAUNCHES = {"chosen": {}, "balanced": {"FLATQUANT_ATT_WHOLE_MAX": 0, "FLATQUANT_ATT_CHUNK": 128}, "balanced, few": {"FLATQUANT_ATT_WHOLE_MAX": 0, "FLATQUANT_ATT_WG_PER_CU": 1}}
+LAUNCHES = {"chosen": {}, "balanced": {"FLATQUANT_ATT_WAVES": 0, "FLATQUANT_ATT_CHUNK": 128}, "balanced, few": {"FLATQUANT_ATT_WAVES": 0, "FLATQUANT_ATT_WG_PER_CU": 1},
+            "4 waves": {"FLATQUANT_ATT_WAVES": 4}, "8 waves": {"FLATQUANT_ATT_WAVES": 8}, "16 waves": {"FLATQUANT_ATT_WAVES": 16}}
 
 
 @pytest.mark.parametrize("launch", LAUNCHES)
