@@ -66,16 +66,21 @@ __device__ __forceinline__ uint32_t as_u32(half2v x) { return __builtin_bit_cast
 // instructions take at its value.  They align the products to the largest of them, though, by its exponent as if it were normalised, and drop what
 // lies 24 bits below (measured: one code unit beside others is off by up to 2^-13.4 of itself at S = 0, by nothing at 2 and above for weights within
 // a factor of 20): S is 2 at least.
-template <int QB, int S>
+// RAISED: with 1024 in the exponent, 1024 + 2^S code.
+constexpr uint32_t kRaise = 0x64006400u;
+template <int QB, int S, bool RAISED>
 __device__ __forceinline__ uint32_t field(uint32_t x) {
     static_assert(S >= 2 && S + QB <= 10, "mantissa bits");
-    return x & ((((1u << QB) - 1u) << S) * 0x00010001u);
+    constexpr uint32_t mask = (((1u << QB) - 1u) << S) * 0x00010001u;
+    if constexpr (!RAISED) return x & mask;
+    uint32_t r;                                                                // (one instruction: of two constants the compiler makes two)
+    asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(r) : "v"(x), "s"(mask), "v"(kRaise));
+    return r;
 }
-// code - zero point of such a field; `z`: 1024 + the zero points, in fp16.  1024 in the exponent makes it 1024 + 2^S code; one packed fma takes
-// 1024 and the zero point off, exactly.
+// code - zero point of a raised field; `z`: 1024 + the zero points, in fp16.  One packed fma takes 1024 and the zero point off, exactly.
 template <int S>
 __device__ __forceinline__ half2v code_value(uint32_t f, half2v z) {
-    const half2v raised = as_half2(f | 0x64006400u);
+    const half2v raised = as_half2(f);
     constexpr _Float16 down = (_Float16)(1.0f / (float)(1 << S)), off = (_Float16)(1024.0f - 1024.0f / (float)(1 << S));
     return __builtin_elementwise_fma(raised, half2v{down, down}, half2v{off, off} - z);
 }
@@ -92,13 +97,14 @@ struct KeyCodes<4> {
     static constexpr int first(int p) { return 8 * (p >> 2) + (p & 3); }
     static constexpr int second(int p) { return first(p) + 4; }
     static constexpr int shift(int p) { return p & 1 ? 6 : 2; }
+    template <bool RAISED>
     static __device__ __forceinline__ void fields(const words& w, uint32_t (&o)[16]) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            o[4 * k] = field<4, 2>(w[k] << 2);
-            o[4 * k + 1] = field<4, 6>(w[k] << 2);
-            o[4 * k + 2] = field<4, 2>(w[k] >> 6);
-            o[4 * k + 3] = field<4, 6>(w[k] >> 6);
+            o[4 * k] = field<4, 2, RAISED>(w[k] << 2);
+            o[4 * k + 1] = field<4, 6, RAISED>(w[k] << 2);
+            o[4 * k + 2] = field<4, 2, RAISED>(w[k] >> 6);
+            o[4 * k + 3] = field<4, 6, RAISED>(w[k] >> 6);
         }
     }
 };
@@ -109,17 +115,18 @@ struct KeyCodes<2> {
     static constexpr int first(int p) { return 16 * (p >> 3) + (p & 7); }
     static constexpr int second(int p) { return first(p) + 8; }
     static constexpr int shift(int p) { return shift2(p & 7); }
+    template <bool RAISED>
     static __device__ __forceinline__ void fields(const words& w, uint32_t (&o)[16]) {
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-            o[8 * k] = field<2, 4>(w[k] << 4);
-            o[8 * k + 1] = field<2, 6>(w[k] << 4);
-            o[8 * k + 2] = field<2, 8>(w[k] << 4);
-            o[8 * k + 3] = field<2, 6>(w[k]);
-            o[8 * k + 4] = field<2, 8>(w[k]);
-            o[8 * k + 5] = field<2, 4>(w[k] >> 6);
-            o[8 * k + 6] = field<2, 6>(w[k] >> 6);
-            o[8 * k + 7] = field<2, 8>(w[k] >> 6);
+            o[8 * k] = field<2, 4, RAISED>(w[k] << 4);
+            o[8 * k + 1] = field<2, 6, RAISED>(w[k] << 4);
+            o[8 * k + 2] = field<2, 8, RAISED>(w[k] << 4);
+            o[8 * k + 3] = field<2, 6, RAISED>(w[k]);
+            o[8 * k + 4] = field<2, 8, RAISED>(w[k]);
+            o[8 * k + 5] = field<2, 4, RAISED>(w[k] >> 6);
+            o[8 * k + 6] = field<2, 6, RAISED>(w[k] >> 6);
+            o[8 * k + 7] = field<2, 8, RAISED>(w[k] >> 6);
         }
     }
 };
@@ -133,26 +140,27 @@ struct KeyCodes<3> {
         constexpr int at[16] = {4, 7, 6, 4, 7, 6, 5, 5, 4, 7, 6, 5, 4, 7, 4, 7};
         return at[p];
     }
+    template <bool RAISED>
     static __device__ __forceinline__ void fields(const words& w, uint32_t (&o)[16]) {
         // bits 0 .. 47 in the low halves, 48 .. 95 in the high ones
         const uint32_t x0 = __builtin_amdgcn_perm(w[1], w[0], 0x07060100u), x1 = __builtin_amdgcn_perm(w[2], w[0], 0x05040302u),
                        x2 = __builtin_amdgcn_perm(w[2], w[1], 0x07060100u);
-        o[0] = field<3, 4>(x0 << 4);
-        o[1] = field<3, 7>(x0 << 4);
-        o[2] = field<3, 6>(x0);
-        o[3] = field<3, 4>(x0 >> 5);
-        o[4] = field<3, 7>(x0 >> 5);
-        o[5] = (x0 >> 9 & 0x00400040u) | (x1 << 7 & 0x01800180u);
-        o[6] = field<3, 5>(x1 << 3);
-        o[7] = field<3, 5>(x1);
-        o[8] = field<3, 4>(x1 >> 4);
-        o[9] = field<3, 7>(x1 >> 4);
-        o[10] = (x1 >> 8 & 0x00C000C0u) | (x2 << 8 & 0x01000100u);
-        o[11] = field<3, 5>(x2 << 4);
-        o[12] = field<3, 4>(x2);
-        o[13] = field<3, 7>(x2);
-        o[14] = field<3, 4>(x2 >> 6);
-        o[15] = field<3, 7>(x2 >> 6);
+        o[0] = field<3, 4, RAISED>(x0 << 4);
+        o[1] = field<3, 7, RAISED>(x0 << 4);
+        o[2] = field<3, 6, RAISED>(x0);
+        o[3] = field<3, 4, RAISED>(x0 >> 5);
+        o[4] = field<3, 7, RAISED>(x0 >> 5);
+        o[5] = (x0 >> 9 & 0x00400040u) | (x1 << 7 & 0x01800180u) | (RAISED ? kRaise : 0u);
+        o[6] = field<3, 5, RAISED>(x1 << 3);
+        o[7] = field<3, 5, RAISED>(x1);
+        o[8] = field<3, 4, RAISED>(x1 >> 4);
+        o[9] = field<3, 7, RAISED>(x1 >> 4);
+        o[10] = (x1 >> 8 & 0x00C000C0u) | (x2 << 8 & 0x01000100u) | (RAISED ? kRaise : 0u);
+        o[11] = field<3, 5, RAISED>(x2 << 4);
+        o[12] = field<3, 4, RAISED>(x2);
+        o[13] = field<3, 7, RAISED>(x2);
+        o[14] = field<3, 4, RAISED>(x2 >> 6);
+        o[15] = field<3, 7, RAISED>(x2 >> 6);
     }
 };
 
@@ -163,36 +171,36 @@ struct ValueCodes {
         constexpr int at[8] = {4, 7, 6, 4, 7, 6, 5, 5};
         return QB == 4 ? (c & 1 ? 6 : 2) : QB == 2 ? shift2(c) : at[c];
     }
-    template <int HALF>
+    template <int HALF, bool RAISED>
     static __device__ __forceinline__ void fields(uint32_t a, uint32_t b, uint32_t (&o)[4]) {
         const uint32_t x = __builtin_amdgcn_perm(b, a, 0x05040100u);
         if constexpr (QB == 4) {
             const uint32_t y = HALF ? __builtin_amdgcn_perm(b, a, 0x07060302u) : x;
-            o[0] = field<4, 2>(y << 2);
-            o[1] = field<4, 6>(y << 2);
-            o[2] = field<4, 2>(y >> 6);
-            o[3] = field<4, 6>(y >> 6);
+            o[0] = field<4, 2, RAISED>(y << 2);
+            o[1] = field<4, 6, RAISED>(y << 2);
+            o[2] = field<4, 2, RAISED>(y >> 6);
+            o[3] = field<4, 6, RAISED>(y >> 6);
         } else if constexpr (QB == 2 && HALF == 0) {
-            o[0] = field<2, 4>(x << 4);
-            o[1] = field<2, 6>(x << 4);
-            o[2] = field<2, 8>(x << 4);
-            o[3] = field<2, 6>(x);
+            o[0] = field<2, 4, RAISED>(x << 4);
+            o[1] = field<2, 6, RAISED>(x << 4);
+            o[2] = field<2, 8, RAISED>(x << 4);
+            o[3] = field<2, 6, RAISED>(x);
         } else if constexpr (QB == 2) {
-            o[0] = field<2, 8>(x);
-            o[1] = field<2, 4>(x >> 6);
-            o[2] = field<2, 6>(x >> 6);
-            o[3] = field<2, 8>(x >> 6);
+            o[0] = field<2, 8, RAISED>(x);
+            o[1] = field<2, 4, RAISED>(x >> 6);
+            o[2] = field<2, 6, RAISED>(x >> 6);
+            o[3] = field<2, 8, RAISED>(x >> 6);
         } else if constexpr (HALF == 0) {
-            o[0] = field<3, 4>(x << 4);
-            o[1] = field<3, 7>(x << 4);
-            o[2] = field<3, 6>(x);
-            o[3] = field<3, 4>(x >> 5);
+            o[0] = field<3, 4, RAISED>(x << 4);
+            o[1] = field<3, 7, RAISED>(x << 4);
+            o[2] = field<3, 6, RAISED>(x);
+            o[3] = field<3, 4, RAISED>(x >> 5);
         } else {
             const uint32_t y = __builtin_amdgcn_perm(b, a, 0x07060302u);
-            o[0] = field<3, 7>(x >> 5);
-            o[1] = (x >> 9 & 0x00400040u) | (y << 7 & 0x01800180u);
-            o[2] = field<3, 5>(y << 3);
-            o[3] = field<3, 5>(y);
+            o[0] = field<3, 7, RAISED>(x >> 5);
+            o[1] = (x >> 9 & 0x00400040u) | (y << 7 & 0x01800180u) | (RAISED ? kRaise : 0u);
+            o[2] = field<3, 5, RAISED>(y << 3);
+            o[3] = field<3, 5, RAISED>(y);
         }
     }
 };
@@ -305,16 +313,24 @@ __device__ __forceinline__ Sequence sequence_of(const CacheDev& c, int b) {
     return s;
 }
 
-// Whether a row at position `pos` (in a tree: the last token before the draft, and `seen`) sees token k.
-__device__ __forceinline__ bool sees(const AttnDev& p, int k, int pos, int before, uint64_t seen) {
-    bool ok = k <= pos;
-    if (p.visible) {
-        const int bit = k - before;
-        ok = ok || (bit >= 0 && bit < 64 && (seen >> (bit & 63) & 1));
-    } else if (p.window > 0) {
-        ok = ok && ((int64_t)k > (int64_t)pos - p.window || k < p.sinks);
-    }
-    return ok;
+// Whether a row sees token k: its bounds are [lo, hi], below `firsts`, or (in a tree) the bits of `seen` from token `before` on.
+struct Sight {
+    int lo, hi, firsts;
+    uint64_t seen;
+};
+__device__ __forceinline__ Sight sight_of(const AttnDev& p, int before, int token, int row) {
+    Sight s;
+    s.hi = p.visible ? before - 1 : before + token;
+    const int64_t lo = (int64_t)s.hi - p.window + 1;
+    s.lo = !p.visible && p.window > 0 && lo > 0 ? (int)lo : 0;
+    s.firsts = !p.visible && p.window > 0 ? (p.sinks < s.hi + 1 ? p.sinks : s.hi + 1) : 0;
+    s.seen = p.visible ? p.visible[row] : 0;
+    return s;
+}
+__device__ __forceinline__ bool sees(const Sight& s, int k) { return ((k >= s.lo) & (k <= s.hi)) | (k < s.firsts); }
+__device__ __forceinline__ bool sees_drafted(const Sight& s, int before, int k) {
+    const unsigned bit = (unsigned)k - (unsigned)before;
+    return (bit < 64u) & (int)((bit & 32 ? (uint32_t)(s.seen >> 32) : (uint32_t)s.seen) >> (bit & 31) & 1u);
 }
 // The step of a value that not every row sees: a number, so that a weight of zero makes a product of zero whatever the page holds.
 __device__ __forceinline__ float finite_step(float s) { return __builtin_fminf(s, 65504.0f); }
@@ -406,8 +422,7 @@ __device__ __forceinline__ void few_rows(const AttnDev& p, unsigned char* smem, 
     // Rows: queries in the order of the codes, brought up to 2^9 and down by the codes' shifts (a power of two each, and back in `factor`; the sign of the
     // scale is in the queries), their sums, positions.  Asked for before the first steps: loads return in order.
     half8 raw[NT][4];
-    int pos[NT];
-    uint64_t seen[NT];
+    Sight sight[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         int r = row0 + 16 * n + i;
@@ -416,8 +431,7 @@ __device__ __forceinline__ void few_rows(const AttnDev& p, unsigned char* smem, 
         const _Float16* src = p.q + (seq.first + token) * p.q_stride + (head * p.G + sub) * ATT_D + 32 * g;
 #pragma unroll
         for (int m = 0; m < 4; ++m) raw[n][m] = *reinterpret_cast<const half8*>(src + 8 * m);
-        pos[n] = p.visible ? before - 1 : before + token;
-        seen[n] = p.visible ? p.visible[seq.first + token] : 0;
+        sight[n] = sight_of(p, before, token, seq.first + token);
     }
     __builtin_amdgcn_sched_barrier(0);
     if (any)
@@ -474,7 +488,7 @@ __device__ __forceinline__ void few_rows(const AttnDev& p, unsigned char* smem, 
         for (int t = 0; t < 2; ++t) {
             __builtin_amdgcn_sched_barrier(0);
             uint32_t kk[16];
-            KeyCodes<KB>::fields(ring_key<KB>(slot + t * R::K_PIECE, i, g), kk);
+            KeyCodes<KB>::template fields<false>(ring_key<KB>(slot + t * R::K_PIECE, i, g), kk);
 #pragma unroll
             for (int n = 0; n < NT; ++n) sc[n][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
@@ -509,9 +523,13 @@ __device__ __forceinline__ void few_rows(const AttnDev& p, unsigned char* smem, 
                 for (int r = 0; r < 4; ++r) {
                     const int k = k0 + 16 * t + 4 * g + r;
                     vp[4 * t + r] = usable_parameters(vp[4 * t + r]);
+                    const bool held = page_ok & (k < span.end);
 #pragma unroll
-                    for (int n = 0; n < NT; ++n)
-                        sc[n][t][r] = sees(p, k, pos[n], before, seen[n]) && page_ok && k < span.end ? sc[n][t][r] : -__builtin_inff();
+                    for (int n = 0; n < NT; ++n) {
+                        bool ok = sees(sight[n], k);
+                        if (p.visible) ok |= sees_drafted(sight[n], before, k);
+                        sc[n][t][r] = ok & held ? sc[n][t][r] : -__builtin_inff();
+                    }
                 }
             }
         }
@@ -548,7 +566,7 @@ __device__ __forceinline__ void few_rows(const AttnDev& p, unsigned char* smem, 
             constexpr int HALF = decltype(part)::value;
             uint32_t vv[4][4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) ValueCodes<VB>::template fields<HALF>(vc[2 * k], vc[2 * k + 1], vv[k]);
+            for (int k = 0; k < 4; ++k) ValueCodes<VB>::template fields<HALF, false>(vc[2 * k], vc[2 * k + 1], vv[k]);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const u32x4 a = {vv[0][j], vv[1][j], vv[2][j], vv[3][j]};
@@ -860,15 +878,26 @@ __global__ __launch_bounds__(ATT_NT) void balanced_join_kernel(AttnDev p, int wo
     }
 }
 
+// In the block that this stands in: N times a matrix instruction and then M vector instructions.
+template <int N, int M>
+__device__ __forceinline__ void interleave() {
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, M, 0);
+    }
+}
+
 // ---- many rows: the tokens' codes become fp16 once per workgroup
 //
 // Four waves of 32 rows each on v_mfma_f32_32x32x16_f16, 64 tokens a step: waves 0 and 1 turn the keys of one half of them into fp16,
 // waves 2 and 3 the values, into the LDS buffer of the next step.  Keys lie row by row in the order of their codes, values channel by
-// channel with the eight tokens of a fragment (those whose weights a lane holds) in 16 bytes; 16-byte chunks are exchanged by row so that
-// the reads of a fragment spread over all banks.
+// channel with the eight tokens of a fragment (those whose weights a lane holds) in 16 bytes.  16 bytes of padding a row spread the reads of a fragment
+// over all banks, and leave one address a lane and constants (chunks exchanged by row took 45 registers of addresses, and spilled).
 
 constexpr int SH_ROWS = 32;                // rows per wave
-constexpr int SH_K_BYTES = 64 * ATT_D * 2, SH_V_BYTES = ATT_D * 64 * 2, SH_STEP_BYTES = 2 * 64 * 4;
+constexpr int SH_K_PITCH = 2 * ATT_D + 16, SH_V_PITCH = 2 * 64 + 16;
+constexpr int SH_K_BYTES = 64 * SH_K_PITCH, SH_V_BYTES = ATT_D * SH_V_PITCH, SH_STEP_BYTES = 2 * 64 * 4;
 constexpr int SH_BUFFER = SH_K_BYTES + SH_V_BYTES + SH_STEP_BYTES;
 constexpr int SH_LDS = 2 * SH_BUFFER;
 
@@ -907,8 +936,7 @@ __global__ __launch_bounds__(ATT_NT, 2) void shared_attention_kernel(AttnDev p) 
         int r = wrow0 + c;
         r = r < row_end ? r : row_end - 1;
         const int token = r / p.G, sub = r - token * p.G;
-        const int pos = p.visible ? before - 1 : before + token;
-        const uint64_t seen = p.visible ? p.visible[seq.first + token] : 0;
+        const Sight sight = sight_of(p, before, token, seq.first + token);
         half8 q[8];                                                            // fragment k: chunk 2 k + h of the key rows
         {
             const _Float16* src = p.q + (seq.first + token) * p.q_stride + (head * p.G + sub) * ATT_D;
@@ -936,16 +964,17 @@ __global__ __launch_bounds__(ATT_NT, 2) void shared_attention_kernel(AttnDev p) 
         float ref = ATT_NONE, total = 0.0f;
 
         // codes of steps x and x + 1 of the span, 32 tokens each, which need not follow each other
-        auto load = [&](int x, ShareCodes& s) {
-            int pg[4], k0[2];
-            s.pages = 0;
+        auto pages_of = [&](int x, int (&pg)[4]) {
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const int xx = x + (k >> 1) < span.steps ? x + (k >> 1) : span.steps - 1;
-                k0[k >> 1] = span.token(xx);
-                const int j = (k0[k >> 1] + 16 * (k & 1)) >> p.c.page_shift;
-                pg[k] = table[j < p.c.table_width ? j : p.c.table_width - 1];  // (behind the width: behind the end)
+                const unsigned j = (unsigned)(span.token(x + (k >> 1)) + 16 * (k & 1)) >> p.c.page_shift;
+                pg[k] = table[j < (unsigned)p.c.table_width ? j : p.c.table_width - 1];    // (behind the width: behind the end)
             }
+        };
+        auto load = [&](int x, const int (&table_pages)[4], ShareCodes& s) {
+            int pg[4] = {table_pages[0], table_pages[1], table_pages[2], table_pages[3]};
+            const int k0[2] = {span.token(x), span.token(x + 1)};
+            s.pages = 0;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const bool ok = (unsigned)pg[k] < (unsigned)p.c.pages;
@@ -988,7 +1017,7 @@ __global__ __launch_bounds__(ATT_NT, 2) void shared_attention_kernel(AttnDev p) 
 #pragma unroll
                     for (int k = 0; k < KB; ++k) cw[k] = s.w[KB * half + k];
                     uint32_t kk[16];
-                    KeyCodes<KB>::fields(cw, kk);
+                    KeyCodes<KB>::template fields<true>(cw, kk);
                     each<4>([&](auto mm) {
                         constexpr int m = decltype(mm)::value;
                         const int chunk = 4 * (2 * h + half) + m;
@@ -997,7 +1026,7 @@ __global__ __launch_bounds__(ATT_NT, 2) void shared_attention_kernel(AttnDev p) 
                             constexpr int e = decltype(ee)::value;
                             o[e] = as_u32(code_value<KeyCodes<KB>::shift(4 * m + e)>(kk[4 * m + e], z));
                         });
-                        *reinterpret_cast<u32x4*>(base + tok * 256 + ((chunk ^ (tok & 15)) << 4)) = o;
+                        *reinterpret_cast<u32x4*>(base + tok * SH_K_PITCH + 16 * chunk) = o;
                     });
                 }
                 if (h == 0) steps[tok] = step_of(s.params[0]) * p.scale2;
@@ -1011,15 +1040,15 @@ __global__ __launch_bounds__(ATT_NT, 2) void shared_attention_kernel(AttnDev p) 
                     for (int k = 0; k < 4; ++k) {
                         z[k] = raised_zeros(s.params[2 * k], s.params[2 * k + 1]);
                         const int down = VB == 3 && i == 15 ? 8 : 0;
-                        ValueCodes<VB>::template fields<HALF>(s.w[2 * k] >> down, s.w[2 * k + 1] >> down, vv[k]);
+                        ValueCodes<VB>::template fields<HALF, true>(s.w[2 * k] >> down, s.w[2 * k + 1] >> down, vv[k]);
                     }
                     each<4>([&](auto jj) {
                         constexpr int j = decltype(jj)::value;
-                        const int d = 8 * i + 4 * HALF + j;
+                        const int row = 16 * (4 * HALF + j) + i;               // of channel 8 i + 4 HALF + j: the lanes' rows lie next to each other
                         u32x4 o;
 #pragma unroll
                         for (int k = 0; k < 4; ++k) o[k] = as_u32(code_value<ValueCodes<VB>::shift(4 * HALF + j)>(vv[k][j], z[k]));
-                        *reinterpret_cast<u32x4*>(base + SH_K_BYTES + d * 128 + ((chunk ^ ((d >> 3 ^ d) & 7)) << 4)) = o;
+                        *reinterpret_cast<u32x4*>(base + SH_K_BYTES + row * SH_V_PITCH + 16 * chunk) = o;
                     });
                 };
                 values(std::integral_constant<int, 0>{});
@@ -1032,83 +1061,105 @@ __global__ __launch_bounds__(ATT_NT, 2) void shared_attention_kernel(AttnDev p) 
                 }
             }
         };
-        auto work = [&](int x, int buf, int pages) {
-            const unsigned char* base = sh_smem + buf * SH_BUFFER;
-            const float* steps = reinterpret_cast<const float*>(base + SH_K_BYTES + SH_V_BYTES) + 4 * h;
+        // Two tiles of 32 tokens a step.  The matrix instructions of one stage stand between the vector instructions of another:
+        // QK of tile 0 with the conversion of the next step, QK of tile 1 with the weights of tile 0, PV of tile 0 with the weights of tile 1.
+        auto scores = [&](const unsigned char* base, int t, f32x16& sc) {
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                if (x + t >= x_end) break;
-                const int k0 = span.token(x + t);
-                if (!p.visible && k0 > pos_hi) break;                          // (the first tokens lie before everything else)
-                f32x16 sc;
+            for (int k = 0; k < 16; ++k) sc[k] = 0.0f;
+            half8 a[8];
 #pragma unroll
-                for (int k = 0; k < 16; ++k) sc[k] = 0.0f;
+            for (int k = 0; k < 8; ++k) a[k] = *reinterpret_cast<const half8*>(base + (32 * t + c) * SH_K_PITCH + 16 * h + 32 * k);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const half8 a = *reinterpret_cast<const half8*>(base + (32 * t + c) * 256 + (((2 * k + h) ^ (c & 15)) << 4));
-                    sc = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, q[k], sc, 0, 0, 0);
-                }
-                float vs[16], fk[16];
+            for (int k = 0; k < 8; ++k) sc = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[k], q[k], sc, 0, 0, 0);
+        };
+        auto factors = [&](const unsigned char* base, int at, float (&f)[16]) {
+            const float* from = reinterpret_cast<const float*>(base + SH_K_BYTES + SH_V_BYTES) + at + 4 * h;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const f32x4 a = *reinterpret_cast<const f32x4*>(steps + 32 * t + 8 * k), z = *reinterpret_cast<const f32x4*>(steps + 64 + 32 * t + 8 * k);
+            for (int k = 0; k < 4; ++k) {
+                const f32x4 v = *reinterpret_cast<const f32x4*>(from + 8 * k);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        fk[4 * k + e] = a[e];
-                        vs[4 * k + e] = z[e];
-                    }
-                }
-                const int pages_ok = pages >> (2 * t) & 3, all_see = p.visible ? before - 1 : pos_lo;
-                if (!(pages_ok == 3 && k0 + 31 <= all_see && k0 + 32 <= span.end && (p.window <= 0 || p.visible || k0 > pos_hi - p.window))) {
-#pragma unroll
-                    for (int k = 0; k < 16; ++k) {
-                        const int kk = k0 + 8 * (k >> 2) + 4 * h + (k & 3);
-                        const bool ok = sees(p, kk, pos, before, seen) && (pages_ok >> (k >> 3) & 1) && kk < span.end;
-                        sc[k] = ok ? sc[k] * fk[k] : -__builtin_inff();
-                        fk[k] = 1.0f;
-                        vs[k] = finite_step(vs[k]);
-                    }
-                }
-                float prod[16], sum;
-                auto by = [&](int k) { return fk[k]; };
-                auto step = [&](int k) { return vs[k]; };
-                if (weigh<16>(sc, by, step, ref, prod, sum)) {
-                    const float f = raise_reference<16>(sc, by, step, ref, [](float top) { return __builtin_fmaxf(top, __shfl_xor(top, 32)); });
-                    total *= f;
-#pragma unroll
-                    for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-                        for (int k = 0; k < 16; ++k) acc[dt][k] *= f;
-                    weigh<16>(sc, by, step, ref, prod, sum);
-                }
-                total += sum;
-                half8 pw[2];
-#pragma unroll
-                for (int k = 0; k < 16; ++k) pw[k >> 3][k & 7] = (_Float16)prod[k];
-#pragma unroll
-                for (int s = 0; s < 2; ++s)
-#pragma unroll
-                    for (int dt = 0; dt < 4; ++dt) {
-                        const int d = 32 * dt + c;
-                        const half8 a = *reinterpret_cast<const half8*>(base + SH_K_BYTES + d * 128 + (((4 * t + 2 * s + h) ^ ((d >> 3 ^ d) & 7)) << 4));
-                        acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, pw[s], acc[dt], 0, 0, 0);
-                    }
+                for (int e = 0; e < 4; ++e) f[4 * k + e] = v[e];
             }
+        };
+        // scores of tokens that a row does not see: -infinity (the factors are one then, and the steps numbers)
+        auto mask = [&](int x, int t, int pages, f32x16& sc, float (&fk)[16], float (&vs)[16]) {
+            const int k0 = span.token(x + t);
+            const int pages_ok = pages >> (2 * t) & 3, all_see = p.visible ? before - 1 : pos_lo;
+            if (pages_ok == 3 && k0 + 31 <= all_see && k0 + 32 <= span.end && x + t < x_end && (p.window <= 0 || p.visible || k0 > pos_hi - p.window)) return;
+            const int end = x + t < x_end ? span.end : 0;
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+                const int kk = k0 + 8 * (k >> 2) + 4 * h + (k & 3);
+                bool ok = sees(sight, kk);
+                if (p.visible) ok |= sees_drafted(sight, before, kk);
+                sc[k] = ok & (kk < end) & (pages_ok >> (k >> 3) & 1) ? sc[k] * fk[k] : -__builtin_inff();
+                fk[k] = 1.0f;
+                vs[k] = finite_step(vs[k]);
+            }
+        };
+        auto raise = [&](const f32x16& sc, const float (&fk)[16], const float (&vs)[16], float (&prod)[16], float& sum) {
+            auto by = [&](int k) { return fk[k]; };
+            auto step = [&](int k) { return vs[k]; };
+            const float f = raise_reference<16>(sc, by, step, ref, [](float top) { return __builtin_fmaxf(top, __shfl_xor(top, 32)); });
+            total *= f;
+#pragma unroll
+            for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+                for (int k = 0; k < 16; ++k) acc[dt][k] *= f;
+            weigh<16>(sc, by, step, ref, prod, sum);
+        };
+        auto values = [&](const unsigned char* base, int t, const half8 (&pw)[2]) {
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int dt = 0; dt < 4; ++dt) {
+                    const half8 a = *reinterpret_cast<const half8*>(base + SH_K_BYTES + (32 * dt + c) * SH_V_PITCH + 16 * h + 64 * t + 32 * s);
+                    acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, pw[s], acc[dt], 0, 0, 0);
+                }
+        };
+        auto halves = [&](const float (&prod)[16], half8 (&pw)[2]) {
+#pragma unroll
+            for (int k = 0; k < 16; ++k) pw[k >> 3][k & 7] = (_Float16)prod[k];
         };
 
         if (x_begin < x_end) {
             ShareCodes s;
-            load(x_begin, s);
+            int pg[4], next[4];
+            pages_of(x_begin, pg);
+            pages_of(x_begin + 2, next);
+            load(x_begin, pg, s);
             convert(s, 0);
             int pages = s.pages;
-            load(x_begin + 2, s);
+            load(x_begin + 2, next, s);
+            pages_of(x_begin + 4, next);
             __syncthreads();
             int buf = 0;
             for (int x = x_begin; x < x_end; x += 2) {
-                if (busy) work(x, buf, pages);
+                const unsigned char* base = sh_smem + buf * SH_BUFFER;
+                const bool sees_some = busy && (p.visible || span.token(x) <= pos_hi);       // (the first tokens lie before everything else)
+                if (sees_some) {
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        f32x16 sc;
+                        float fk[16], vs[16], prod[16], sum;
+                        half8 pw[2];
+                        auto by = [&](int k) { return fk[k]; };
+                        auto step = [&](int k) { return vs[k]; };
+                        scores(base, t, sc);
+                        factors(base, 32 * t, fk);
+                        factors(base, 64 + 32 * t, vs);
+                        mask(x, t, pages, sc, fk, vs);
+                        if (weigh<16>(sc, by, step, ref, prod, sum)) raise(sc, fk, vs, prod, sum);
+                        total += sum;
+                        halves(prod, pw);
+                        values(base, t, pw);
+                    }
+                }
                 convert(s, buf ^ 1);
-                pages = s.pages;
-                load(x + 4, s);
+                const int next_pages = s.pages;
+                load(x + 4, next, s);
+                pages_of(x + 6, next);
+                pages = next_pages;
                 __syncthreads();
                 buf ^= 1;
             }
@@ -1120,24 +1171,23 @@ __global__ __launch_bounds__(ATT_NT, 2) void shared_attention_kernel(AttnDev p) 
             if (used == 1) {
                 const float inv = total > 0.0f ? 1.0f / total : 0.0f;
                 _Float16* dst = p.out + row_token * p.out_stride + hq * ATT_D;
+                // rows 16 j + i of the product: a lane has all eight j of i = 4 h + {0 .. 3, 8 .. 11}, channels 8 i .. 8 i + 7
 #pragma unroll
-                for (int dt = 0; dt < 4; ++dt)
+                for (int k = 0; k < 8; ++k) {
+                    half8 y;
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        typedef _Float16 half4 __attribute__((ext_vector_type(4)));
-                        half4 y;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) y[e] = (_Float16)(acc[dt][4 * k + e] * inv);
-                        *reinterpret_cast<half4*>(dst + 32 * dt + 8 * k + 4 * h) = y;
-                    }
+                    for (int j = 0; j < 8; ++j) y[j] = (_Float16)(acc[j >> 1][k + 8 * (j & 1)] * inv);
+                    *reinterpret_cast<half8*>(dst + 8 * (8 * (k >> 2) + 4 * h + (k & 3))) = y;
+                }
             } else {
                 const int64_t at = (row_token * p.Hq + hq) * p.splits + blockIdx.z;
                 float* dst = p.part + at * ATT_D;
 #pragma unroll
-                for (int dt = 0; dt < 4; ++dt)
+                for (int k = 0; k < 8; ++k)
 #pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        *reinterpret_cast<f32x4*>(dst + 32 * dt + 8 * k + 4 * h) = f32x4{acc[dt][4 * k], acc[dt][4 * k + 1], acc[dt][4 * k + 2], acc[dt][4 * k + 3]};
+                    for (int j = 0; j < 8; j += 4)
+                        *reinterpret_cast<f32x4*>(dst + 8 * (8 * (k >> 2) + 4 * h + (k & 3)) + j) =
+                            f32x4{acc[j >> 1][k], acc[j >> 1][k + 8], acc[(j >> 1) + 1][k], acc[(j >> 1) + 1][k + 8]};
                 if (h == 0) {
                     reinterpret_cast<float2*>(p.stats)[at] = float2{ref, total};
                 }
