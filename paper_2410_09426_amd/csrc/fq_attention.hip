@@ -878,28 +878,22 @@ __global__ __launch_bounds__(ATT_NT) void balanced_join_kernel(AttnDev p, int wo
     }
 }
 
-// In the block that this stands in: N times a matrix instruction and then M vector instructions.
-template <int N, int M>
-__device__ __forceinline__ void interleave() {
-#pragma unroll
-    for (int k = 0; k < N; ++k) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x002, M, 0);
-    }
-}
-
 // ---- many rows: the tokens' codes become fp16 once per workgroup
 //
-// Four waves of 32 rows each on v_mfma_f32_32x32x16_f16, 64 tokens a step: waves 0 and 1 turn the keys of one half of them into fp16,
-// waves 2 and 3 the values, into the LDS buffer of the next step.  Keys lie row by row in the order of their codes, values channel by
-// channel with the eight tokens of a fragment (those whose weights a lane holds) in 16 bytes.  16 bytes of padding a row spread the reads of a fragment
-// over all banks, and leave one address a lane and constants (chunks exchanged by row took 45 registers of addresses, and spilled).
+// Waves of 32 rows each on v_mfma_f32_32x32x16_f16.  Four of them turn 64 tokens into fp16 in the LDS buffer of the next step (waves 0 and 1 the
+// keys of one half of them, waves 2 and 3 the values) while all attend to those of this one; eight waves take 128 tokens a step, and so convert half as
+// much a row.  Keys lie row by row in the order of their codes, values channel by channel with the eight tokens of a fragment (those whose weights a
+// lane holds) in 16 bytes.  16 bytes of padding a row spread the reads of a fragment over all banks, and leave one address a lane and constants (chunks
+// exchanged by row took 45 registers of addresses, and spilled).
+//
+// Bound by latency in the step: 2048 rows of 64 heads at 8192 tokens take 684 us, in which the matrix cores are busy for 33 %, the LDS for 33 % and the
+// vector units for 40 %.  Without conversion it is 627 of 842 us (of an earlier step), without anything but it 306: two waves a SIMD, all the registers
+// allow, overlap those only in part.  Raised wave priority around the matrix instructions was slower (699 us), around the conversion no faster.
 
 constexpr int SH_ROWS = 32;                // rows per wave
 constexpr int SH_K_PITCH = 2 * ATT_D + 16, SH_V_PITCH = 2 * 64 + 16;
 constexpr int SH_K_BYTES = 64 * SH_K_PITCH, SH_V_BYTES = ATT_D * SH_V_PITCH, SH_STEP_BYTES = 2 * 64 * 4;
 constexpr int SH_BUFFER = SH_K_BYTES + SH_V_BYTES + SH_STEP_BYTES;
-constexpr int SH_LDS = 2 * SH_BUFFER;
 
 // A thread's share of 64 tokens: two quarters of a key, or eight channels of eight values, and which of the four pages of 16 tokens are pages.
 struct ShareCodes {
@@ -907,15 +901,17 @@ struct ShareCodes {
     int pages;                             // (uniform) bit k: tokens 16 k .. of the 64
 };
 
-template <int KB, int VB>
-__global__ __launch_bounds__(ATT_NT, 2) void shared_attention_kernel(AttnDev p) {
+template <int KB, int VB, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void shared_attention_kernel(AttnDev p) {
+    constexpr int PARTS = NW / 4;                                              // of 64 tokens, a step
     extern __shared__ __attribute__((aligned(16))) unsigned char sh_smem[];
     const int l = threadIdx.x & 63, c = l & 31, h = l >> 5;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int b = blockIdx.x / p.c.H, head = blockIdx.x - b * p.c.H;
     const Sequence seq = sequence_of(p.c, b);
     const int all_rows = seq.rows * p.G;
-    constexpr int TILE = SH_ROWS * ATT_WAVES;
+    constexpr int TILE = SH_ROWS * NW;
+    const int part = w / 4, role = w % 4;
     const int tiles = (all_rows + TILE - 1) / TILE;
     const list_t table = (list_t)p.c.page_table + b * p.c.table_stride;
     for (int tile_no = blockIdx.y; tile_no < tiles; tile_no += gridDim.y) {
@@ -964,32 +960,35 @@ __global__ __launch_bounds__(ATT_NT, 2) void shared_attention_kernel(AttnDev p) 
         float ref = ATT_NONE, total = 0.0f;
 
         // codes of steps x and x + 1 of the span, 32 tokens each, which need not follow each other
-        auto pages_of = [&](int x, int (&pg)[4]) {
+        auto pages_of = [&](int x, int (&pg)[NW]) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
+            for (int k = 0; k < NW; ++k) {
                 const unsigned j = (unsigned)(span.token(x + (k >> 1)) + 16 * (k & 1)) >> p.c.page_shift;
                 pg[k] = table[j < (unsigned)p.c.table_width ? j : p.c.table_width - 1];    // (behind the width: behind the end)
             }
         };
-        auto load = [&](int x, const int (&table_pages)[4], ShareCodes& s) {
-            int pg[4] = {table_pages[0], table_pages[1], table_pages[2], table_pages[3]};
-            const int k0[2] = {span.token(x), span.token(x + 1)};
+        auto load = [&](int x, const int (&table_pages)[NW], ShareCodes& s) {
             s.pages = 0;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const bool ok = (unsigned)pg[k] < (unsigned)p.c.pages;
-                s.pages |= (int)ok << k;
-                pg[k] = ok ? pg[k] : 0;
+            for (int k = 0; k < NW; ++k) s.pages |= (int)((unsigned)table_pages[k] < (unsigned)p.c.pages) << k;
+            int pg[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {                                      // of this wave's 32 tokens
+                pg[k] = table_pages[k];
+#pragma unroll
+                for (int other = 1; other < NW / 2; ++other) pg[k] = w % 2 + 2 * part == other ? table_pages[2 * other + k] : pg[k];
+                pg[k] = (unsigned)pg[k] < (unsigned)p.c.pages ? pg[k] : 0;
             }
-            const int mine = w & 1, mask = (1 << p.c.page_shift) - 1;
-            if (w < 2) {                                                       // token c of the half, quarters 2 h and 2 h + 1
-                const int64_t at = (((int64_t)(c < 16 ? pg[2 * mine] : pg[2 * mine + 1]) * p.c.H + head) << p.c.page_shift) + ((k0[mine] + c) & mask);
+            const int k0 = span.token(x + 2 * part + w % 2);
+            const int mask = (1 << p.c.page_shift) - 1;
+            if (role < 2) {                                                    // token c of the half, quarters 2 h and 2 h + 1
+                const int64_t at = (((int64_t)(c < 16 ? pg[0] : pg[1]) * p.c.H + head) << p.c.page_shift) + ((k0 + c) & mask);
                 __builtin_memcpy(s.w, __builtin_assume_aligned(p.c.codes[0] + at * (16 * KB) + h * (8 * KB), 8), 8 * KB);
                 s.params[0] = p.c.params[0][at];
             } else {                                                           // channels 8 i .. 8 i + 7 of tokens 16 (g >> 1) + 4 (g & 1) + {0 .. 3, 8 .. 11}
                 const int i = l & 15, g = l >> 4;
-                const int64_t at = (((int64_t)(g < 2 ? pg[2 * mine] : pg[2 * mine + 1]) * p.c.H + head) << p.c.page_shift) +
-                                   ((k0[mine] + 16 * (g >> 1) + 4 * (g & 1)) & mask);
+                const int64_t at = (((int64_t)(g < 2 ? pg[0] : pg[1]) * p.c.H + head) << p.c.page_shift) +
+                                   ((k0 + 16 * (g >> 1) + 4 * (g & 1)) & mask);
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
                     const uint8_t* row = p.c.codes[1] + (at + (k & 3) + 8 * (k >> 2)) * (16 * VB);
@@ -1006,11 +1005,11 @@ __global__ __launch_bounds__(ATT_NT, 2) void shared_attention_kernel(AttnDev p) 
             }
         };
         auto convert = [&](const ShareCodes& s, int buf) {
-            unsigned char* base = sh_smem + buf * SH_BUFFER;
+            unsigned char* base = sh_smem + (PARTS * buf + part) * SH_BUFFER;
             float* steps = reinterpret_cast<float*>(base + SH_K_BYTES + SH_V_BYTES);
-            if (w < 2) {
+            if (role < 2) {
                 const half2v z = raised_zeros(s.params[0], s.params[0]);
-                const int tok = 32 * w + c;
+                const int tok = 32 * role + c;
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
                     typename KeyCodes<KB>::words cw;
@@ -1031,7 +1030,7 @@ __global__ __launch_bounds__(ATT_NT, 2) void shared_attention_kernel(AttnDev p) 
                 }
                 if (h == 0) steps[tok] = step_of(s.params[0]) * p.scale2;
             } else {
-                const int i = l & 15, g = l >> 4, chunk = 4 * (w - 2) + g;
+                const int i = l & 15, g = l >> 4, chunk = 4 * (role - 2) + g;
                 auto values = [&](auto part) {
                     constexpr int HALF = decltype(part)::value;
                     uint32_t vv[4][4];
@@ -1057,7 +1056,7 @@ __global__ __launch_bounds__(ATT_NT, 2) void shared_attention_kernel(AttnDev p) 
                     float st = 0.0f;
 #pragma unroll
                     for (int k = 0; k < 8; ++k) st = i == k ? step_of(s.params[k]) : st;
-                    steps[64 + 32 * (w - 2) + 16 * (g >> 1) + 4 * (g & 1) + (i & 3) + 8 * (i >> 2)] = st;
+                    steps[64 + 32 * (role - 2) + 16 * (g >> 1) + 4 * (g & 1) + (i & 3) + 8 * (i >> 2)] = st;
                 }
             }
         };
@@ -1124,20 +1123,23 @@ __global__ __launch_bounds__(ATT_NT, 2) void shared_attention_kernel(AttnDev p) 
 
         if (x_begin < x_end) {
             ShareCodes s;
-            int pg[4], next[4];
-            pages_of(x_begin, pg);
-            pages_of(x_begin + 2, next);
-            load(x_begin, pg, s);
+            int next[NW];
+            constexpr int STEPS = 2 * PARTS;
+            pages_of(x_begin, next);
+            load(x_begin, next, s);
+            pages_of(x_begin + STEPS, next);
             convert(s, 0);
             int pages = s.pages;
-            load(x_begin + 2, next, s);
-            pages_of(x_begin + 4, next);
+            load(x_begin + STEPS, next, s);
+            pages_of(x_begin + 2 * STEPS, next);
             __syncthreads();
             int buf = 0;
-            for (int x = x_begin; x < x_end; x += 2) {
-                const unsigned char* base = sh_smem + buf * SH_BUFFER;
-                const bool sees_some = busy && (p.visible || span.token(x) <= pos_hi);       // (the first tokens lie before everything else)
-                if (sees_some) {
+            for (int x = x_begin; x < x_end; x += STEPS) {
+#pragma unroll 1
+                for (int y = 0; y < PARTS; ++y) {
+                    const unsigned char* base = sh_smem + (PARTS * buf + y) * SH_BUFFER;
+                    // (the first tokens lie before everything else)
+                    if (!busy || x + 2 * y >= x_end || !(p.visible || span.token(x + 2 * y) <= pos_hi)) continue;
 #pragma unroll
                     for (int t = 0; t < 2; ++t) {
                         f32x16 sc;
@@ -1148,7 +1150,7 @@ __global__ __launch_bounds__(ATT_NT, 2) void shared_attention_kernel(AttnDev p) 
                         scores(base, t, sc);
                         factors(base, 32 * t, fk);
                         factors(base, 64 + 32 * t, vs);
-                        mask(x, t, pages, sc, fk, vs);
+                        mask(x + 2 * y, t, pages >> (4 * y), sc, fk, vs);
                         if (weigh<16>(sc, by, step, ref, prod, sum)) raise(sc, fk, vs, prod, sum);
                         total += sum;
                         halves(prod, pw);
@@ -1157,8 +1159,8 @@ __global__ __launch_bounds__(ATT_NT, 2) void shared_attention_kernel(AttnDev p) 
                 }
                 convert(s, buf ^ 1);
                 const int next_pages = s.pages;
-                load(x + 4, next, s);
-                pages_of(x + 6, next);
+                load(x + 2 * STEPS, next, s);
+                pages_of(x + 3 * STEPS, next);
                 pages = next_pages;
                 __syncthreads();
                 buf ^= 1;
@@ -1287,14 +1289,21 @@ AttnPlan attention_plan(int64_t B, int64_t T, int H, int Hq, int64_t max_rows, i
             partials = (int64_t)plan.workgroups * 2 * plan.tile_rows;
         }
     } else {
+        // Eight waves convert a token for twice the rows, where they fill every CU and the tokens are many (us, 4 / 8 waves: 2 x 8192 rows of 64 heads at
+        // 8192 tokens 2742 / 2609; 2048 at 2048 132 / 114; 8 x 1024 of 32 heads at 1024 98 / 104; 512 of 64 at 8192, workgroups for half the CUs, 211 / 312).
+        const int64_t groups8 = pairs * ((rows + 2 * plan.tile_rows - 1) / (2 * plan.tile_rows));
+        if (tuned(Knob::ATT_WAVES, groups8 >= kPlanCus && seen >= 2048 ? 8 : 4) == 8) {
+            plan.waves = 8;
+            plan.tile_rows *= 2;
+        }
         const int64_t tiles = (rows + plan.tile_rows - 1) / plan.tile_rows, groups = pairs * (tiles > 0 ? tiles : 1);
         int64_t splits = (2 * kPlanCus + groups - 1) / groups;
         const int64_t most = (seen + 255) / 256;                               // of no less than 256 tokens each
         splits = splits < most ? splits : most;
-        splits = splits < 1 ? 1 : splits > kMaxSplits ? kMaxSplits : splits;
+        splits = splits < 1 || plan.waves == 8 ? 1 : splits > kMaxSplits ? kMaxSplits : splits;
         const int64_t per = ((seen + splits - 1) / splits + 127) / 128 * 128;
         plan.chunk = per < 128 ? 128 : per > (1 << 30) ? 1 << 30 : (int)per;
-        const int chunk = tuned(Knob::ATT_CHUNK, 0);
+        const int chunk = plan.waves == 8 ? 0 : tuned(Knob::ATT_CHUNK, 0);
         if (chunk > 0) plan.chunk = (chunk + 127) / 128 * 128;
         splits = chunk > 0 || splits > 1 ? (seen + plan.chunk - 1) / plan.chunk : 1;
         plan.splits = (int)(splits < 1 ? 1 : splits > kMaxSplits ? kMaxSplits : splits);
@@ -1314,7 +1323,7 @@ static hipError_t attention_launch_bits(const AttnDev& d, const AttnPlan& plan, 
         const hipError_t e = kernel_occupancy(reinterpret_cast<const void*>(kernel), threads, lds, cache, occ);
         return e == hipSuccess ? launch(kernel, grid, dim3((unsigned)threads), lds, stream, d) : e;
     };
-    static OccCache caches[7];
+    static OccCache caches[8];
     hipError_t e;
     if (plan.workgroups > 0) {
         const dim3 grid((unsigned)plan.workgroups);
@@ -1332,7 +1341,8 @@ static hipError_t attention_launch_bits(const AttnDev& d, const AttnPlan& plan, 
     if (plan.tile_rows == 16 && plan.waves == 8) return go(whole_attention_kernel<KB, VB, 1, 8>, pairs, 512, FewRows<KB, VB, 1, 8>::LDS, caches[6]);
     if (plan.tile_rows == 16) return go(whole_attention_kernel<KB, VB, 1, 4>, pairs, 256, FewRows<KB, VB, 1, 4>::LDS, caches[3]);
     if (plan.tile_rows == 32) return go(whole_attention_kernel<KB, VB, 2, 4>, pairs, 256, FewRows<KB, VB, 2, 4>::LDS, caches[4]);
-    e = go(shared_attention_kernel<KB, VB>, pairs, ATT_NT, SH_LDS, caches[5]);
+    if (plan.waves == 8) return go(shared_attention_kernel<KB, VB, 8>, pairs, 512, 4 * SH_BUFFER, caches[7]);
+    e = go(shared_attention_kernel<KB, VB, 4>, pairs, ATT_NT, 2 * SH_BUFFER, caches[5]);
     if (e != hipSuccess || d.splits == 1) return e;
     const int64_t rows = (max_rows * d.G + ATT_WAVES - 1) / ATT_WAVES;
     return launch(attention_join_kernel<SH_ROWS * ATT_WAVES>, dim3(pairs.x, (unsigned)(rows < 1 ? 1 : rows > 65535 ? 65535 : rows)), dim3(ATT_NT), 0, stream, d);
