@@ -330,7 +330,6 @@ fq_status flatquant_cache_write(const fq_kv_cache* cache, const fq_kv_batch* bat
     st = cache_rows(cache, batch, k, k_stride, v, v_stride, r);
     if (st != FQ_OK) return st;
     if ((reinterpret_cast<uintptr_t>(P_k) & 15) || (reinterpret_cast<uintptr_t>(P_v) & 15)) return FQ_MISALIGNED;
-    if (P_k || P_v) return FQ_UNSUPPORTED_SHAPE;
     r.P[0] = static_cast<const _Float16*>(P_k); r.P[1] = static_cast<const _Float16*>(P_v);
     r.Hp = Hp; r.clip[0] = k_clip; r.clip[1] = v_clip;
     return fq::finish(fq::cache_write_launch(d, r, static_cast<hipStream_t>(stream)));

@@ -20,6 +20,7 @@
 // workgroups, whose partial results (M, sum, channels, in fp32) a second kernel joins.
 #include "fq_internal.h"
 #include "fq_device.h"
+#include "fq_cache_device.h"
 
 namespace fq {
 
@@ -31,7 +32,6 @@ constexpr int ATT_PITCH = ATT_D + 4;       // floats per row of partial channels
 constexpr int kMaxSplits = 128;
 constexpr float ATT_NONE = -1e30f;         // reference of a row that has seen nothing: below every finite score
 
-typedef _Float16 half2v __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 // Lists that no kernel writes, read at uniform addresses: by scalar loads, which do not stand in the queue of the codes' loads.
@@ -58,9 +58,6 @@ __device__ __forceinline__ void each(F&& f) {                                  /
 }
 
 // ---- codes to fp16
-
-__device__ __forceinline__ half2v as_half2(uint32_t x) { return __builtin_bit_cast(half2v, x); }
-__device__ __forceinline__ uint32_t as_u32(half2v x) { return __builtin_bit_cast(uint32_t, x); }
 
 // Two codes in bits [S, S + QB) of the halves of x, S + QB <= 10: as fp16 bits that is 2^(S - 24) code, a subnormal number, which the matrix
 // instructions take at its value.  They align the products to the largest of them, though, by its exponent as if it were normalised, and drop what

@@ -167,6 +167,7 @@ struct CacheRows {            // row tensors of a write or a read; a null pointe
 };
 hipError_t cache_write_launch(const CacheDev& c, const CacheRows& r, hipStream_t stream);
 hipError_t cache_read_launch(const CacheDev& c, const CacheRows& r, hipStream_t stream);
+hipError_t kv_paged_launch(const CacheDev& c, const CacheRows& r, int x, hipStream_t stream);
 struct AttnArgs {
     const _Float16* q;
     _Float16* out;

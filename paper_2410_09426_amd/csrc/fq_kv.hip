@@ -23,6 +23,7 @@
 // and leave with 16-byte stores.
 #include "fq_internal.h"
 #include "fq_device.h"
+#include "fq_cache_device.h"
 
 namespace fq {
 
@@ -53,6 +54,13 @@ struct KvDev {
     int64_t T;
     int H, Hp;
     float clip;
+};
+
+// Rows that lie `stride` halves apart, into the pages of a cache.
+struct KvPagedDev : KvDev {
+    CacheDev c;
+    uint32_t* params;
+    int64_t stride;
 };
 
 // The grid of one group from the range of its values (always containing 0), and 8 codes on it.
@@ -97,10 +105,10 @@ struct KvGrid {
 
 // BITS = 2, 3, 4: asymmetric codes of that width + step + zero point per group.  BITS = 0: the transformed rows
 // themselves, rounded to fp16 (p.out_codes then points at an fp16 [T, H, D] tensor): the query side of a transformed
-// key cache.
-template <int BITS>
-__global__ __launch_bounds__(KV_NT) __attribute__((amdgpu_waves_per_eu(2))) void kv_kernel(KvDev p) {
-    constexpr bool QUANT = BITS != 0;
+// key cache.  DEV = KvPagedDev: the codes go to their tokens' places in the pages of a cache.
+template <int BITS, typename DEV>
+__global__ __launch_bounds__(KV_NT) __attribute__((amdgpu_waves_per_eu(2))) void kv_kernel(DEV p) {
+    constexpr bool QUANT = BITS != 0, PAGED = std::is_same_v<DEV, KvPagedDev>;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     u32x4* Pf = reinterpret_cast<u32x4*>(smem);                               // fragment table
     _Float16* Pflat = reinterpret_cast<_Float16*>(smem + KV_FRAG_BYTES);      // prologue only
@@ -125,7 +133,9 @@ __global__ __launch_bounds__(KV_NT) __attribute__((amdgpu_waves_per_eu(2))) void
     };
     auto issue = [&](int64_t blk, u32x4 (&r)[KV_KB]) {
         const int64_t b = blk < nblk ? blk : nblk - 1;
-        const u32x4* row = reinterpret_cast<const u32x4*>(p.kv + first_group(b) * KV_D) + (size_t)group_ofs(b, c) * (KV_D / 8);
+        const u32x4* row;
+        if constexpr (PAGED) row = reinterpret_cast<const u32x4*>(p.kv + (b * KV_TOK + (p.T - 1 - b * KV_TOK < c ? p.T - 1 - b * KV_TOK : c)) * p.stride + head * KV_D);
+        else row = reinterpret_cast<const u32x4*>(p.kv + first_group(b) * KV_D) + (size_t)group_ofs(b, c) * (KV_D / 8);
 #pragma unroll
         for (int kb = 0; kb < KV_KB; ++kb) r[kb] = row[2 * kb + h];   // cached: a 128-byte line is shared by 4 of these loads
     };
@@ -257,18 +267,27 @@ __global__ __launch_bounds__(KV_NT) __attribute__((amdgpu_waves_per_eu(2))) void
         // the last token's row (their lanes re-read its input), so they are stored onto it: same bytes, no branch.
         const int64_t g0 = first_group(blk);
         constexpr int NUNIT = 32 * QB;
+        int64_t place = NO_TOKEN;
+        if constexpr (PAGED) place = token_place(p.c, min((int64_t)blk * KV_TOK + c, p.T - 1), head);
 #pragma unroll
         for (int k = 0; k < (NUNIT + 63) / 64; ++k) {
             const int q = l + 64 * k;
             if (NUNIT % 64 == 0 || q < NUNIT) {
                 const int r = q / QB, ch = q % QB;
                 const u32x4 v = *reinterpret_cast<const u32x4*>(stage + r * KV_STAGE_PITCH + 16 * ch);
+                if constexpr (PAGED) {
+                    const int64_t at = __shfl((long long)place, r);
+                    if (at >= 0) reinterpret_cast<u32x4*>(p.out_codes)[at * QB + ch] = v;
+                    continue;
+                }
                 u32x4* dst = reinterpret_cast<u32x4*>(p.out_codes + g0 * (KV_D * QB / 8)) + (size_t)group_ofs(blk, r) * QB + ch;
                 if constexpr (QB == 3) *dst = v;   // 48-byte rows end inside a 32-byte sector: leave them to L2 to merge with their neighbours
                 else __builtin_nontemporal_store(v, dst);
             }
         }
-        if (h == 0) {   // both half-waves hold the same step and zero point: one of them stores
+        if constexpr (PAGED) {
+            if (h == 0 && place >= 0) p.params[place] = (uint32_t)__builtin_bit_cast(uint16_t, g.step) | (uint32_t)g.z << 16;
+        } else if (h == 0) {   // both half-waves hold the same step and zero point: one of them stores
             const size_t go = group_ofs(blk, c);
             (p.out_scales + g0)[go] = g.step;
             (p.out_zeros + g0)[go] = (_Float16)g.z;
@@ -290,8 +309,9 @@ __global__ __launch_bounds__(KV_NT) __attribute__((amdgpu_waves_per_eu(2))) void
 // stay in registers), and four times as many CUs take part.  The groups' ranges meet in LDS.  Same arithmetic in the same
 // order as above: the same bits.  What bounds it: latency (the launch, P_h and the rows on their way, eight MFMAs in a row, the
 // exchange of the ranges).
-template <int BITS>
-__global__ __launch_bounds__(KV_NT) void kv_few_kernel(KvDev p) {
+template <int BITS, typename DEV>
+__global__ __launch_bounds__(KV_NT) void kv_few_kernel(DEV p) {
+    constexpr bool PAGED = std::is_same_v<DEV, KvPagedDev>;
     constexpr int QB = BITS ? BITS : 4;
     constexpr int PITCH = 32 + 8;                                 // halves per row of a wave's 32 columns of P_h
     __shared__ __attribute__((aligned(16))) _Float16 Pw_all[KV_WAVES * KV_D * PITCH];
@@ -309,9 +329,13 @@ __global__ __launch_bounds__(KV_NT) void kv_few_kernel(KvDev p) {
     const int64_t g0 = (int64_t)blockIdx.x * KV_TOK * p.H + head, left = p.T - 1 - (int64_t)blockIdx.x * KV_TOK;
     const size_t gofs = (size_t)((int64_t)c < left ? c : (int)left) * p.H;
     const u32x4* row = reinterpret_cast<const u32x4*>(p.kv + g0 * KV_D) + gofs * (KV_D / 8);
+    const int64_t token = (int64_t)blockIdx.x * KV_TOK + (c < left ? (int64_t)c : left);
+    if constexpr (PAGED) row = reinterpret_cast<const u32x4*>(p.kv + token * p.stride + head * KV_D);
 #pragma unroll
     for (int kb = 0; kb < KV_KB; ++kb) rows[kb] = row[2 * kb + h];
     __builtin_amdgcn_sched_barrier(0);
+    int64_t place = NO_TOKEN;
+    if constexpr (PAGED) place = token_place(p.c, token, head);
 #pragma unroll
     for (int k = 0; k < 8; ++k) *reinterpret_cast<u32x4*>(Pw + (16 * k + (l >> 2)) * PITCH + 8 * (l & 3)) = v[k];
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -359,7 +383,10 @@ __global__ __launch_bounds__(KV_NT) void kv_few_kernel(KvDev p) {
     // the half-waves exchange so that each lane has two consecutive runs of 8 codes: 2 QB bytes
     const auto sw = __builtin_amdgcn_permlane32_swap(pk[0], pk[1], false, false);
     const uint32_t p0 = sw[0], p1 = sw[1];
-    uint8_t* out = p.out_codes + (g0 + gofs) * (16 * QB) + 4 * QB * w;
+    uint8_t* out = p.out_codes + (PAGED ? place : (int64_t)(g0 + gofs)) * (16 * QB) + 4 * QB * w;
+    if constexpr (PAGED) {
+        if (place < 0) return;                                    // (nothing waits for this lane from here on)
+    }
     if constexpr (QB == 4) {
         *reinterpret_cast<uint2*>(out + 8 * h) = uint2{p0, p1};
     } else if constexpr (QB == 2) {
@@ -369,28 +396,27 @@ __global__ __launch_bounds__(KV_NT) void kv_few_kernel(KvDev p) {
         *reinterpret_cast<uint32_t*>(out + 8 * h) = h ? (lo >> 16) | (hi << 16) : lo;
         *reinterpret_cast<uint16_t*>(out + 4 + 2 * h) = (uint16_t)(h ? lo : hi);
     }
-    if (w == 0 && h == 0) {
+    if constexpr (PAGED) {
+        if (w == 0 && h == 0) p.params[place] = (uint32_t)__builtin_bit_cast(uint16_t, g.step) | (uint32_t)g.z << 16;
+    } else if (w == 0 && h == 0) {
         (p.out_scales + g0)[gofs] = g.step;
         (p.out_zeros + g0)[gofs] = (_Float16)g.z;
     }
 }
 
-template <int BITS>
-static hipError_t kv_launch_mode(const KvArgs& a, hipStream_t stream) {
-    KvDev d;
-    d.kv = a.kv; d.P = a.P; d.out_codes = a.out_codes; d.out_scales = a.out_scales; d.out_zeros = a.out_zeros;
-    d.T = a.T; d.H = a.H; d.Hp = a.Hp; d.clip = a.clip;
+template <int BITS, typename DEV>
+static hipError_t kv_launch_dev(const DEV& a, hipStream_t stream) {
     const int64_t nblk = (a.T + KV_TOK - 1) / KV_TOK;
     // Up to one workgroup per CU the few-group kernel: 64 x 32 groups 4.5 -> 3.4 us at 4 bits, 5.1 -> 3.4 at 3, 4.4 -> 3.1 as fp16 rows
     // (1.6 us of it launch); with 320 of them both take 4.6, with 512 4.9 / 4.7, with 1024 7.3 / 4.9 (every workgroup fetches P_h).
     // FLATQUANT_KV_FEW forces it (1) or the other one (0).
     if (tuned(Knob::KV_FEW, nblk * a.H <= cu_count()) != 0)
-        return launch(kv_few_kernel<BITS>, dim3((unsigned)nblk, (unsigned)a.H), dim3(KV_NT), 0, stream, d);
+        return launch(kv_few_kernel<BITS, DEV>, dim3((unsigned)nblk, (unsigned)a.H), dim3(KV_NT), 0, stream, a);
     constexpr int LDS = BITS ? KV_LDS_BYTES : KV_OUT_LDS_BYTES;
     static OccCache occ_cache;
     int occ = 0;
     {
-        hipError_t e = kernel_occupancy(reinterpret_cast<const void*>(kv_kernel<BITS>), KV_NT, LDS, occ_cache, occ);
+        hipError_t e = kernel_occupancy(reinterpret_cast<const void*>(kv_kernel<BITS, DEV>), KV_NT, LDS, occ_cache, occ);
         if (e != hipSuccess) return e;
     }
     // One workgroup per CU (its LDS holds the fragment table and, while that is built, all of P_h).  With P_h staged in
@@ -404,7 +430,29 @@ static hipError_t kv_launch_mode(const KvArgs& a, hipStream_t stream) {
     if (gx < 1) gx = 1;
     const int64_t rounds = (need + gx - 1) / gx;                         // same number of steps (+-1) for every workgroup
     gx = (need + rounds - 1) / rounds;
-    return launch(kv_kernel<BITS>, dim3((unsigned)gx, (unsigned)a.H), dim3(KV_NT), LDS, stream, d);
+    return launch(kv_kernel<BITS, DEV>, dim3((unsigned)gx, (unsigned)a.H), dim3(KV_NT), LDS, stream, a);
+}
+
+template <int BITS>
+static hipError_t kv_launch_mode(const KvArgs& a, hipStream_t stream) {
+    KvDev d;
+    d.kv = a.kv; d.P = a.P; d.out_codes = a.out_codes; d.out_scales = a.out_scales; d.out_zeros = a.out_zeros;
+    d.T = a.T; d.H = a.H; d.Hp = a.Hp; d.clip = a.clip;
+    return kv_launch_dev<BITS>(d, stream);
+}
+
+// The keys (x = 0) or values (1) of a batch, through r.P[x], into the cache's pages: the bits of kv_launch on the same rows.
+hipError_t kv_paged_launch(const CacheDev& c, const CacheRows& r, int x, hipStream_t stream) {
+    KvPagedDev d;
+    d.kv = static_cast<const _Float16*>(r.rows[x]); d.P = r.P[x]; d.out_codes = c.codes[x]; d.out_scales = d.out_zeros = nullptr;
+    d.T = c.T; d.H = c.H; d.Hp = r.Hp; d.clip = r.clip[x];
+    d.c = c; d.params = c.params[x]; d.stride = r.stride[x];
+    switch (c.bits[x]) {
+        case 2: return kv_launch_dev<2>(d, stream);
+        case 3: return kv_launch_dev<3>(d, stream);
+        case 4: return kv_launch_dev<4>(d, stream);
+        default: return hipErrorInvalidValue;
+    }
 }
 
 hipError_t kv_launch(const KvArgs& a0, hipStream_t stream) {

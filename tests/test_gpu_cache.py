@@ -158,3 +158,61 @@ def test_tree_attention(rows, lengths, H, G, page, bits, launch, tuning):
     q = c.row_tensor(H * G)
     got = run_attention(c, q, G, 0.088, masks=masks)
     check_attention(c, q, G, 0.088, got, masks=masks)
+
+
+@pytest.mark.parametrize("bits", [(4, 4), (3, 2), (2, 3)])
+@pytest.mark.parametrize("rows,lengths,H,Hp,page", [((1, 1, 1), (7, 65, 1), 4, 4, 64), ((40, 0, 33, 1), (50, 3, 33, 200), 3, 1, 16), ((2500, 700), (2500, 900), 5, 5, 32)])
+@pytest.mark.parametrize("few", [0, 1])
+def test_write_through_matrices(rows, lengths, H, Hp, page, bits, few, tuning):
+    """The codes, steps and zero points of flatquant_kv_transform_quant_bits on the same rows, in their tokens' places and nowhere else."""
+    print(f"[case] write {rows} of {lengths} through {Hp} matrices, {H} heads, {bits} bits, few {few}", flush=True)
+    tuning("FLATQUANT_KV_FEW", few)
+    c = Batch(31, rows, lengths, H, page, *bits, pad=2, filled=False, no_page=((0, 0),)).upload()
+    st = torch.cuda.current_stream()
+    P = [_dev((c.r.standard_normal((Hp, D, D)) * 0.1).astype(np.float16)) for _ in "kv"]
+    x = [_dev(c.row_tensor(H, 8 * n)) for n in (1, 0)]
+    before = {n: c.d[n].clone() for n in ("kc", "kp", "vc", "vp")}
+    fq.flatquant_cache_write(c.cache(), c.batch(), x[0], x[0].shape[1], x[1], x[1].shape[1], P[0], None, Hp, 0.95, 0.9, stream=st)
+    torch.cuda.synchronize()
+    half = Batch(31, rows, lengths, H, page, *bits, pad=2, filled=False, no_page=((0, 0),)).upload()      # the values' half without a matrix
+    fq.flatquant_cache_write(half.cache(), half.batch(), None, 0, x[1], x[1].shape[1], None, None, 1, 0.95, 0.9, stream=st)
+    assert torch.equal(half.d["vc"], c.d["vc"]) and torch.equal(half.d["vp"], c.d["vp"])
+    fq.flatquant_cache_write(c.cache(), c.batch(), None, 0, x[1], x[1].shape[1], None, P[1], Hp, 0.95, 0.9, stream=st)
+    for name, m, y, qb, clip in zip("kv", P, x, bits, (0.95, 0.9)):
+        flat = y[:, :H * D].contiguous()
+        codes = torch.empty((c.T, H, 16 * qb), dtype=torch.uint8, device="cuda")
+        steps, zeros = (torch.empty((c.T, H), dtype=torch.float16, device="cuda") for _ in range(2))
+        fq.flatquant_kv_transform_quant_bits(flat, m, Hp, clip, qb, c.T, H, D, codes, steps, zeros, stream=st)
+        torch.cuda.synchronize()
+        word = _host(steps).view(np.uint16).astype(np.uint32) | _host(zeros).astype(np.uint32) << 16
+        want_c, want_p = before[name + "c"].cpu().numpy(), before[name + "p"].cpu().numpy().view(np.uint32)
+        for b in range(c.B):
+            for i in range(rows[b]):
+                at = c.host[0].place(c.table[b, :c.width], lengths[b] - rows[b] + i)
+                if at is not None:
+                    want_c[at[0], :, at[1]] = codes[c.starts[b] + i].cpu().numpy()
+                    want_p[at[0], :, at[1]] = word[c.starts[b] + i]
+        assert np.array_equal(c.d[name + "c"].cpu().numpy(), want_c) and np.array_equal(c.d[name + "p"].cpu().numpy().view(np.uint32), want_p)
+
+
+def test_groups_that_hold_no_numbers_leave_the_others_alone():
+    """Infinities and NaN in a group: its step overflows or ignores them; its neighbours in the row, the wave and the page are as without."""
+    c = Batch(5, (70,), (70,), 3, 16, 4, 3, filled=False).upload()
+    k, v = c.row_tensor(3), c.row_tensor(3)
+    print("[case] write 70 rows, some without numbers", flush=True)
+    _write(c, k, v)
+    _same_pages(c)
+    for t, h, value in ((0, 0, np.inf), (1, 1, -np.inf), (2, 2, np.nan), (66, 0, np.nan)):
+        for x in (k, v):
+            x[t, h * D + 5] = value
+    dk, dv = _dev(k), _dev(v)
+    fq.flatquant_cache_write(c.cache(), c.batch(), dk, 3 * D, dv, 3 * D, None, None, 1, 0.95, 0.9, stream=torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    for name, x in zip("kv", c.host):
+        codes, params = c.d[name + "c"].cpu().numpy(), c.d[name + "p"].cpu().numpy().view(np.uint32)
+        for t, h in ((0, 0), (1, 1), (2, 2), (66, 0)):
+            page, slot = x.place(c.table[0, :c.width], t)
+            if t < 2:                                             # a step that overflows has zero codes
+                assert not codes[page, h, slot].any() and params[page, h, slot] == 0x7C00
+            x.codes[page, h, slot], x.params[page, h, slot] = codes[page, h, slot], params[page, h, slot]
+    _same_pages(c)
