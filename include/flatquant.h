@@ -245,6 +245,8 @@ typedef struct fq_kv_cache {
  *   max_rows, max_length  upper bounds of n_b and lengths[b] as the host knows them: they choose the launch and say how much
  *               work there is; results do not depend on them.
  * The arrays are read on the stream, so one captured graph serves lengths and pages as they change.
+ * Limits (FQ_UNSUPPORTED_SHAPE beyond): T <= 2^29, B * H < 2^24, H <= 65535, table_width * page_tokens <= 2^31 - 2^16, pages < 2^31 and
+ * pages * H * page_tokens <= 2^48; of row tensors strides <= 2^40 and T * stride <= 2^48, of queries T * Hq < 2^31 - 256.
  */
 typedef struct fq_kv_batch {
     const int32_t* row_starts;
@@ -268,8 +270,10 @@ typedef struct fq_kv_batch {
  * formulas, ties included.  With one they are the bits of flatquant_kv_transform_quant_bits on the same rows.
  *   k, v   fp16 [T, H, 128], row t at k + t * k_stride halves; 16-byte aligned, strides multiples of 8 and >= 128 H.  Either may be NULL:
  *          that half of the cache is left as it is.
- *   P_k, P_v  fp16 [Hp, 128, 128] or NULL; Hp == 1 or H, for both.
+ *   P_k, P_v  fp16 [Hp, 128, 128], 16-byte aligned, or NULL; Hp == 1 or H, for both.
  *   k_clip, v_clip > 0.
+ * A group with an infinity gets that for its step, and zero codes; a NaN is not looked at for the range and gets code 0.  (With a matrix they
+ * are in every channel of their group.)  No other group changes.
  * No two of the batch's tokens may share a place in the pages (sequences write into pages of their own).
  */
 fq_status flatquant_cache_write(const fq_kv_cache* cache, const fq_kv_batch* batch, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
@@ -286,7 +290,7 @@ fq_status flatquant_cache_read(const fq_kv_cache* cache, const fq_kv_batch* batc
  *     out[t, h, :] = sum_j w_j v_j,   w = softmax over the visible tokens j of ( scale * q[t, h, :] . k_j ),
  * k_j and v_j the de-quantized rows of key/value head h / (Hq / H).  A row at position p sees token j of its sequence if j <= p and, with a
  * window (window > 0), j > p - window or j < sinks: the last `window` tokens and the first `sinks`.  window == 0 is no window, and sinks
- * is then not looked at.  A row that sees nothing gets zeros.  Pages whose tokens no row sees are not touched.
+ * is then not looked at.  A row that sees nothing gets zeros.  What lies in places that a row does not see, whatever it is, does not change it.
  * Scores, maxima and sums are fp32; the weights (times the value's step) are rounded to fp16 for the matrix instructions.
  *   q, out  fp16 [T, Hq, 128], rows q_stride / out_stride halves apart (multiples of 8, >= 128 Hq), 16-byte aligned, not overlapping.
  *   Hq      a multiple of H.
@@ -392,6 +396,9 @@ int fq_abi_version(void);
  * FLATQUANT_GEMM_ROWS (16 / 32 / 48 / 64 output channels per workgroup), FLATQUANT_GEMM_TOKENS (8 / 16 / 32 / 64 tokens per
  * workgroup), FLATQUANT_GEMM_WAVES (4 / 8 / 16) and FLATQUANT_GEMM_DEPTH (1..8 line slots per wave) of the few-token products,
  * FLATQUANT_GEMM_RING_MAX_T (token count up to which the few-token kernel is used), FLATQUANT_KV_FEW (1 / 0: the KV kernel for few groups, or the one for many),
+ * FLATQUANT_ATT_WAVES (attention over the cache: 4 / 8 / 16 waves per workgroup, a workgroup a tile of rows; 0: few rows' tokens dealt out evenly to a fixed
+ * number of workgroups), FLATQUANT_ATT_WG_PER_CU (that number), FLATQUANT_ATT_CHUNK (least number of tokens that one of them takes of a
+ * sequence; for many rows, tokens per split of a long axis),
  * FLATQUANT_KV_FOLD_HEADS (0: a shared P_h is applied head by head like separate ones).  enable != 0 sets the override to `value`, enable == 0 removes it.  Each override starts from the environment variable of the same name, read once per process.
  * Process-wide; affects launches issued after the call returns.  Unknown names return FQ_INVALID_ARG.
  */

@@ -272,7 +272,7 @@ static fq_status cache_args(const fq_kv_cache* cache, const fq_kv_batch* batch, 
         return FQ_INVALID_ARG;
     const int page = cache->page_tokens;
     if (page < 16 || page > 1024 || (page & (page - 1)) || cache->H > 65535 || cache->pages > 0x7fffffffLL) return FQ_UNSUPPORTED_SHAPE;
-    if (batch->T > (1LL << 29) || batch->B > 0xffffff / cache->H || batch->table_width > 0x7fffffffLL) return FQ_UNSUPPORTED_SHAPE;   // grid and index limits
+    if (batch->T > (1LL << 29) || batch->B > 0xffffff / cache->H || batch->table_width > 0x7fff0000LL / page) return FQ_UNSUPPORTED_SHAPE;   // grid and index limits
     if (cache->pages > (1LL << 48) / cache->H / page) return FQ_UNSUPPORTED_SHAPE;
     if (batch->T == 0 || batch->B == 0) {
         empty = true;
@@ -312,7 +312,7 @@ static fq_status cache_rows(const fq_kv_cache* cache, const fq_kv_batch* batch, 
         if (!x[i]) continue;
         if (stride[i] < row) return FQ_INVALID_ARG;
         if ((reinterpret_cast<uintptr_t>(x[i]) & 15) || (stride[i] & 7)) return FQ_MISALIGNED;
-        if (stride[i] > (1LL << 40)) return FQ_UNSUPPORTED_SHAPE;
+        if (stride[i] > (1LL << 40) || stride[i] > (1LL << 48) / batch->T) return FQ_UNSUPPORTED_SHAPE;
         if (in_cache(cache, batch, x[i], ((batch->T - 1) * stride[i] + row) * 2)) return FQ_INVALID_ARG;
     }
     return FQ_OK;
@@ -331,6 +331,8 @@ fq_status flatquant_cache_write(const fq_kv_cache* cache, const fq_kv_batch* bat
     if (st != FQ_OK) return st;
     if ((reinterpret_cast<uintptr_t>(P_k) & 15) || (reinterpret_cast<uintptr_t>(P_v) & 15)) return FQ_MISALIGNED;
     r.P[0] = static_cast<const _Float16*>(P_k); r.P[1] = static_cast<const _Float16*>(P_v);
+    for (int x = 0; x < 2; ++x)
+        if (r.P[x] && r.rows[x] && in_cache(cache, batch, r.P[x], 32768LL * Hp)) return FQ_INVALID_ARG;
     r.Hp = Hp; r.clip[0] = k_clip; r.clip[1] = v_clip;
     return fq::finish(fq::cache_write_launch(d, r, static_cast<hipStream_t>(stream)));
 }
@@ -359,7 +361,8 @@ static fq_status cache_attention(const fq_kv_cache* cache, const fq_kv_batch* ba
     const int64_t row = 128LL * Hq;
     if (Hq < 1 || Hq % cache->H != 0 || !std::isfinite(scale) || window < 0 || sinks < 0 || q_stride < row || out_stride < row || workspace_bytes < 0)
         return FQ_INVALID_ARG;
-    if (Hq > (1 << 24) || batch->T > 0x7fffff00LL / Hq || q_stride > (1LL << 40) || out_stride > (1LL << 40) || (tree && batch->max_rows > 64)) return FQ_UNSUPPORTED_SHAPE;
+    const int64_t most = batch->T > 256 ? (1LL << 48) / batch->T : 1LL << 40;
+    if (Hq > (1 << 24) || batch->T > 0x7fffff00LL / Hq || q_stride > most || out_stride > most || (tree && batch->max_rows > 64)) return FQ_UNSUPPORTED_SHAPE;
     if (empty) return FQ_OK;
     if (!q || !out || (tree && !visible)) return FQ_INVALID_ARG;
     fq::AttnPlan plan = fq::attention_plan(batch->B, batch->T, cache->H, Hq, batch->max_rows, batch->max_length, batch->max_length);

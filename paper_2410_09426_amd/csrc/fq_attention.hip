@@ -30,7 +30,7 @@ constexpr int ATT_NT = 64 * ATT_WAVES;
 constexpr int ATT_STEP = 32;               // tokens per step of a wave
 constexpr int ATT_PITCH = ATT_D + 4;       // floats per row of partial channels in LDS
 constexpr int kMaxSplits = 128;
-constexpr float ATT_NONE = -1e30f;         // reference of a row that has seen nothing: below every finite score
+constexpr float ATT_NONE = -0x1p125f;        // reference of a row that has seen nothing: below every finite score
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
@@ -275,9 +275,8 @@ struct Span {
 };
 __device__ __forceinline__ Span span_of(const AttnDev& p, int length, int pos_lo, int pos_hi) {
     Span s;
-    const int64_t held = (int64_t)p.c.table_width << p.c.page_shift;
+    const int64_t held = (int64_t)p.c.table_width << p.c.page_shift;           // (2^31 - 2^16 at most: steps behind the end are still ints)
     s.end = held < length ? (int)held : length;
-    s.end = s.end < 0x7FFFFF00 ? s.end : 0x7FFFFF00;                           // a step behind it is still an int
     s.begin = s.first_steps = 0;
     if (!p.visible) {
         s.end = pos_hi < s.end ? pos_hi + 1 : s.end;
@@ -346,26 +345,30 @@ __device__ __forceinline__ float zero_sum(uint32_t pair, uint32_t params, float 
     return sum;
 }
 // Weights 2^(factor score - ref), their products with the values' steps and the weights' sum; true if a lane of the wave needs a higher reference.
-template <int N, typename Scores, typename Factor, typename Step>
+// CAPPED, with a raised reference: of scores beyond 2^24 that reference is off by more than their exponents bear, and the products are held at 2^14.
+template <int N, bool CAPPED, typename Scores, typename Factor, typename Step>
 __device__ __forceinline__ bool weigh(const Scores& score, Factor factor, Step step, float ref, float (&prod)[N], float& sum) {
     float big = 0.0f;
     sum = 0.0f;
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(score[k], factor(k), -ref));
+        float e = __builtin_amdgcn_exp2f(__builtin_fmaf(score[k], factor(k), -ref));
+        if constexpr (CAPPED) e = __builtin_fminf(e, 0x1p14f * __builtin_amdgcn_rcpf(__builtin_fmaxf(step(k), 0x1p-25f)));
         sum += e;
         prod[k] = e * step(k);
         big = __builtin_fmaxf(big, prod[k]);
     }
     return __any(big > 32768.0f || sum > 0x1p40f);
 }
-// Raises the reference so that the row's largest product here is at most 2^7 (a step below 2^-25 counts as that); returns the factor for what has been summed.
+// Raises the reference so that the row's largest product here is at most 2^7 (a step below 2^-25 counts as that), or 2^11 for scores near 2^24: so much lower that
+// the largest weight of all scores, however large, is not lost to the reference's rounding.  Returns the factor for what has been summed.
 template <int N, typename Scores, typename Factor, typename Step, typename Row>
 __device__ __forceinline__ float raise_reference(const Scores& score, Factor factor, Step step, float& ref, Row row_max) {
     float top = ATT_NONE;
 #pragma unroll
     for (int k = 0; k < N; ++k) top = __builtin_fmaxf(top, score[k] * factor(k) + __builtin_fmaxf(__builtin_amdgcn_logf(step(k)), -25.0f));
-    const float to = __builtin_fmaxf(ref, row_max(top) - 7.0f), f = __builtin_amdgcn_exp2f(ref - to);
+    top = __builtin_fminf(row_max(top), 0x1p120f);
+    const float to = __builtin_fmaxf(ref, top - 7.0f - __builtin_fabsf(top) * 0x1p-22f), f = __builtin_amdgcn_exp2f(ref - to);
     ref = to;
     return f;
 }
@@ -538,13 +541,13 @@ __device__ __forceinline__ void few_rows(const AttnDev& p, unsigned char* smem, 
             auto step = [&](int k) { return (float)step_bits(vp[k]); };
 #pragma unroll
             for (int k = 0; k < 8; ++k) s8[k] = sc[n][k >> 2][k & 3];
-            if (weigh<8>(s8, by, step, ref[n], prod, sum)) {
+            if (weigh<8, false>(s8, by, step, ref[n], prod, sum)) {
                 const float f = raise_reference<8>(s8, by, step, ref[n], [](float top) { return across_groups(top, fmax_op); });
                 total[n] *= f;
                 zeros[n] *= f;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) acc[n][j] *= f;
-                weigh<8>(s8, by, step, ref[n], prod, sum);
+                weigh<8, true>(s8, by, step, ref[n], prod, sum);
             }
             total[n] += sum;
             u32x4 pp;
@@ -1102,7 +1105,7 @@ __global__ __launch_bounds__(64 * NW, 2) void shared_attention_kernel(AttnDev p)
             for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
                 for (int k = 0; k < 16; ++k) acc[dt][k] *= f;
-            weigh<16>(sc, by, step, ref, prod, sum);
+            weigh<16, true>(sc, by, step, ref, prod, sum);
         };
         auto values = [&](const unsigned char* base, int t, const half8 (&pw)[2]) {
 #pragma unroll
@@ -1148,7 +1151,7 @@ __global__ __launch_bounds__(64 * NW, 2) void shared_attention_kernel(AttnDev p)
                         factors(base, 32 * t, fk);
                         factors(base, 64 + 32 * t, vs);
                         mask(x + 2 * y, t, pages >> (4 * y), sc, fk, vs);
-                        if (weigh<16>(sc, by, step, ref, prod, sum)) raise(sc, fk, vs, prod, sum);
+                        if (weigh<16, false>(sc, by, step, ref, prod, sum)) raise(sc, fk, vs, prod, sum);
                         total += sum;
                         halves(prod, pw);
                         values(base, t, pw);
