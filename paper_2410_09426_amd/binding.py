@@ -6,7 +6,7 @@ tensors); nothing is computed in Python.  There is no fallback for the
 kernels: if the library is missing, loading raises.
 
 All entry points have the parameters of their C counterparts, plus ``stream=None, check=True`` where they launch.  Those of a model's
-forward pass (``NATIVE``) are functions of the extension module ``_fqcall`` (csrc/fq_python.cpp), which calls the library that
+forward pass (``NATIVE`` and, on the paged key/value cache, ``CACHE_CALLS``) are functions of the extension module ``_fqcall`` (csrc/fq_python.cpp), which calls the library that
 ``lib()`` has loaded.  The module is compiled for one interpreter; under another one, or where it has not been built, the same functions
 call through ctypes like the rest (2.6 us of host time for a product's arguments instead of 0.5).
 """
@@ -112,7 +112,7 @@ def lib() -> ctypes.CDLL:
         L.fq_abi_version.restype = i32
         _lib = L
         if _fqcall:
-            _fqcall.bind({n: ctypes.cast(getattr(L, n), vp).value for n in NATIVE})
+            _fqcall.bind({n: ctypes.cast(getattr(L, n), vp).value for n in NATIVE + CACHE_CALLS})
     return _lib
 
 
@@ -150,13 +150,10 @@ def _ctypes_call(name: str):
 try:
     _fqcall = importlib.import_module(__package__ + "._fqcall")
 except ModuleNotFoundError:                     # not built, or built for another interpreter
-    globals().update((n, _ctypes_call(n)) for n in NATIVE)
+    globals().update((n, _ctypes_call(n)) for n in NATIVE + CACHE_CALLS)
 else:
     _fqcall.connect(lib, FlatQuantError)
-    globals().update((n, getattr(_fqcall, n)) for n in NATIVE)
-
-
-globals().update((n, _ctypes_call(n)) for n in CACHE_CALLS)
+    globals().update((n, getattr(_fqcall, n)) for n in NATIVE + CACHE_CALLS)
 
 
 class _HostStruct:

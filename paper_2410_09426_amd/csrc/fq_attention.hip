@@ -528,7 +528,7 @@ __device__ __forceinline__ void few_rows(const AttnDev& p, unsigned char* smem, 
                     for (int n = 0; n < NT; ++n) {
                         bool ok = sees(sight[n], k);
                         if (p.visible) ok |= sees_drafted(sight[n], before, k);
-                        sc[n][t][r] = ok & held ? sc[n][t][r] : -__builtin_inff();
+                        sc[n][t][r] = (ok & held) ? sc[n][t][r] : -__builtin_inff();
                     }
                 }
             }
@@ -1091,7 +1091,7 @@ __global__ __launch_bounds__(64 * NW, 2) void shared_attention_kernel(AttnDev p)
                 const int kk = k0 + 8 * (k >> 2) + 4 * h + (k & 3);
                 bool ok = sees(sight, kk);
                 if (p.visible) ok |= sees_drafted(sight, before, kk);
-                sc[k] = ok & (kk < end) & (pages_ok >> (k >> 3) & 1) ? sc[k] * fk[k] : -__builtin_inff();
+                sc[k] = (ok & (kk < end) & (pages_ok >> (k >> 3) & 1)) ? sc[k] * fk[k] : -__builtin_inff();
                 fk[k] = 1.0f;
                 vs[k] = finite_step(vs[k]);
             }

@@ -17,7 +17,7 @@
 
 namespace {
 
-enum Entry { TRANSFORM, MX, MX_TILED, WEIGHT, W4A4, MX_GEMM, KV, KV_BITS, HEAD, COUNT };
+enum Entry { TRANSFORM, MX, MX_TILED, WEIGHT, W4A4, MX_GEMM, KV, KV_BITS, HEAD, CACHE_WRITE, CACHE_READ, CACHE_ATTENTION, CACHE_TREE, COUNT };
 void* g_entry[COUNT];                 // addresses in the loaded library; null until then
 PyObject* g_error = nullptr;          // binding.FlatQuantError(status, where)
 PyObject* g_load = nullptr;           // binding.lib: loads the library and binds its addresses, or raises
@@ -205,7 +205,13 @@ Signature kMxGemm{MX_GEMM, "flatquant_mxfp4_gemm", {GEMM()}};
 Signature kKv{KV, "flatquant_kv_transform_quant", {"kv", "P", "Hp", "clip", "T", "H", "D", "out_codes", "out_scales", "out_zeros", "stream", "check"}};
 Signature kKvBits{KV_BITS, "flatquant_kv_transform_quant_bits", {"kv", "P", "Hp", "clip", "bits", "T", "H", "D", "out_codes", "out_scales", "out_zeros", "stream", "check"}};
 Signature kHead{HEAD, "flatquant_head_transform", {"x", "P", "Hp", "T", "H", "D", "out", "stream", "check"}};
-Signature* const kAll[COUNT] = {&kTransform, &kMx, &kMxTiled, &kWeight, &kW4a4, &kMxGemm, &kKv, &kKvBits, &kHead};
+Signature kCacheWrite{CACHE_WRITE, "flatquant_cache_write", {"cache", "batch", "k", "k_stride", "v", "v_stride", "P_k", "P_v", "Hp", "k_clip", "v_clip", "stream", "check"}};
+Signature kCacheRead{CACHE_READ, "flatquant_cache_read", {"cache", "batch", "k", "k_stride", "v", "v_stride", "stream", "check"}};
+Signature kCacheAttention{CACHE_ATTENTION, "flatquant_cache_attention",
+                          {"cache", "batch", "q", "q_stride", "Hq", "scale", "window", "sinks", "out", "out_stride", "workspace", "workspace_bytes", "stream", "check"}};
+Signature kCacheTree{CACHE_TREE, "flatquant_cache_tree_attention",
+                     {"cache", "batch", "q", "q_stride", "Hq", "scale", "visible", "out", "out_stride", "workspace", "workspace_bytes", "stream", "check"}};
+Signature* const kAll[COUNT] = {&kTransform, &kMx, &kMxTiled, &kWeight, &kW4a4, &kMxGemm, &kKv, &kKvBits, &kHead, &kCacheWrite, &kCacheRead, &kCacheAttention, &kCacheTree};
 
 #define ARGS PyObject*, PyObject *const *a, Py_ssize_t n, PyObject *kw
 #define TYPE(entry) decltype(&entry)
@@ -256,6 +262,76 @@ PyObject* py_head(ARGS) {
     Py_END_ALLOW_THREADS
     return finish(kHead, st, v[kHead.n - 1]);
 }
+// the paged key/value cache
+PyObject* py_cache_write(ARGS) {
+    PyObject* v[kMaxArgs];
+    TYPE(flatquant_cache_write) fn;
+    if (!collect(kCacheWrite, a, n, kw, v)) return nullptr;
+    Reader r{v};
+    const void *cache = r.ptr(), *batch = r.ptr(), *k = r.ptr();
+    const int64_t k_stride = r.i64();
+    const void* x = r.ptr();
+    const int64_t v_stride = r.i64();
+    const void *P_k = r.ptr(), *P_v = r.ptr();
+    const int Hp = r.i32();
+    const float k_clip = r.f32(), v_clip = r.f32();
+    void* stream = r.stream();
+    if (!r.ok || !entry(kCacheWrite.entry, fn)) return nullptr;
+    fq_status st;
+    Py_BEGIN_ALLOW_THREADS
+    st = fn((const fq_kv_cache*)cache, (const fq_kv_batch*)batch, k, k_stride, x, v_stride, P_k, P_v, Hp, k_clip, v_clip, stream);
+    Py_END_ALLOW_THREADS
+    return finish(kCacheWrite, st, v[kCacheWrite.n - 1]);
+}
+PyObject* py_cache_read(ARGS) {
+    PyObject* v[kMaxArgs];
+    TYPE(flatquant_cache_read) fn;
+    if (!collect(kCacheRead, a, n, kw, v)) return nullptr;
+    Reader r{v};
+    const void *cache = r.ptr(), *batch = r.ptr();
+    void* k = r.ptr();
+    const int64_t k_stride = r.i64();
+    void* x = r.ptr();
+    const int64_t v_stride = r.i64();
+    void* stream = r.stream();
+    if (!r.ok || !entry(kCacheRead.entry, fn)) return nullptr;
+    fq_status st;
+    Py_BEGIN_ALLOW_THREADS
+    st = fn((const fq_kv_cache*)cache, (const fq_kv_batch*)batch, k, k_stride, x, v_stride, stream);
+    Py_END_ALLOW_THREADS
+    return finish(kCacheRead, st, v[kCacheRead.n - 1]);
+}
+// the window and the first tokens of one are the masks of the other
+template <bool TREE>
+PyObject* cache_attention(const Signature& s, PyObject* const* args, Py_ssize_t nargs, PyObject* kw) {
+    PyObject* v[kMaxArgs];
+    TYPE(flatquant_cache_attention) causal;
+    TYPE(flatquant_cache_tree_attention) tree;
+    if (!collect(s, args, nargs, kw, v)) return nullptr;
+    Reader r{v};
+    const fq_kv_cache* cache = (const fq_kv_cache*)r.ptr();
+    const fq_kv_batch* batch = (const fq_kv_batch*)r.ptr();
+    const void* q = r.ptr();
+    const int64_t q_stride = r.i64();
+    const int Hq = r.i32();
+    const float scale = r.f32();
+    const void* visible = TREE ? r.ptr() : nullptr;
+    const int window = TREE ? 0 : r.i32(), sinks = TREE ? 0 : r.i32();
+    void* out = r.ptr();
+    const int64_t out_stride = r.i64();
+    void* workspace = r.ptr();
+    const int64_t bytes = r.i64();
+    void* stream = r.stream();
+    if (!r.ok || !(TREE ? entry(s.entry, tree) : entry(s.entry, causal))) return nullptr;
+    fq_status st;
+    Py_BEGIN_ALLOW_THREADS
+    st = TREE ? tree(cache, batch, q, q_stride, Hq, scale, (const uint64_t*)visible, out, out_stride, workspace, bytes, stream)
+              : causal(cache, batch, q, q_stride, Hq, scale, window, sinks, out, out_stride, workspace, bytes, stream);
+    Py_END_ALLOW_THREADS
+    return finish(s, st, v[s.n - 1]);
+}
+PyObject* py_cache_attention(ARGS) { return cache_attention<false>(kCacheAttention, a, n, kw); }
+PyObject* py_cache_tree(ARGS) { return cache_attention<true>(kCacheTree, a, n, kw); }
 // connect(load, error): `load` is called when an entry point is needed whose address is not known; `error` is what is raised
 PyObject* py_connect(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (n != 2) {
@@ -267,10 +343,12 @@ PyObject* py_connect(PyObject*, PyObject* const* a, Py_ssize_t n) {
     for (void*& e : g_entry) e = nullptr;
     Py_RETURN_NONE;
 }
-// bind({name: address}): the entry points of the library just loaded
+// bind({name: address}): the entry points of the library just loaded; those of the cache stay as they are if they are not named
 PyObject* py_bind(PyObject*, PyObject* addresses) {
     void* found[COUNT];
     for (Signature* s : kAll) {
+        found[s->entry] = g_entry[s->entry];
+        if (s->entry >= CACHE_WRITE && !PyMapping_HasKeyString(addresses, s->name)) continue;
         PyObject* o = PyMapping_GetItemString(addresses, s->name);
         if (!o) return nullptr;
         found[s->entry] = PyLong_AsVoidPtr(o);
@@ -294,6 +372,10 @@ PyMethodDef kMethods[] = {
     FN("flatquant_kv_transform_quant", py_kv, "(kv, P, Hp, clip, T, H, D, out_codes, out_scales, out_zeros, stream=None, check=True)"),
     FN("flatquant_kv_transform_quant_bits", py_kv_bits, "(kv, P, Hp, clip, bits, T, H, D, out_codes, out_scales, out_zeros, stream=None, check=True)"),
     FN("flatquant_head_transform", py_head, "(x, P, Hp, T, H, D, out, stream=None, check=True)"),
+    FN("flatquant_cache_write", py_cache_write, "(cache, batch, k, k_stride, v, v_stride, P_k, P_v, Hp, k_clip, v_clip, stream=None, check=True)"),
+    FN("flatquant_cache_read", py_cache_read, "(cache, batch, k, k_stride, v, v_stride, stream=None, check=True)"),
+    FN("flatquant_cache_attention", py_cache_attention, "(cache, batch, q, q_stride, Hq, scale, window, sinks, out, out_stride, workspace, workspace_bytes, stream=None, check=True)"),
+    FN("flatquant_cache_tree_attention", py_cache_tree, "(cache, batch, q, q_stride, Hq, scale, visible, out, out_stride, workspace, workspace_bytes, stream=None, check=True)"),
     {"connect", (PyCFunction)(void (*)(void))py_connect, METH_FASTCALL, nullptr},
     {"bind", py_bind, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};

@@ -230,3 +230,28 @@ def test_oracle_bound_rejects_planted_mistakes():
     for x in worse:
         assert (np.abs(x - out) / tol).max() > 1.0
     assert (np.abs(out.astype(np.float16) - out) / tol).max() < 1.0
+
+
+def test_calls_reach_the_c_function_of_their_name():
+    """With a recording function in the place of each C function, native or through ctypes: every argument in its place and its C type."""
+    import importlib
+    calls = importlib.import_module("paper_2410_09426_amd._fqcall")
+    seen, keep = [], []
+    real = {n: ctypes.cast(getattr(fq.lib(), n), ctypes.c_void_p).value for n in fq.NATIVE + fq.CACHE_CALLS}
+    fakes = dict(real)
+    for name in fq.CACHE_CALLS:
+        c = getattr(fq.lib(), name)
+        keep.append(ctypes.CFUNCTYPE(c.restype, *c.argtypes)(lambda *a, name=name: seen.append((name, *a)) or fq.FQ_OK))
+        fakes[name] = ctypes.cast(keep[-1], ctypes.c_void_p).value
+    calls.bind(fakes)
+    try:
+        calls.bind({n: real[n] for n in fq.NATIVE})                       # what is not named stays
+        for name in fq.CACHE_CALLS:
+            types = getattr(fq.lib(), name).argtypes[:-1]                 # without the stream
+            args = [0.25 if t is ctypes.c_float else 2 ** 40 + k if t is ctypes.c_int64 else 100 + k if t is ctypes.c_int else 2 ** 45 + k for k, t in enumerate(types)]
+            assert getattr(fq, name)(*args, 2 ** 44) == fq.FQ_OK
+            assert seen.pop() == (name, *args, 2 ** 44) and not seen
+    finally:
+        calls.bind(real)
+    for name in fq.CACHE_CALLS:                                           # the signature of the one is that of the other
+        assert str(inspect.signature(getattr(fq, name))) == str(inspect.signature(fq._ctypes_call(name)))
