@@ -925,8 +925,10 @@ __global__ __launch_bounds__(64 * NW, 2) void shared_attention_kernel(AttnDev p)
         const int x_begin = (int)blockIdx.z * per;
         const int x_end = (int)blockIdx.z == p.splits - 1 ? span.steps : min(span.steps, x_begin + per);
 
-        // this wave's rows
-        const int wrow0 = row0 + SH_ROWS * w, wrow_end = wrow0 + SH_ROWS < row_end ? wrow0 + SH_ROWS : row_end;
+        // this wave's rows; of 64 or fewer, waves 2 and 3 have those of waves 0 and 1, and each the tokens of its half of a step
+        const bool halved = NW == 4 && row_end - row0 <= 2 * SH_ROWS;
+        const int my_half = w >> 1;
+        const int wrow0 = row0 + SH_ROWS * (halved ? w & 1 : w), wrow_end = wrow0 + SH_ROWS < row_end ? wrow0 + SH_ROWS : row_end;
         const bool busy = wrow0 < wrow_end;
         const int pos_lo = before + wrow0 / p.G, pos_hi = before + (wrow_end - 1) / p.G;
         int r = wrow0 + c;
@@ -1142,6 +1144,7 @@ __global__ __launch_bounds__(64 * NW, 2) void shared_attention_kernel(AttnDev p)
                     if (!busy || x + 2 * y >= x_end || !(p.visible || span.token(x + 2 * y) <= pos_hi)) continue;
 #pragma unroll
                     for (int t = 0; t < 2; ++t) {
+                        if (halved && t != my_half) continue;
                         f32x16 sc;
                         float fk[16], vs[16], prod[16], sum;
                         half8 pw[2];
@@ -1167,7 +1170,32 @@ __global__ __launch_bounds__(64 * NW, 2) void shared_attention_kernel(AttnDev p)
             }
         }
         total += __shfl_xor(total, 32);
-        if (wrow0 + c < wrow_end) {
+        if (halved) {                                                          // waves 2 and 3 hand theirs over, through what the loop is done with
+            f32x4* sums = reinterpret_cast<f32x4*>(sh_smem) + (w & 1) * (16 * 64);
+            float2* stats = reinterpret_cast<float2*>(sh_smem + 2 * 16 * 64 * 16) + (w & 1) * 64;
+            if (my_half == 1) {
+#pragma unroll
+                for (int k = 0; k < 16; ++k) {
+                    const f32x16& from = acc[k >> 2];
+                    sums[64 * k + l] = f32x4{from[4 * (k & 3)], from[4 * (k & 3) + 1], from[4 * (k & 3) + 2], from[4 * (k & 3) + 3]};
+                }
+                stats[l] = float2{ref, total};
+            }
+            __syncthreads();
+            if (my_half == 0) {
+                const float2 other = stats[l];
+                const float top = __builtin_fmaxf(ref, other.x), f = __builtin_amdgcn_exp2f(ref - top), g = __builtin_amdgcn_exp2f(other.x - top);
+                ref = top;
+                total = total * f + other.y * g;
+#pragma unroll
+                for (int k = 0; k < 16; ++k) {
+                    const f32x4 o = sums[64 * k + l];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[k >> 2][4 * (k & 3) + e] = acc[k >> 2][4 * (k & 3) + e] * f + o[e] * g;
+                }
+            }
+        }
+        if (wrow0 + c < wrow_end && !(halved && my_half == 1)) {
             const int64_t row_token = seq.first + token;
             const int hq = head * p.G + sub;
             if (used == 1) {
