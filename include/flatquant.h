@@ -243,7 +243,7 @@ typedef struct fq_kv_cache {
  *               not visible to attention.  Pages that two sequences share are only read.
  *   T           rows of the row tensors; row_starts is taken as if cut to 0 .. T.
  *   max_rows, max_length  upper bounds of n_b and lengths[b] as the host knows them: they choose the launch and say how much
- *               work there is; results do not depend on them.
+ *               work there is.  Wrong ones cost time; results differ by rounding alone.
  * The arrays are read on the stream, so one captured graph serves lengths and pages as they change.
  * Limits (FQ_UNSUPPORTED_SHAPE beyond): T <= 2^29, B * H < 2^24, H <= 65535, table_width * page_tokens <= 2^31 - 2^16, pages < 2^31 and
  * pages * H * page_tokens <= 2^48; of row tensors strides <= 2^40 and T * stride <= 2^48, of queries T * Hq < 2^31 - 256.
@@ -281,7 +281,7 @@ fq_status flatquant_cache_write(const fq_kv_cache* cache, const fq_kv_batch* bat
 
 /*
  * Reads the batch's rows (the last n_b tokens of every sequence) back: k[t, h, d] = fp16( step * (code - zero point) ), v the same.
- * Row tensors as above, either NULL.  The tokens' pages are only read.
+ * Row tensors as above, either NULL; the two may not share memory, nor may rows of one lie between rows of the other.  The tokens' pages are only read.
  */
 fq_status flatquant_cache_read(const fq_kv_cache* cache, const fq_kv_batch* batch, void* k, int64_t k_stride, void* v, int64_t v_stride, void* stream);
 
