@@ -917,7 +917,6 @@ __global__ __launch_bounds__(64 * NW, 2) void shared_attention_kernel(AttnDev p)
     constexpr int TILE = SH_ROWS * NW;
     const int part = w / 4, role = w % 4;
     const int tiles = (all_rows + TILE - 1) / TILE;
-    const list_t table = (list_t)p.c.page_table + b * p.c.table_stride;
     for (int tile_no = blockIdx.y; tile_no < tiles; tile_no += gridDim.y) {
         const int row0 = (tiles - 1 - tile_no) * TILE;
         const int row_end = row0 + TILE < all_rows ? row0 + TILE : all_rows;
@@ -966,25 +965,19 @@ __global__ __launch_bounds__(64 * NW, 2) void shared_attention_kernel(AttnDev p)
         float ref = ATT_NONE, total = 0.0f;
 
         // codes of steps x and x + 1 of the span, 32 tokens each, which need not follow each other
-        auto pages_of = [&](int x, int (&pg)[NW]) {
-#pragma unroll
-            for (int k = 0; k < NW; ++k) {
-                const unsigned j = (unsigned)(span.token(x + (k >> 1)) + 16 * (k & 1)) >> p.c.page_shift;
-                pg[k] = table[j < (unsigned)p.c.table_width ? j : p.c.table_width - 1];    // (behind the width: behind the end)
-            }
+        // The page of tokens 16 n .. of the step from x on, by every lane n of NW: looked up in all lanes at once (a scalar look-up each took more time than the
+        // conversion), a step before the loads that follow it, in whose queue it stands.
+        auto page_of = [&](int x) {
+            const int n = l % NW, y = x + (n >> 1);
+            const unsigned token = (unsigned)((y < span.first_steps ? ATT_STEP * y : span.begin + ATT_STEP * (y - span.first_steps)) + 16 * (n & 1));
+            const unsigned j = token >> p.c.page_shift, last = (unsigned)p.c.table_width - 1u;
+            return p.c.page_table[b * p.c.table_stride + (j < last ? j : last)];           // (behind the width: behind the end)
         };
-        auto load = [&](int x, const int (&table_pages)[NW], ShareCodes& s) {
-            s.pages = 0;
-#pragma unroll
-            for (int k = 0; k < NW; ++k) s.pages |= (int)((unsigned)table_pages[k] < (unsigned)p.c.pages) << k;
-            int pg[2];
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {                                      // of this wave's 32 tokens
-                pg[k] = table_pages[k];
-#pragma unroll
-                for (int other = 1; other < NW / 2; ++other) pg[k] = w % 2 + 2 * part == other ? table_pages[2 * other + k] : pg[k];
-                pg[k] = (unsigned)pg[k] < (unsigned)p.c.pages ? pg[k] : 0;
-            }
+        auto load = [&](int x, int page, ShareCodes& s) {
+            const bool ok = (unsigned)page < (unsigned)p.c.pages;
+            s.pages = (int)__ballot(ok) & ((1 << NW) - 1);
+            const int held = ok ? page : 0, mine = 2 * (2 * part + w % 2);
+            const int pg[2] = {__builtin_amdgcn_readlane(held, mine), __builtin_amdgcn_readlane(held, mine + 1)};      // of this wave's 32 tokens
             const int k0 = span.token(x + 2 * part + w % 2);
             const int mask = (1 << p.c.page_shift) - 1;
             if (role < 2) {                                                    // token c of the half, quarters 2 h and 2 h + 1
@@ -1129,15 +1122,13 @@ __global__ __launch_bounds__(64 * NW, 2) void shared_attention_kernel(AttnDev p)
 
         if (x_begin < x_end) {
             ShareCodes s;
-            int next[NW];
             constexpr int STEPS = 2 * PARTS;
-            pages_of(x_begin, next);
-            load(x_begin, next, s);
-            pages_of(x_begin + STEPS, next);
+            int next = page_of(x_begin + STEPS);
+            load(x_begin, page_of(x_begin), s);
             convert(s, 0);
             int pages = s.pages;
             load(x_begin + STEPS, next, s);
-            pages_of(x_begin + 2 * STEPS, next);
+            next = page_of(x_begin + 2 * STEPS);
             __syncthreads();
             int buf = 0;
             for (int x = x_begin; x < x_end; x += STEPS) {
@@ -1167,7 +1158,7 @@ __global__ __launch_bounds__(64 * NW, 2) void shared_attention_kernel(AttnDev p)
                 convert(s, buf ^ 1);
                 const int next_pages = s.pages;
                 load(x + 2 * STEPS, next, s);
-                pages_of(x + 3 * STEPS, next);
+                next = page_of(x + 3 * STEPS);
                 pages = next_pages;
                 __syncthreads();
                 buf ^= 1;
