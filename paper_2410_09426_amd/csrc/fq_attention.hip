@@ -69,15 +69,41 @@ __device__ __forceinline__ void each(F&& f) {                                  /
 // a factor of 20): S is 2 at least.
 // RAISED: with 1024 in the exponent, 1024 + 2^S code.
 constexpr uint32_t kRaise = 0x64006400u;
-template <int QB, int S, bool RAISED>
-__device__ __forceinline__ uint32_t field(uint32_t x) {
+template <int QB, int S>
+constexpr uint32_t field_mask() {
     static_assert(S >= 2 && S + QB <= 10, "mantissa bits");
-    constexpr uint32_t mask = (((1u << QB) - 1u) << S) * 0x00010001u;
-    if constexpr (!RAISED) return x & mask;
-    uint32_t r;                                                                // (one instruction: of two constants the compiler makes two)
-    asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(r) : "v"(x), "s"(mask), "v"(kRaise));
-    return r;
+    return (((1u << QB) - 1u) << S) * 0x00010001u;
 }
+// The masks of raised fields, by S, in scalar registers that are written here: the compiler would keep them across a loop, out of registers, and fetch them back
+// with more instructions.
+template <int QB>
+struct Masks {
+    uint32_t m[9];
+    __device__ __forceinline__ Masks() {
+        asm volatile("s_mov_b32 %0, %1" : "=s"(m[0]) : "i"(0x000F000Fu));      // of zero points
+        fill<2>();
+    }
+    template <int S>
+    __device__ __forceinline__ void fill() {
+        constexpr bool used = QB == 4 ? S == 2 || S == 6 : QB == 3 ? S >= 4 && S <= 7 : S == 4 || S == 6 || S == 8;
+        if constexpr (used) asm volatile("s_mov_b32 %0, %1" : "=s"(m[S]) : "i"(field_mask<QB, S>()));
+        if constexpr (S < 8) fill<S + 1>();
+    }
+};
+struct NoMasks {};
+template <int QB, int S, typename M>
+__device__ __forceinline__ uint32_t field(uint32_t x, const M& masks) {
+    if constexpr (std::is_same_v<M, NoMasks>) {
+        return x & field_mask<QB, S>();
+    } else {
+        uint32_t r;                                                            // (one instruction: of two constants the compiler makes two)
+        asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(r) : "v"(x), "s"(masks.m[S]), "v"(kRaise));
+        return r;
+    }
+}
+__device__ __forceinline__ constexpr uint32_t raise_of(const NoMasks&) { return 0u; }
+template <int QB>
+__device__ __forceinline__ constexpr uint32_t raise_of(const Masks<QB>&) { return kRaise; }
 // code - zero point of a raised field; `z`: 1024 + the zero points, in fp16.  One packed fma takes 1024 and the zero point off, exactly.
 template <int S>
 __device__ __forceinline__ half2v code_value(uint32_t f, half2v z) {
@@ -85,8 +111,11 @@ __device__ __forceinline__ half2v code_value(uint32_t f, half2v z) {
     constexpr _Float16 down = (_Float16)(1.0f / (float)(1 << S)), off = (_Float16)(1024.0f - 1024.0f / (float)(1 << S));
     return __builtin_elementwise_fma(raised, half2v{down, down}, half2v{off, off} - z);
 }
-__device__ __forceinline__ half2v raised_zeros(uint32_t low, uint32_t high) {  // of two tokens' parameters
-    return as_half2((__builtin_amdgcn_perm(high, low, 0x07060302u) & 0x000F000Fu) | 0x64006400u);
+template <int QB>
+__device__ __forceinline__ half2v raised_zeros(const Masks<QB>& masks, uint32_t low, uint32_t high) {  // of two tokens' parameters
+    uint32_t r;
+    asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(r) : "v"(__builtin_amdgcn_perm(high, low, 0x07060302u)), "s"(masks.m[0]), "v"(kRaise));
+    return as_half2(r);
 }
 
 // The 32 codes of a lane's quarter of a key, as 16 pairs of fields; pair p is (first(p), second(p)) of the 32, at bit shift(p).
@@ -98,14 +127,14 @@ struct KeyCodes<4> {
     static constexpr int first(int p) { return 8 * (p >> 2) + (p & 3); }
     static constexpr int second(int p) { return first(p) + 4; }
     static constexpr int shift(int p) { return p & 1 ? 6 : 2; }
-    template <bool RAISED>
-    static __device__ __forceinline__ void fields(const words& w, uint32_t (&o)[16]) {
+    template <typename M>
+    static __device__ __forceinline__ void fields(const words& w, uint32_t (&o)[16], const M& masks) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            o[4 * k] = field<4, 2, RAISED>(w[k] << 2);
-            o[4 * k + 1] = field<4, 6, RAISED>(w[k] << 2);
-            o[4 * k + 2] = field<4, 2, RAISED>(w[k] >> 6);
-            o[4 * k + 3] = field<4, 6, RAISED>(w[k] >> 6);
+            o[4 * k] = field<4, 2>(w[k] << 2, masks);
+            o[4 * k + 1] = field<4, 6>(w[k] << 2, masks);
+            o[4 * k + 2] = field<4, 2>(w[k] >> 6, masks);
+            o[4 * k + 3] = field<4, 6>(w[k] >> 6, masks);
         }
     }
 };
@@ -116,18 +145,18 @@ struct KeyCodes<2> {
     static constexpr int first(int p) { return 16 * (p >> 3) + (p & 7); }
     static constexpr int second(int p) { return first(p) + 8; }
     static constexpr int shift(int p) { return shift2(p & 7); }
-    template <bool RAISED>
-    static __device__ __forceinline__ void fields(const words& w, uint32_t (&o)[16]) {
+    template <typename M>
+    static __device__ __forceinline__ void fields(const words& w, uint32_t (&o)[16], const M& masks) {
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-            o[8 * k] = field<2, 4, RAISED>(w[k] << 4);
-            o[8 * k + 1] = field<2, 6, RAISED>(w[k] << 4);
-            o[8 * k + 2] = field<2, 8, RAISED>(w[k] << 4);
-            o[8 * k + 3] = field<2, 6, RAISED>(w[k]);
-            o[8 * k + 4] = field<2, 8, RAISED>(w[k]);
-            o[8 * k + 5] = field<2, 4, RAISED>(w[k] >> 6);
-            o[8 * k + 6] = field<2, 6, RAISED>(w[k] >> 6);
-            o[8 * k + 7] = field<2, 8, RAISED>(w[k] >> 6);
+            o[8 * k] = field<2, 4>(w[k] << 4, masks);
+            o[8 * k + 1] = field<2, 6>(w[k] << 4, masks);
+            o[8 * k + 2] = field<2, 8>(w[k] << 4, masks);
+            o[8 * k + 3] = field<2, 6>(w[k], masks);
+            o[8 * k + 4] = field<2, 8>(w[k], masks);
+            o[8 * k + 5] = field<2, 4>(w[k] >> 6, masks);
+            o[8 * k + 6] = field<2, 6>(w[k] >> 6, masks);
+            o[8 * k + 7] = field<2, 8>(w[k] >> 6, masks);
         }
     }
 };
@@ -141,27 +170,27 @@ struct KeyCodes<3> {
         constexpr int at[16] = {4, 7, 6, 4, 7, 6, 5, 5, 4, 7, 6, 5, 4, 7, 4, 7};
         return at[p];
     }
-    template <bool RAISED>
-    static __device__ __forceinline__ void fields(const words& w, uint32_t (&o)[16]) {
+    template <typename M>
+    static __device__ __forceinline__ void fields(const words& w, uint32_t (&o)[16], const M& masks) {
         // bits 0 .. 47 in the low halves, 48 .. 95 in the high ones
         const uint32_t x0 = __builtin_amdgcn_perm(w[1], w[0], 0x07060100u), x1 = __builtin_amdgcn_perm(w[2], w[0], 0x05040302u),
                        x2 = __builtin_amdgcn_perm(w[2], w[1], 0x07060100u);
-        o[0] = field<3, 4, RAISED>(x0 << 4);
-        o[1] = field<3, 7, RAISED>(x0 << 4);
-        o[2] = field<3, 6, RAISED>(x0);
-        o[3] = field<3, 4, RAISED>(x0 >> 5);
-        o[4] = field<3, 7, RAISED>(x0 >> 5);
-        o[5] = (x0 >> 9 & 0x00400040u) | (x1 << 7 & 0x01800180u) | (RAISED ? kRaise : 0u);
-        o[6] = field<3, 5, RAISED>(x1 << 3);
-        o[7] = field<3, 5, RAISED>(x1);
-        o[8] = field<3, 4, RAISED>(x1 >> 4);
-        o[9] = field<3, 7, RAISED>(x1 >> 4);
-        o[10] = (x1 >> 8 & 0x00C000C0u) | (x2 << 8 & 0x01000100u) | (RAISED ? kRaise : 0u);
-        o[11] = field<3, 5, RAISED>(x2 << 4);
-        o[12] = field<3, 4, RAISED>(x2);
-        o[13] = field<3, 7, RAISED>(x2);
-        o[14] = field<3, 4, RAISED>(x2 >> 6);
-        o[15] = field<3, 7, RAISED>(x2 >> 6);
+        o[0] = field<3, 4>(x0 << 4, masks);
+        o[1] = field<3, 7>(x0 << 4, masks);
+        o[2] = field<3, 6>(x0, masks);
+        o[3] = field<3, 4>(x0 >> 5, masks);
+        o[4] = field<3, 7>(x0 >> 5, masks);
+        o[5] = (x0 >> 9 & 0x00400040u) | (x1 << 7 & 0x01800180u) | raise_of(masks);
+        o[6] = field<3, 5>(x1 << 3, masks);
+        o[7] = field<3, 5>(x1, masks);
+        o[8] = field<3, 4>(x1 >> 4, masks);
+        o[9] = field<3, 7>(x1 >> 4, masks);
+        o[10] = (x1 >> 8 & 0x00C000C0u) | (x2 << 8 & 0x01000100u) | raise_of(masks);
+        o[11] = field<3, 5>(x2 << 4, masks);
+        o[12] = field<3, 4>(x2, masks);
+        o[13] = field<3, 7>(x2, masks);
+        o[14] = field<3, 4>(x2 >> 6, masks);
+        o[15] = field<3, 7>(x2 >> 6, masks);
     }
 };
 
@@ -172,36 +201,36 @@ struct ValueCodes {
         constexpr int at[8] = {4, 7, 6, 4, 7, 6, 5, 5};
         return QB == 4 ? (c & 1 ? 6 : 2) : QB == 2 ? shift2(c) : at[c];
     }
-    template <int HALF, bool RAISED>
-    static __device__ __forceinline__ void fields(uint32_t a, uint32_t b, uint32_t (&o)[4]) {
+    template <int HALF, typename M>
+    static __device__ __forceinline__ void fields(uint32_t a, uint32_t b, uint32_t (&o)[4], const M& masks) {
         const uint32_t x = __builtin_amdgcn_perm(b, a, 0x05040100u);
         if constexpr (QB == 4) {
             const uint32_t y = HALF ? __builtin_amdgcn_perm(b, a, 0x07060302u) : x;
-            o[0] = field<4, 2, RAISED>(y << 2);
-            o[1] = field<4, 6, RAISED>(y << 2);
-            o[2] = field<4, 2, RAISED>(y >> 6);
-            o[3] = field<4, 6, RAISED>(y >> 6);
+            o[0] = field<4, 2>(y << 2, masks);
+            o[1] = field<4, 6>(y << 2, masks);
+            o[2] = field<4, 2>(y >> 6, masks);
+            o[3] = field<4, 6>(y >> 6, masks);
         } else if constexpr (QB == 2 && HALF == 0) {
-            o[0] = field<2, 4, RAISED>(x << 4);
-            o[1] = field<2, 6, RAISED>(x << 4);
-            o[2] = field<2, 8, RAISED>(x << 4);
-            o[3] = field<2, 6, RAISED>(x);
+            o[0] = field<2, 4>(x << 4, masks);
+            o[1] = field<2, 6>(x << 4, masks);
+            o[2] = field<2, 8>(x << 4, masks);
+            o[3] = field<2, 6>(x, masks);
         } else if constexpr (QB == 2) {
-            o[0] = field<2, 8, RAISED>(x);
-            o[1] = field<2, 4, RAISED>(x >> 6);
-            o[2] = field<2, 6, RAISED>(x >> 6);
-            o[3] = field<2, 8, RAISED>(x >> 6);
+            o[0] = field<2, 8>(x, masks);
+            o[1] = field<2, 4>(x >> 6, masks);
+            o[2] = field<2, 6>(x >> 6, masks);
+            o[3] = field<2, 8>(x >> 6, masks);
         } else if constexpr (HALF == 0) {
-            o[0] = field<3, 4, RAISED>(x << 4);
-            o[1] = field<3, 7, RAISED>(x << 4);
-            o[2] = field<3, 6, RAISED>(x);
-            o[3] = field<3, 4, RAISED>(x >> 5);
+            o[0] = field<3, 4>(x << 4, masks);
+            o[1] = field<3, 7>(x << 4, masks);
+            o[2] = field<3, 6>(x, masks);
+            o[3] = field<3, 4>(x >> 5, masks);
         } else {
             const uint32_t y = __builtin_amdgcn_perm(b, a, 0x07060302u);
-            o[0] = field<3, 7, RAISED>(x >> 5);
-            o[1] = (x >> 9 & 0x00400040u) | (y << 7 & 0x01800180u) | (RAISED ? kRaise : 0u);
-            o[2] = field<3, 5, RAISED>(y << 3);
-            o[3] = field<3, 5, RAISED>(y);
+            o[0] = field<3, 7>(x >> 5, masks);
+            o[1] = (x >> 9 & 0x00400040u) | (y << 7 & 0x01800180u) | raise_of(masks);
+            o[2] = field<3, 5>(y << 3, masks);
+            o[3] = field<3, 5>(y, masks);
         }
     }
 };
@@ -492,7 +521,7 @@ __device__ __forceinline__ void few_rows(const AttnDev& p, unsigned char* smem, 
         for (int t = 0; t < 2; ++t) {
             __builtin_amdgcn_sched_barrier(0);
             uint32_t kk[16];
-            KeyCodes<KB>::template fields<false>(ring_key<KB>(slot + t * R::K_PIECE, i, g), kk);
+            KeyCodes<KB>::fields(ring_key<KB>(slot + t * R::K_PIECE, i, g), kk, NoMasks{});
 #pragma unroll
             for (int n = 0; n < NT; ++n) sc[n][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
@@ -570,7 +599,7 @@ __device__ __forceinline__ void few_rows(const AttnDev& p, unsigned char* smem, 
             constexpr int HALF = decltype(part)::value;
             uint32_t vv[4][4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) ValueCodes<VB>::template fields<HALF, false>(vc[2 * k], vc[2 * k + 1], vv[k]);
+            for (int k = 0; k < 4; ++k) ValueCodes<VB>::template fields<HALF>(vc[2 * k], vc[2 * k + 1], vv[k], NoMasks{});
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const u32x4 a = {vv[0][j], vv[1][j], vv[2][j], vv[3][j]};
@@ -1007,7 +1036,8 @@ __global__ __launch_bounds__(64 * NW, 2) void shared_attention_kernel(AttnDev p)
             unsigned char* base = sh_smem + (PARTS * buf + part) * SH_BUFFER;
             float* steps = reinterpret_cast<float*>(base + SH_K_BYTES + SH_V_BYTES);
             if (role < 2) {
-                const half2v z = raised_zeros(s.params[0], s.params[0]);
+                const Masks<KB> masks;
+                const half2v z = raised_zeros(masks, s.params[0], s.params[0]);
                 const int tok = 32 * role + c;
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
@@ -1015,7 +1045,7 @@ __global__ __launch_bounds__(64 * NW, 2) void shared_attention_kernel(AttnDev p)
 #pragma unroll
                     for (int k = 0; k < KB; ++k) cw[k] = s.w[KB * half + k];
                     uint32_t kk[16];
-                    KeyCodes<KB>::template fields<true>(cw, kk);
+                    KeyCodes<KB>::fields(cw, kk, masks);
                     each<4>([&](auto mm) {
                         constexpr int m = decltype(mm)::value;
                         const int chunk = 4 * (2 * h + half) + m;
@@ -1030,15 +1060,16 @@ __global__ __launch_bounds__(64 * NW, 2) void shared_attention_kernel(AttnDev p)
                 if (h == 0) steps[tok] = step_of(s.params[0]) * p.scale2;
             } else {
                 const int i = l & 15, g = l >> 4, chunk = 4 * (role - 2) + g;
+                const Masks<VB> masks;
                 auto values = [&](auto part) {
                     constexpr int HALF = decltype(part)::value;
                     uint32_t vv[4][4];
                     half2v z[4];
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
-                        z[k] = raised_zeros(s.params[2 * k], s.params[2 * k + 1]);
+                        z[k] = raised_zeros(masks, s.params[2 * k], s.params[2 * k + 1]);
                         const int down = VB == 3 && i == 15 ? 8 : 0;
-                        ValueCodes<VB>::template fields<HALF, true>(s.w[2 * k] >> down, s.w[2 * k + 1] >> down, vv[k]);
+                        ValueCodes<VB>::template fields<HALF>(s.w[2 * k] >> down, s.w[2 * k + 1] >> down, vv[k], masks);
                     }
                     each<4>([&](auto jj) {
                         constexpr int j = decltype(jj)::value;
@@ -1051,11 +1082,10 @@ __global__ __launch_bounds__(64 * NW, 2) void shared_attention_kernel(AttnDev p)
                 };
                 values(std::integral_constant<int, 0>{});
                 values(std::integral_constant<int, 1>{});
-                if (i < 8) {
-                    float st = 0.0f;
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) st = i == k ? step_of(s.params[k]) : st;
-                    steps[64 + 32 * (role - 2) + 16 * (g >> 1) + 4 * (g & 1) + (i & 3) + 8 * (i >> 2)] = st;
+                if (i == 0) {
+                    f32x4* at = reinterpret_cast<f32x4*>(steps + 64 + 32 * (role - 2) + 16 * (g >> 1) + 4 * (g & 1));
+                    at[0] = f32x4{step_of(s.params[0]), step_of(s.params[1]), step_of(s.params[2]), step_of(s.params[3])};
+                    at[2] = f32x4{step_of(s.params[4]), step_of(s.params[5]), step_of(s.params[6]), step_of(s.params[7])};
                 }
             }
         };
