@@ -928,9 +928,20 @@ constexpr int SH_K_PITCH = 2 * ATT_D + 16, SH_V_PITCH = 2 * 64 + 16;
 constexpr int SH_K_BYTES = 64 * SH_K_PITCH, SH_V_BYTES = ATT_D * SH_V_PITCH, SH_STEP_BYTES = 2 * 64 * 4;
 constexpr int SH_BUFFER = SH_K_BYTES + SH_V_BYTES + SH_STEP_BYTES;
 
+// x, as far as the compiler can tell another one every time: what follows from it is worked out where it is used and not kept in registers over the loop, of
+// which a wave has all (a spilled one waits for every load on its way).
+__device__ __forceinline__ int again(int x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
 // A thread's share of 64 tokens: two quarters of a key, or eight channels of eight values, and which of the four pages of 16 tokens are pages.
+// (Vectors that both kinds of waves assign as a whole, behind their branch: of arrays that each branch stores into, two words stay in memory, and every step then
+// waits for its loads at once.)
 struct ShareCodes {
-    uint32_t w[8], params[8];
+    u32x4 words[2], parameters[2];
+    __device__ __forceinline__ uint32_t w(int k) const { return words[k >> 2][k & 3]; }
+    __device__ __forceinline__ uint32_t params(int k) const { return parameters[k >> 2][k & 3]; }
     int pages;                             // (uniform) bit k: tokens 16 k .. of the 64
 };
 
@@ -966,7 +977,6 @@ __global__ __launch_bounds__(64 * NW, 2) void shared_attention_kernel(AttnDev p)
         int r = wrow0 + c;
         r = r < row_end ? r : row_end - 1;
         const int token = r / p.G, sub = r - token * p.G;
-        const Sight sight = sight_of(p, before, token, seq.first + token);
         half8 q[8];                                                            // fragment k: chunk 2 k + h of the key rows
         {
             const _Float16* src = p.q + (seq.first + token) * p.q_stride + (head * p.G + sub) * ATT_D;
@@ -997,7 +1007,7 @@ __global__ __launch_bounds__(64 * NW, 2) void shared_attention_kernel(AttnDev p)
         // The page of tokens 16 n .. of the step from x on, by every lane n of NW: looked up in all lanes at once (a scalar look-up each took more time than the
         // conversion), a step before the loads that follow it, in whose queue it stands.
         auto page_of = [&](int x) {
-            const int n = l % NW, y = x + (n >> 1);
+            const int n = again(l) % NW, y = x + (n >> 1);
             const unsigned token = (unsigned)((y < span.first_steps ? ATT_STEP * y : span.begin + ATT_STEP * (y - span.first_steps)) + 16 * (n & 1));
             const unsigned j = token >> p.c.page_shift, last = (unsigned)p.c.table_width - 1u;
             return p.c.page_table[b * p.c.table_stride + (j < last ? j : last)];           // (behind the width: behind the end)
@@ -1009,27 +1019,41 @@ __global__ __launch_bounds__(64 * NW, 2) void shared_attention_kernel(AttnDev p)
             const int pg[2] = {__builtin_amdgcn_readlane(held, mine), __builtin_amdgcn_readlane(held, mine + 1)};      // of this wave's 32 tokens
             const int k0 = span.token(x + 2 * part + w % 2);
             const int mask = (1 << p.c.page_shift) - 1;
+            const int lane = again(l);
+            u32x4 words[2] = {}, parameters[2] = {};
             if (role < 2) {                                                    // token c of the half, quarters 2 h and 2 h + 1
+                const int c = lane & 31, h = lane >> 5;
                 const int64_t at = (((int64_t)(c < 16 ? pg[0] : pg[1]) * p.c.H + head) << p.c.page_shift) + ((k0 + c) & mask);
-                __builtin_memcpy(s.w, __builtin_assume_aligned(p.c.codes[0] + at * (16 * KB) + h * (8 * KB), 8), 8 * KB);
-                s.params[0] = p.c.params[0][at];
+                typedef uint32_t words2 __attribute__((ext_vector_type(2)));
+                const words2* from = reinterpret_cast<const words2*>(p.c.codes[0] + at * (16 * KB) + h * (8 * KB));
+#pragma unroll
+                for (int k = 0; k < KB; ++k) {
+                    const words2 two = from[k];
+                    words[k >> 1][2 * (k & 1)] = two[0];
+                    words[k >> 1][2 * (k & 1) + 1] = two[1];
+                }
+                parameters[0][0] = p.c.params[0][at];
             } else {                                                           // channels 8 i .. 8 i + 7 of tokens 16 (g >> 1) + 4 (g & 1) + {0 .. 3, 8 .. 11}
-                const int i = l & 15, g = l >> 4;
+                const int i = lane & 15, g = lane >> 4;
                 const int64_t at = (((int64_t)(g < 2 ? pg[0] : pg[1]) * p.c.H + head) << p.c.page_shift) +
                                    ((k0 + 16 * (g >> 1) + 4 * (g & 1)) & mask);
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
                     const uint8_t* row = p.c.codes[1] + (at + (k & 3) + 8 * (k >> 2)) * (16 * VB);
-                    if constexpr (VB == 4) s.w[k] = reinterpret_cast<const uint32_t*>(row)[i];
-                    else if constexpr (VB == 2) s.w[k] = reinterpret_cast<const uint16_t*>(row)[i];
-                    else __builtin_memcpy(&s.w[k], row + (i < 15 ? 3 * i : 44), 4);
+                    if constexpr (VB == 4) words[k >> 2][k & 3] = reinterpret_cast<const uint32_t*>(row)[i];
+                    else if constexpr (VB == 2) words[k >> 2][k & 3] = reinterpret_cast<const uint16_t*>(row)[i];
+                    else {
+                        typedef uint32_t loose __attribute__((aligned(1)));
+                        words[k >> 2][k & 3] = *reinterpret_cast<const loose*>(row + (i < 15 ? 3 * i : 44));
+                    }
                 }
-                const u32x4 lo = *reinterpret_cast<const u32x4*>(p.c.params[1] + at), hi = *reinterpret_cast<const u32x4*>(p.c.params[1] + at + 8);
+                parameters[0] = *reinterpret_cast<const u32x4*>(p.c.params[1] + at);
+                parameters[1] = *reinterpret_cast<const u32x4*>(p.c.params[1] + at + 8);
+            }
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    s.params[k] = lo[k];
-                    s.params[4 + k] = hi[k];
-                }
+            for (int k = 0; k < 2; ++k) {
+                s.words[k] = words[k];
+                s.parameters[k] = parameters[k];
             }
         };
         auto convert = [&](const ShareCodes& s, int buf) {
@@ -1037,13 +1061,13 @@ __global__ __launch_bounds__(64 * NW, 2) void shared_attention_kernel(AttnDev p)
             float* steps = reinterpret_cast<float*>(base + SH_K_BYTES + SH_V_BYTES);
             if (role < 2) {
                 const Masks<KB> masks;
-                const half2v z = raised_zeros(masks, s.params[0], s.params[0]);
+                const half2v z = raised_zeros(masks, s.params(0), s.params(0));
                 const int tok = 32 * role + c;
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
                     typename KeyCodes<KB>::words cw;
 #pragma unroll
-                    for (int k = 0; k < KB; ++k) cw[k] = s.w[KB * half + k];
+                    for (int k = 0; k < KB; ++k) cw[k] = s.w(KB * half + k);
                     uint32_t kk[16];
                     KeyCodes<KB>::fields(cw, kk, masks);
                     each<4>([&](auto mm) {
@@ -1057,7 +1081,7 @@ __global__ __launch_bounds__(64 * NW, 2) void shared_attention_kernel(AttnDev p)
                         *reinterpret_cast<u32x4*>(base + tok * SH_K_PITCH + 16 * chunk) = o;
                     });
                 }
-                if (h == 0) steps[tok] = step_of(s.params[0]) * p.scale2;
+                if (h == 0) steps[tok] = step_of(s.params(0)) * p.scale2;
             } else {
                 const int i = l & 15, g = l >> 4, chunk = 4 * (role - 2) + g;
                 const Masks<VB> masks;
@@ -1067,9 +1091,9 @@ __global__ __launch_bounds__(64 * NW, 2) void shared_attention_kernel(AttnDev p)
                     half2v z[4];
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
-                        z[k] = raised_zeros(masks, s.params[2 * k], s.params[2 * k + 1]);
+                        z[k] = raised_zeros(masks, s.params(2 * k), s.params(2 * k + 1));
                         const int down = VB == 3 && i == 15 ? 8 : 0;
-                        ValueCodes<VB>::template fields<HALF>(s.w[2 * k] >> down, s.w[2 * k + 1] >> down, vv[k], masks);
+                        ValueCodes<VB>::template fields<HALF>(s.w(2 * k) >> down, s.w(2 * k + 1) >> down, vv[k], masks);
                     }
                     each<4>([&](auto jj) {
                         constexpr int j = decltype(jj)::value;
@@ -1084,8 +1108,8 @@ __global__ __launch_bounds__(64 * NW, 2) void shared_attention_kernel(AttnDev p)
                 values(std::integral_constant<int, 1>{});
                 if (i == 0) {
                     f32x4* at = reinterpret_cast<f32x4*>(steps + 64 + 32 * (role - 2) + 16 * (g >> 1) + 4 * (g & 1));
-                    at[0] = f32x4{step_of(s.params[0]), step_of(s.params[1]), step_of(s.params[2]), step_of(s.params[3])};
-                    at[2] = f32x4{step_of(s.params[4]), step_of(s.params[5]), step_of(s.params[6]), step_of(s.params[7])};
+                    at[0] = f32x4{step_of(s.params(0)), step_of(s.params(1)), step_of(s.params(2)), step_of(s.params(3))};
+                    at[2] = f32x4{step_of(s.params(4)), step_of(s.params(5)), step_of(s.params(6)), step_of(s.params(7))};
                 }
             }
         };
@@ -1115,6 +1139,8 @@ __global__ __launch_bounds__(64 * NW, 2) void shared_attention_kernel(AttnDev p)
             const int pages_ok = pages >> (2 * t) & 3, all_see = p.visible ? before - 1 : pos_lo;
             if (pages_ok == 3 && k0 + 31 <= all_see && k0 + 32 <= span.end && x + t < x_end && (p.window <= 0 || p.visible || k0 > pos_hi - p.window)) return;
             const int end = x + t < x_end ? span.end : 0;
+            const int row = again(token);
+            const Sight sight = sight_of(p, before, row, seq.first + row);
 #pragma unroll
             for (int k = 0; k < 16; ++k) {
                 const int kk = k0 + 8 * (k >> 2) + 4 * h + (k & 3);
