@@ -919,9 +919,10 @@ __global__ __launch_bounds__(ATT_NT) void balanced_join_kernel(AttnDev p, int wo
 // lane holds) in 16 bytes.  16 bytes of padding a row spread the reads of a fragment over all banks, and leave one address a lane and constants (chunks
 // exchanged by row took 45 registers of addresses, and spilled).
 //
-// Bound by latency in the step: 2048 rows of 64 heads at 8192 tokens take 684 us, in which the matrix cores are busy for 33 %, the LDS for 33 % and the
-// vector units for 40 %.  Without conversion it is 627 of 842 us (of an earlier step), without anything but it 306: two waves a SIMD, all the registers
-// allow, overlap those only in part.  Raised wave priority around the matrix instructions was slower (699 us), around the conversion no faster.
+// Bound by issue: 2048 rows of 64 heads at 8192 tokens take 615 us of a kernel alone (0.78 PFLOP/s), in which the matrix cores are busy for 38 % and the vector
+// units for 45 % (a wave's 16 weights of a tile cost 90 instructions and 16 exponentials, twice what its 16 matrix instructions take): two waves a SIMD, all
+// that the registers allow, overlap the two only in part.  Raised wave priority around the matrix instructions was slower (640), and so was the conversion at
+// the start of a step for half of the waves (635).
 
 constexpr int SH_ROWS = 32;                // rows per wave
 constexpr int SH_K_PITCH = 2 * ATT_D + 16, SH_V_PITCH = 2 * 64 + 16;
@@ -1188,7 +1189,7 @@ __global__ __launch_bounds__(64 * NW, 2) void shared_attention_kernel(AttnDev p)
             __syncthreads();
             int buf = 0;
             for (int x = x_begin; x < x_end; x += STEPS) {
-#pragma unroll 1
+#pragma unroll
                 for (int y = 0; y < PARTS; ++y) {
                     const unsigned char* base = sh_smem + (PARTS * buf + y) * SH_BUFFER;
                     // (the first tokens lie before everything else)
@@ -1370,9 +1371,10 @@ AttnPlan attention_plan(int64_t B, int64_t T, int H, int Hq, int64_t max_rows, i
         }
     } else {
         // Eight waves convert a token for twice the rows, where they fill every CU and the tokens are many (us, 4 / 8 waves: 2 x 8192 rows of 64 heads at
-        // 8192 tokens 2742 / 2609; 2048 at 2048 132 / 114; 8 x 1024 of 32 heads at 1024 98 / 104; 512 of 64 at 8192, workgroups for half the CUs, 211 / 312).
+        // 8192 tokens 2454 / 2260; 2048 of 64 at 2048 126 / 104; 8 x 256 of 32 at 1500 70 / 63; 8 x 1024 of 32 at 1024 88 / 93; 512 of 64 at 8192, workgroups
+        // for half of the CUs, 195 / 269).
         const int64_t groups8 = pairs * ((rows + 2 * plan.tile_rows - 1) / (2 * plan.tile_rows));
-        if (tuned(Knob::ATT_WAVES, groups8 >= kPlanCus && seen >= 2048 ? 8 : 4) == 8 && pairs < 1 << 23) {   // (a grid has less than 2^32 threads)
+        if (tuned(Knob::ATT_WAVES, groups8 >= kPlanCus && seen >= 1280 ? 8 : 4) == 8 && pairs < 1 << 23) {   // (a grid has less than 2^32 threads)
             plan.waves = 8;
             plan.tile_rows *= 2;
         }
