@@ -216,3 +216,41 @@ def test_groups_that_hold_no_numbers_leave_the_others_alone():
                 assert not codes[page, h, slot].any() and params[page, h, slot] == 0x7C00
             x.codes[page, h, slot], x.params[page, h, slot] = codes[page, h, slot], params[page, h, slot]
     _same_pages(c)
+
+
+@pytest.mark.parametrize("bits", [(4, 3), (2, 4)])
+def test_many_rows_are_written_like_few(bits):
+    """One call of 134400 (row, head) groups and the same rows in calls of 130 rows each; keys and values alone."""
+    rows, H = 4200, 32
+    print(f"[case] write {rows} rows of {H} heads, {bits} bits, whole and in parts", flush=True)
+    c = Batch(78, (rows,), (rows,), H, 64, *bits, filled=False).upload()
+    st = torch.cuda.current_stream()
+    k, v = (torch.randn((rows, H * D), device="cuda", generator=torch.Generator("cuda").manual_seed(n)).half() for n in (1, 2))
+    fq.flatquant_cache_write(c.cache(), c.batch(), k, H * D, v, H * D, None, None, 1, 0.95, 0.9, stream=st)
+    whole = [c.d[n].clone() for n in ("kc", "kp", "vc", "vp")]
+    for alone in (True, False):
+        for n in ("kc", "kp", "vc", "vp"):
+            c.d[n].copy_(torch.from_numpy(c.host["kv".index(n[0])].codes if n[1] == "c" else c.host["kv".index(n[0])].params.view(np.int32)))
+        if alone:
+            fq.flatquant_cache_write(c.cache(), c.batch(), k, H * D, None, 0, None, None, 1, 0.95, 0.9, stream=st)
+            fq.flatquant_cache_write(c.cache(), c.batch(), None, 0, v, H * D, None, None, 1, 0.95, 0.9, stream=st)
+        else:
+            for t in range(0, rows, 130):
+                n = min(130, rows - t)
+                starts, lengths = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([0, n], [t + n]))
+                part = fq.KvBatch(starts, lengths, c.d["table"], 1, n, c.width, c.table.shape[1], n, t + n)
+                fq.flatquant_cache_write(c.cache(), part, k[t:t + n], H * D, v[t:t + n], H * D, None, None, 1, 0.95, 0.9, stream=st)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, c.d[n]) for a, n in zip(whole, ("kc", "kp", "vc", "vp"))), alone
+    pos = np.arange(0, rows, 97)
+    for x, y, name, clip in zip(c.host, (k, v), "kv", (0.95, 0.9)):
+        q, s, z = co.grid32(_host(y).reshape(rows, H, D)[pos], clip, x.bits)
+        at = (c.table[0, pos // 64], slice(None), pos % 64)
+        assert np.array_equal(c.d[name + "c"].cpu().numpy()[at], co.pack(q, x.bits)) and np.array_equal(c.d[name + "p"].cpu().numpy().view(np.uint32)[at], co.parameters(s, z))
+    out = torch.empty_like(k)
+    fq.flatquant_cache_read(c.cache(), c.batch(), None, 0, out, H * D, stream=st)
+    torch.cuda.synchronize()
+    codes, params = c.d["vc"].cpu().numpy(), c.d["vp"].cpu().numpy().view(np.uint32)
+    host = co.Pages(c.pages, H, 64, bits[1])
+    host.codes[:], host.params[:] = codes, params
+    assert np.array_equal(_host(out)[pos].reshape(-1, H, D), host.values(c.table[0, :c.width], pos).transpose(1, 0, 2).astype(np.float16))
