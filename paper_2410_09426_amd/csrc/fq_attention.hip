@@ -361,9 +361,8 @@ __device__ __forceinline__ bool sees_drafted(const Sight& s, int before, int k) 
     const unsigned bit = (unsigned)k - (unsigned)before;
     return (bit < 64u) & (int)((bit & 32 ? (uint32_t)(s.seen >> 32) : (uint32_t)s.seen) >> (bit & 31) & 1u);
 }
-// The step of a value that not every row sees: a number, so that a weight of zero makes a product of zero whatever the page holds.
-__device__ __forceinline__ float finite_step(float s) { return __builtin_fminf(s, 65504.0f); }
-// ... and its parameters: a step that is a number, a zero point of four bits.
+// Parameters of a value that not every row sees: a step that is a number and a zero point of four bits, so that a weight of zero makes a product of zero
+// whatever the page holds.
 __device__ __forceinline__ uint32_t usable_parameters(uint32_t w) { return (w & 0x7C00u) == 0x7C00u ? 0u : w & 0x000FFFFFu; }
 __device__ __forceinline__ float times_step(uint32_t params, float x) {
     float r;
@@ -1134,7 +1133,8 @@ __global__ __launch_bounds__(64 * NW, 2) void shared_attention_kernel(AttnDev p)
                 for (int e = 0; e < 4; ++e) f[4 * k + e] = v[e];
             }
         };
-        // scores of tokens that a row does not see: -infinity (the factors are one then, and the steps numbers)
+        // scores of tokens that a row does not see: -infinity (the factors are one then), and steps of zero: a weight of zero times what the page holds, an
+        // infinity of either sign or a NaN, need not be zero
         auto mask = [&](int x, int t, int pages, f32x16& sc, float (&fk)[16], float (&vs)[16]) {
             const int k0 = span.token(x + t);
             const int pages_ok = pages >> (2 * t) & 3, all_see = p.visible ? before - 1 : pos_lo;
@@ -1147,9 +1147,10 @@ __global__ __launch_bounds__(64 * NW, 2) void shared_attention_kernel(AttnDev p)
                 const int kk = k0 + 8 * (k >> 2) + 4 * h + (k & 3);
                 bool ok = sees(sight, kk);
                 if (p.visible) ok |= sees_drafted(sight, before, kk);
-                sc[k] = (ok & (kk < end) & (pages_ok >> (k >> 3) & 1)) ? sc[k] * fk[k] : -__builtin_inff();
+                ok = ok & (kk < end) & (pages_ok >> (k >> 3) & 1);
+                sc[k] = ok ? sc[k] * fk[k] : -__builtin_inff();
                 fk[k] = 1.0f;
-                vs[k] = finite_step(vs[k]);
+                vs[k] = ok ? vs[k] : 0.0f;
             }
         };
         auto raise = [&](const f32x16& sc, const float (&fk)[16], const float (&vs)[16], float (&prod)[16], float& sum) {
