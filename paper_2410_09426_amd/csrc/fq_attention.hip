@@ -1376,9 +1376,15 @@ AttnPlan attention_plan(int64_t B, int64_t T, int H, int Hq, int64_t max_rows, i
     } else {
         // Eight waves convert a token for twice the rows, where they fill every CU and the tokens are many (us, 4 / 8 waves: 2 x 8192 rows of 64 heads at
         // 8192 tokens 2454 / 2260; 2048 of 64 at 2048 126 / 104; 8 x 256 of 32 at 1500 70 / 63; 8 x 1024 of 32 at 1024 88 / 93; 512 of 64 at 8192, workgroups
-        // for half of the CUs, 195 / 269).
-        const int64_t groups8 = pairs * ((rows + 2 * plan.tile_rows - 1) / (2 * plan.tile_rows));
-        if (tuned(Knob::ATT_WAVES, groups8 >= kPlanCus && seen >= 1280 ? 8 : 4) == 8 && pairs < 1 << 23) {   // (a grid has less than 2^32 threads)
+        // for half of the CUs, 195 / 269), and the rows are enough for them: the last tile of eight has idle waves behind its last row, the last of four takes 64 rows or
+        // fewer in half the time.  (8 heads of 4 queries; 64 sequences of 13 rows at 3000 tokens 98 / 149, of 32 135 / 160; 32 of 80 at 8000 393 / 408, of 128
+        // 543 / 482.)  One workgroup for each CU, all at the same time, bears half as many rows, or in a short context a quarter, which four waves would have to split
+        // and join: 32 sequences of 48 rows at 3000 117 / 105, of 24 at 1500 56 / 48 and at 8000 178 / 207, of 13 at 1500 43 / 46.
+        const int64_t tiles8 = (rows + 2 * plan.tile_rows - 1) / (2 * plan.tile_rows), groups8 = pairs * tiles8;
+        const int64_t rest = rows % plan.tile_rows, rows4 = rows - rest + (rest > plan.tile_rows / 2 ? plan.tile_rows : rest > 0 ? plan.tile_rows / 2 : 0);
+        const bool filled = tiles8 * 2 * plan.tile_rows * 8 <= rows4 * 9 ||
+                            (groups8 == kPlanCus && (rows > plan.tile_rows || (rows > plan.tile_rows / 2 && seen < 3000)));
+        if (tuned(Knob::ATT_WAVES, groups8 >= kPlanCus && seen >= 1280 && filled ? 8 : 4) == 8 && pairs < 1 << 23) {   // (a grid has less than 2^32 threads)
             plan.waves = 8;
             plan.tile_rows *= 2;
         }
