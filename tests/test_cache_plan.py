@@ -32,3 +32,20 @@ def plan(B, rows, length, H=8, G=4, seen=None):
 def test_eight_waves_have_rows(B, rows, length, waves):
     p = plan(B, rows, length)
     assert p.waves == waves and p.tile_rows == (256 if waves == 8 else 128)
+
+
+@pytest.mark.parametrize("B,rows,length,balanced", [
+    (1, 5, 900, False), (1, 6, 4500, True), (1, 8, 2500, True),   # a few pairs: from about 2000 tokens on
+    (16, 7, 1800, False), (16, 5, 6000, True), (30, 8, 3000, False), (30, 5, 10000, True),
+    (45, 6, 3000, False), (40, 6, 16000, True), (64, 7, 9000, False),      # more than one a CU
+    (300, 5, 100, False),                                         # more sequences than that launch holds
+])
+def test_tiles_of_32_rows_are_balanced_by_what_they_take(B, rows, length, balanced):
+    p = plan(B, rows, length)
+    assert p.tile_rows == 32 and p.waves == 4 and (p.workgroups > 0) == balanced
+
+
+@pytest.mark.parametrize("B,rows,length,waves", [(1, 1, 900, 8), (1, 3, 20000, 0), (16, 2, 3500, 16), (16, 1, 20000, 0), (50, 1, 6000, 8), (64, 4, 3000, 8)])
+def test_tiles_of_16_rows(B, rows, length, waves):
+    p = plan(B, rows, length)
+    assert p.tile_rows == 16 and ((p.workgroups > 0) if waves == 0 else (p.workgroups == 0 and p.waves == waves))
