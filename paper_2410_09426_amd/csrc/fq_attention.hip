@@ -1362,6 +1362,9 @@ AttnPlan attention_plan(int64_t B, int64_t T, int H, int Hq, int64_t max_rows, i
         // A workgroup a pair, or balanced?  us, measured at 16 rows, u = units of 128 tokens: a pair of 8 waves takes 6 + 0.58 u, of 16 waves 8 + 0.44 u (up to one a CU),
         // the balanced launch 14 (two kernels and the cut) and what its bytes take, 0.94 u of a pair on every CU, of three quarters of the longest.
         // 1 x 32 pairs of 1000 tokens 10.7 (8 waves) / 14.6, of 4000 22.0 (16) / 14.8; 128 of 4096 22.7 / 24.7, of 16000 66 / 51; 512 of 4096 46.9 (8) / 52.
+        // More pairs than two workgroups of 8 waves a CU hold: of 4 waves, three a CU, in short contexts (us, 4 / 8 waves: 520 of 300 tokens 10.6 / 12.0, of 1000 20.0 / 21.2, of
+        // 2500 35 / 33, of 4000 61 / 47; 768 of 1000 21.5 / 22.6, of 4000 65 / 68; 1024 of 300 13.7 / 17.3, of 3000 62 / 66, of 4000 85 / 82; 2048 of 1000 46.5 / 54.3, of 4000
+        // 155 / 147).
         // Tiles of 32 rows have workgroups of 4 waves: 7 + 1.23 u, the balanced launch 23 and 0.72 u of a pair on every CU.  20 rows, 8 heads: 1 sequence of 1000 tokens
         // 16.7 / 18.9, of 8000 83 / 24; 16 of 2000 27 / 31, of 4000 46 / 36, of 8000 85 / 47; 32 of 4000 47 / 46, of 16000 165 / 111; 48 of 4000 65 / 64, of 8000
         // 118 / 95; 64 of 8000 117 / 119; 32 rows the same within 8 %.
@@ -1370,7 +1373,7 @@ AttnPlan attention_plan(int64_t B, int64_t T, int H, int Hq, int64_t max_rows, i
         int waves;
         if (plan.tile_rows == 16) {
             const double pair8 = 6 + 0.58 * u, pair16 = 8 + 0.44 * u;
-            waves = pairs > 2 * kPlanCus ? 4 : pairs > kPlanCus || pair8 < pair16 ? 8 : 16;
+            waves = pairs > 2 * kPlanCus && seen < 3500 ? 4 : pairs > kPlanCus || pair8 < pair16 ? 8 : 16;
             if (balanced && pairs <= kPlanCus && 14 + 0.7 * each < (pair8 < pair16 ? pair8 : pair16)) waves = 0;
         } else {
             waves = balanced && 23 + 0.72 * each < 7 + 1.23 * u ? 0 : 4;

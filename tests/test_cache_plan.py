@@ -45,7 +45,8 @@ def test_tiles_of_32_rows_are_balanced_by_what_they_take(B, rows, length, balanc
     assert p.tile_rows == 32 and p.waves == 4 and (p.workgroups > 0) == balanced
 
 
-@pytest.mark.parametrize("B,rows,length,waves", [(1, 1, 900, 8), (1, 3, 20000, 0), (16, 2, 3500, 16), (16, 1, 20000, 0), (50, 1, 6000, 8), (64, 4, 3000, 8)])
+@pytest.mark.parametrize("B,rows,length,waves", [(1, 1, 900, 8), (1, 3, 20000, 0), (16, 2, 3500, 16), (16, 1, 20000, 0), (50, 1, 6000, 8), (64, 4, 3000, 8),
+                                               (70, 1, 5000, 8), (70, 1, 2000, 4), (300, 2, 9000, 8), (300, 2, 100, 4)])
 def test_tiles_of_16_rows(B, rows, length, waves):
     p = plan(B, rows, length)
     assert p.tile_rows == 16 and ((p.workgroups > 0) if waves == 0 else (p.workgroups == 0 and p.waves == waves))
