@@ -246,7 +246,8 @@ typedef struct fq_kv_cache {
  *               work there is.  Wrong ones cost time; results differ by rounding alone.
  * The arrays are read on the stream, so one captured graph serves lengths and pages as they change.
  * Limits (FQ_UNSUPPORTED_SHAPE beyond): T <= 2^29, B * H < 2^24, H <= 65535, table_width * page_tokens <= 2^31 - 2^16, pages < 2^31 and
- * pages * H * page_tokens <= 2^48; of row tensors strides <= 2^40 and T * stride <= 2^48, of queries T * Hq < 2^31 - 256.
+ * pages * H * page_tokens <= 2^48; of two sequences or more B * table_stride <= 2^48; of row tensors strides <= 2^40 and T * stride <= 2^48, of queries
+ * T * Hq < 2^31 - 256.
  */
 typedef struct fq_kv_batch {
     const int32_t* row_starts;

@@ -273,7 +273,7 @@ static fq_status cache_args(const fq_kv_cache* cache, const fq_kv_batch* batch, 
     const int page = cache->page_tokens;
     if (page < 16 || page > 1024 || (page & (page - 1)) || cache->H > 65535 || cache->pages > 0x7fffffffLL) return FQ_UNSUPPORTED_SHAPE;
     if (batch->T > (1LL << 29) || batch->B > 0xffffff / cache->H || batch->table_width > 0x7fff0000LL / page) return FQ_UNSUPPORTED_SHAPE;   // grid and index limits
-    if (cache->pages > (1LL << 48) / cache->H / page) return FQ_UNSUPPORTED_SHAPE;
+    if (cache->pages > (1LL << 48) / cache->H / page || (batch->B > 1 && batch->table_stride > (1LL << 48) / batch->B)) return FQ_UNSUPPORTED_SHAPE;
     if (batch->T == 0 || batch->B == 0) {
         empty = true;
         return FQ_OK;
@@ -365,11 +365,11 @@ static fq_status cache_attention(const fq_kv_cache* cache, const fq_kv_batch* ba
     if (Hq > (1 << 24) || batch->T > 0x7fffff00LL / Hq || q_stride > most || out_stride > most || (tree && batch->max_rows > 64)) return FQ_UNSUPPORTED_SHAPE;
     if (empty) return FQ_OK;
     if (!q || !out || (tree && !visible)) return FQ_INVALID_ARG;
-    fq::AttnPlan plan = fq::attention_plan(batch->B, batch->T, cache->H, Hq, batch->max_rows, batch->max_length, batch->max_length);
+    const int64_t max_rows = batch->max_rows < batch->T ? batch->max_rows : batch->T;      // hints: any number is fine
+    fq::AttnPlan plan = fq::attention_plan(batch->B, batch->T, cache->H, Hq, max_rows, batch->max_length, batch->max_length);
     if (workspace_bytes < plan.workspace || (plan.workspace > 0 && !workspace)) return FQ_INVALID_ARG;
     if (window > 0) {   // steps of 32 tokens around a tile's windows, and the first tokens
-        const fq::AttnPlan fewer = fq::attention_plan(batch->B, batch->T, cache->H, Hq, batch->max_rows, batch->max_length,
-                                                      (int64_t)window + sinks + batch->max_rows + 64);
+        const fq::AttnPlan fewer = fq::attention_plan(batch->B, batch->T, cache->H, Hq, max_rows, batch->max_length, (int64_t)window + sinks + max_rows + 64);
         if (fewer.workspace <= plan.workspace) plan = fewer;
     }
     auto bad = [](const void* p, int a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; };
@@ -383,7 +383,7 @@ static fq_status cache_attention(const fq_kv_cache* cache, const fq_kv_batch* ba
     fq::AttnArgs a;
     a.q = static_cast<const _Float16*>(q); a.out = static_cast<_Float16*>(out); a.q_stride = q_stride; a.out_stride = out_stride;
     a.Hq = Hq; a.scale = scale; a.window = window; a.sinks = sinks; a.visible = visible; a.workspace = static_cast<float*>(workspace);
-    a.max_rows = batch->max_rows;
+    a.max_rows = max_rows;
     return fq::finish(fq::attention_launch(d, a, plan, static_cast<hipStream_t>(stream)));
 }
 
