@@ -1458,7 +1458,9 @@ hipError_t attention_launch(const CacheDev& c, const AttnArgs& a, const AttnPlan
     d.c = c;
     d.q = a.q; d.out = a.out; d.visible = a.visible; d.part = a.workspace; d.stats = a.workspace + plan.stats_at;
     d.q_stride = a.q_stride; d.out_stride = a.out_stride;
-    d.scale2 = a.scale * 1.44269504088896340736f;
+    // Scores and, times a key's step, factors stay finite: two scores of finite rows that differ do so by 2^-48 of the scale or more, so that from 2^64 on the
+    // larger one has all the weight, whatever the scale.
+    d.scale2 = __builtin_fminf(__builtin_fmaxf(a.scale * 1.44269504088896340736f, -0x1p64f), 0x1p64f);
     d.Hq = a.Hq; d.G = a.Hq / c.H; d.window = a.window; d.sinks = a.sinks;
     d.chunk = plan.chunk; d.splits = plan.splits; d.min_units = tuned(Knob::ATT_CHUNK, 512) / 128;
     d.min_units = d.min_units < 1 ? 1 : d.min_units < 1 << 20 ? d.min_units : 1 << 20;

@@ -1,0 +1,61 @@
+"""Attention over the paged key/value cache at the ends of what scores can be: the largest scales."""
+import numpy as np
+import pytest
+
+from oracle import cache_oracle as co
+from cache_util import D, Batch, run_attention
+
+pytestmark = pytest.mark.gpu
+LAUNCHES = {"chosen": {}, "balanced": {"FLATQUANT_ATT_WAVES": 0, "FLATQUANT_ATT_CHUNK": 128}, "4 waves": {"FLATQUANT_ATT_WAVES": 4},
+            "8 waves": {"FLATQUANT_ATT_WAVES": 8}, "16 waves": {"FLATQUANT_ATT_WAVES": 16}}
+SIZES = [((1, 2), (300, 45), 3), ((9, 4), (70, 300), 3), ((100,), (260,), 2)]      # rows, lengths, query heads a head
+
+
+@pytest.fixture
+def launched(tuning, request):
+    for name, value in LAUNCHES[request.param].items():
+        tuning(name, value)
+    return request.param
+
+
+def _of_sequence(c, b):
+    L = c.lengths[b]
+    return [f(c.table[b, :c.width], np.arange(L)) for f in (c.host[0].values, c.host[1].values, c.host[1].steps)]
+
+
+@pytest.mark.parametrize("launched", LAUNCHES, indirect=True)
+@pytest.mark.parametrize("scale", [1e25, 1e30, -1e30, 3.4e38, -3.4e38])
+@pytest.mark.parametrize("rows,lengths,G", SIZES)
+def test_the_largest_score_has_it_all(rows, lengths, G, scale, launched):
+    """One value, but where scores are equal: rows of zeros get the mean of what they see.  Rows whose two largest scores lie within the rounding of a score
+    of each other are not looked at."""
+    print(f"[case] scale {scale}, {rows} of {lengths}, {launched}", flush=True)
+    H = 2
+    c = Batch(81, rows, lengths, H, 16, 4, 4).upload()
+    q = c.row_tensor(H * G)
+    q[::5, :D] = 0
+    got = run_attention(c, q, G, scale).astype(np.float64)
+    looked = 0
+    for b in range(c.B):
+        k, v, step = _of_sequence(c, b)
+        seen = c.visible(b)
+        for i in range(rows[b]):
+            t, j = c.starts[b] + i, np.flatnonzero(seen[i])
+            for h in range(H * G):
+                y = q[t, h * D:(h + 1) * D].astype(np.float64)
+                s = np.sign(scale) * (k[h // G][j] @ y)
+                if y.any():
+                    top = np.argsort(s)[::-1][:2]
+                    # a score: 280 roundings of fp32 over its products, and 132 * 2^-18 max |q| code units (co.attention64), twice
+                    off = 2 * (280 * 2.0 ** -24 * (np.abs(k[h // G][j]) @ np.abs(y)).max() * 16 + 132 * 2.0 ** -18 * np.abs(y).max())
+                    if len(j) > 1 and s[top[0]] - s[top[1]] <= off:
+                        continue
+                    w = np.zeros(len(j))
+                    w[top[0]] = 1.0
+                else:
+                    w = np.full(len(j), 1.0 / len(j))
+                vj, sj = v[h // G][j], step[h // G][j]
+                tol = co.attention_bound((w @ vj)[None], (w @ np.abs(vj))[None], np.array([w @ sj]), np.zeros(1), lengths[b])[0]
+                assert np.all(np.abs(got[t, h] - w @ vj) <= tol), (t, h)
+                looked += 1
+    assert looked > c.starts[-1] * H * G // 2
