@@ -1,9 +1,10 @@
-"""Attention over the paged key/value cache at the ends of what scores can be: the largest scales."""
+"""Attention over the paged key/value cache at the ends of what scores can be: the largest scales, rows whose queries are no numbers beside rows whose are,
+and long contexts."""
 import numpy as np
 import pytest
 
 from oracle import cache_oracle as co
-from cache_util import D, Batch, run_attention
+from cache_util import D, Batch, check_attention, run_attention
 
 pytestmark = pytest.mark.gpu
 LAUNCHES = {"chosen": {}, "balanced": {"FLATQUANT_ATT_WAVES": 0, "FLATQUANT_ATT_CHUNK": 128}, "4 waves": {"FLATQUANT_ATT_WAVES": 4},
@@ -59,3 +60,40 @@ def test_the_largest_score_has_it_all(rows, lengths, G, scale, launched):
                 assert np.all(np.abs(got[t, h] - w @ vj) <= tol), (t, h)
                 looked += 1
     assert looked > c.starts[-1] * H * G // 2
+
+
+@pytest.mark.parametrize("launched", LAUNCHES, indirect=True)
+@pytest.mark.parametrize("rows,lengths,G", SIZES)
+def test_queries_that_are_no_numbers_leave_the_other_rows_alone(rows, lengths, G, launched):
+    print(f"[case] queries of infinity and NaN, {rows} of {lengths}, {launched}", flush=True)
+    H = 2
+    c = Batch(82, rows, lengths, H, 16, 4, 3).upload()
+    q = c.row_tensor(H * G)
+    bad = np.zeros((c.T, H * G), dtype=bool)
+    for n, value in enumerate((np.inf, -np.inf, np.nan, 65504.0)):
+        t, h = (n * 7) % c.T, (n * 5 + 1) % (H * G)
+        q[t, h * D + 11 * n] = value
+        bad[t, h] = True
+    got = run_attention(c, q, G, 0.09)
+    fine = np.where(np.repeat(bad, D, axis=1), np.float16(0), q)
+    want, tol = c.attention(fine.reshape(c.T, H * G, D), G, 0.09)
+    n = c.starts[-1]
+    err = np.abs(got[:n].astype(np.float64) - want[:n])
+    assert np.all(err[~bad[:n]] <= tol[:n][~bad[:n]])
+
+
+@pytest.mark.parametrize("rows,lengths,H,G,bits,window,sinks", [
+    ((1, 1), (20000, 9000), 1, 4, (4, 4), 0, 0),
+    ((2, 6), (9001, 17000), 1, 5, (2, 4), 0, 0),
+    ((3, 1), (12000, 30), 1, 4, (3, 3), 5000, 9),
+    ((40, 3), (12000, 7000), 1, 2, (4, 3), 0, 0),
+    ((40, 3), (12000, 7000), 1, 2, (2, 2), 4100, 70),
+])
+def test_long_contexts(rows, lengths, H, G, bits, window, sinks):
+    print(f"[case] {rows} of {lengths}, {H} x {G} heads, {bits} bits, window {window} + {sinks}", flush=True)
+    c = Batch(83, rows, lengths, H, 64, *bits).upload()
+    q = c.row_tensor(H * G, gain=2.0)
+    check_attention(c, q, G, 0.09, run_attention(c, q, G, 0.09, window, sinks), window=window, sinks=sinks)
+    if not window and max(rows) <= 64:
+        masks = c.r.integers(0, 2 ** 63, c.T).astype(np.uint64)
+        check_attention(c, q, G, 0.09, run_attention(c, q, G, 0.09, masks=masks), masks=masks)
