@@ -56,6 +56,7 @@ _CACHE_PARAMS = {
     "flatquant_cache_tree_attention": ("cache batch q q_stride Hq scale visible out out_stride workspace workspace_bytes", "ppplifpplpl"),
 }
 CACHE_CALLS = tuple(_CACHE_PARAMS)
+_PARAMS = {**_NATIVE_PARAMS, **_CACHE_PARAMS}
 
 _lib = None
 _fqcall = None
@@ -77,7 +78,7 @@ def lib() -> ctypes.CDLL:
                 "(there is no CPU fallback for the FlatQuant kernels)")
         L = ctypes.CDLL(LIB_PATH)
         vp, i32, i64, f32 = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_float
-        for name, (params, types) in {**_NATIVE_PARAMS, **_CACHE_PARAMS}.items():
+        for name, (params, types) in _PARAMS.items():
             getattr(L, name).argtypes = [{"p": vp, "i": i32, "l": i64, "f": f32}[t] for t in types] + [vp]
             getattr(L, name).restype = i32
         L.fq_cache_attention_workspace.argtypes = [vp, vp, i32]
@@ -112,7 +113,7 @@ def lib() -> ctypes.CDLL:
         L.fq_abi_version.restype = i32
         _lib = L
         if _fqcall:
-            _fqcall.bind({n: ctypes.cast(getattr(L, n), vp).value for n in NATIVE + CACHE_CALLS})
+            _fqcall.bind({n: ctypes.cast(getattr(L, n), vp).value for n in _PARAMS})
     return _lib
 
 
@@ -134,7 +135,7 @@ def _stream(stream) -> Optional[int]:
 
 def _ctypes_call(name: str):
     """A launching entry point through ctypes, written out from its parameters."""
-    params, types = (_NATIVE_PARAMS.get(name) or _CACHE_PARAMS[name])
+    params, types = _PARAMS[name]
     convert = {"p": "_ptr", "i": "int", "l": "int", "f": "float"}
     values = ", ".join(f"{convert[t]}({p})" for p, t in zip(params.split(), types))
     scope = {}
@@ -150,10 +151,10 @@ def _ctypes_call(name: str):
 try:
     _fqcall = importlib.import_module(__package__ + "._fqcall")
 except ModuleNotFoundError:                     # not built, or built for another interpreter
-    globals().update((n, _ctypes_call(n)) for n in NATIVE + CACHE_CALLS)
+    globals().update((n, _ctypes_call(n)) for n in _PARAMS)
 else:
     _fqcall.connect(lib, FlatQuantError)
-    globals().update((n, getattr(_fqcall, n)) for n in NATIVE + CACHE_CALLS)
+    globals().update((n, getattr(_fqcall, n)) for n in _PARAMS)
 
 
 class _HostStruct:

@@ -343,12 +343,16 @@ PyObject* py_connect(PyObject*, PyObject* const* a, Py_ssize_t n) {
     for (void*& e : g_entry) e = nullptr;
     Py_RETURN_NONE;
 }
-// bind({name: address}): the entry points of the library just loaded; those of the cache stay as they are if they are not named
+// bind({name: address}): entry points of the library just loaded; those that are not named stay as they are
 PyObject* py_bind(PyObject*, PyObject* addresses) {
+    if (!PyMapping_Check(addresses)) {
+        PyErr_SetString(PyExc_TypeError, "bind({name: address})");
+        return nullptr;
+    }
     void* found[COUNT];
     for (Signature* s : kAll) {
         found[s->entry] = g_entry[s->entry];
-        if (s->entry >= CACHE_WRITE && !PyMapping_HasKeyString(addresses, s->name)) continue;
+        if (!PyMapping_HasKeyString(addresses, s->name)) continue;
         PyObject* o = PyMapping_GetItemString(addresses, s->name);
         if (!o) return nullptr;
         found[s->entry] = PyLong_AsVoidPtr(o);
