@@ -29,7 +29,7 @@ def hipcc() -> str:
 # The wave-per-token kernel takes plain arguments in the order it needs them; the first 14 dwords are delivered in
 # registers at wave start (kernel-argument preloading), which takes a scalar-memory round trip off the front of every wave.
 PRELOAD = ["-mllvm", "-amdgpu-kernarg-preload-count=16"]
-FILE_FLAGS = {"fq_kv.hip": ["-fno-honor-nans"], "fq_tq_wave.hip": PRELOAD, "fq_gemm.hip": PRELOAD, "fq_gemm_mx.hip": PRELOAD, "fq_attention.hip": PRELOAD}
+FILE_FLAGS = {"fq_kv.hip": ["-fno-honor-nans"], "fq_tq_wave.hip": PRELOAD, "fq_gemm.hip": PRELOAD, "fq_gemm_mx.hip": PRELOAD}
 
 
 def link(cmd, verbose: bool) -> None:
