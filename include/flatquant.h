@@ -292,6 +292,7 @@ fq_status flatquant_cache_read(const fq_kv_cache* cache, const fq_kv_batch* batc
  * k_j and v_j the de-quantized rows of key/value head h / (Hq / H).  A row at position p sees token j of its sequence if j <= p and, with a
  * window (window > 0), j > p - window or j < sinks: the last `window` tokens and the first `sinks`.  window == 0 is no window, and sinks
  * is then not looked at.  A row that sees nothing gets zeros.  What lies in places that a row does not see, whatever it is, does not change it.
+ * A row that sees a group whose step is an infinity or a NaN gets NaN.
  * Scores, maxima and sums are fp32; the weights (times the value's step) are rounded to fp16 for the matrix instructions.
  *   q, out  fp16 [T, Hq, 128], rows q_stride / out_stride halves apart (multiples of 8, >= 128 Hq), 16-byte aligned, not overlapping.
  *   Hq      a multiple of H.

@@ -372,6 +372,11 @@ __device__ __forceinline__ float times_step(uint32_t params, float x) {
     asm("v_fma_mix_f32 %0, %1, %2, 0 op_sel_hi:[1,0,0]" : "=v"(r) : "v"(params), "v"(x));
     return r;
 }
+// x, or NaN where a token's step is no number.
+__device__ __forceinline__ float if_number(uint32_t params, float x) {
+    asm("v_fma_mix_f32 %0, %1, 0, %0 op_sel_hi:[1,0,0]" : "+v"(x) : "v"(params));
+    return x;
+}
 // sum + product (a half of `pair`) times the zero point in a token's parameters, both read where they are.
 template <int HI>
 __device__ __forceinline__ float zero_sum(uint32_t pair, uint32_t params, float sum) {
@@ -388,7 +393,10 @@ __device__ __forceinline__ bool weigh(const Scores& score, Factor factor, Step s
 #pragma unroll
     for (int k = 0; k < N; ++k) {
         float e = __builtin_amdgcn_exp2f(__builtin_fmaf(score[k], factor(k), -ref));
-        if constexpr (CAPPED) e = __builtin_fminf(e, 0x1p14f * __builtin_amdgcn_rcpf(__builtin_fmaxf(step(k), 0x1p-25f)));
+        if constexpr (CAPPED) {
+            const float cap = 0x1p14f * __builtin_amdgcn_rcpf(__builtin_fmaxf(step(k), 0x1p-25f));
+            e = e > cap ? cap : e;                                             // (a NaN stays one)
+        }
         sum += e;
         prod[k] = e * step(k);
         big = __builtin_fmaxf(big, prod[k]);
@@ -557,14 +565,14 @@ __device__ __forceinline__ void few_rows(const AttnDev& p, unsigned char* smem, 
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int k = k0 + 16 * t + 4 * g + r;
-                    vp[4 * t + r] = usable_parameters(vp[4 * t + r]);
                     const bool held = page_ok & (k < span.end);
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
                         bool ok = sees(sight[n], k);
                         if (p.visible) ok |= sees_drafted(sight[n], before, k);
-                        sc[n][t][r] = (ok & held) ? sc[n][t][r] : -__builtin_inff();
+                        sc[n][t][r] = (ok & held) ? if_number(vp[4 * t + r], sc[n][t][r]) : -__builtin_inff();
                     }
+                    vp[4 * t + r] = usable_parameters(vp[4 * t + r]);
                 }
             }
         }

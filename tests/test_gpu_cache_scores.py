@@ -1,5 +1,5 @@
 """Attention over the paged key/value cache at the ends of what scores can be: the largest scales, rows whose queries are no numbers beside rows whose are,
-and long contexts."""
+groups whose steps are none, and long contexts."""
 import numpy as np
 import pytest
 
@@ -80,6 +80,34 @@ def test_queries_that_are_no_numbers_leave_the_other_rows_alone(rows, lengths, G
     n = c.starts[-1]
     err = np.abs(got[:n].astype(np.float64) - want[:n])
     assert np.all(err[~bad[:n]] <= tol[:n][~bad[:n]])
+
+
+@pytest.mark.parametrize("launched", LAUNCHES, indirect=True)
+@pytest.mark.parametrize("which", [0, 1])
+@pytest.mark.parametrize("rows,lengths,G,at", [((1, 2), (300, 45), 3, (299, 43)), ((1, 2), (300, 45), 3, (100, 44)), ((9, 4), (70, 300), 3, (66, 298)), ((9, 4), (70, 300), 3, (3, 64)),
+                                               ((100,), (260,), 2, (190,)), ((100,), (260,), 2, (50,))])
+def test_groups_whose_step_is_no_number(rows, lengths, G, at, which, launched):
+    """A key or a value that overflowed when it was written (an infinite step, zero codes): NaN for the rows of its head that see it, whether the other rows
+    of the step do or not, and nothing for the others."""
+    print(f"[case] {('key', 'value')[which]} {at} of {rows} of {lengths}, {launched}", flush=True)
+    H = 2
+    c = Batch(84, rows, lengths, H, 16, 4, 3)
+    x = c.host[which]
+    for b, j in enumerate(at):
+        page, slot = x.place(c.table[b, :c.width], j)
+        x.codes[page, 0, slot], x.params[page, 0, slot] = 0, 0x7C00
+    c.upload()
+    q = c.row_tensor(H * G)
+    got = run_attention(c, q, G, 0.09)
+    sees = np.zeros(c.T, dtype=bool)
+    for b, j in enumerate(at):
+        sees[c.starts[b]:c.starts[b + 1]] = c.visible(b)[:, j]
+    assert sees.any() and np.isnan(got[sees][:, :G]).all()
+    for x in c.host:
+        x.params[(x.params & 0xFFFF) == 0x7C00] = 0                 # as zeros, for the rows that do not see them
+    want, tol = c.attention(q.reshape(c.T, H * G, D), G, 0.09)
+    err = np.abs(got.astype(np.float64) - want)
+    assert np.all(err[:, G:] <= tol[:, G:]) and np.all(err[~sees] <= tol[~sees])
 
 
 @pytest.mark.parametrize("rows,lengths,H,G,bits,window,sinks", [
