@@ -235,7 +235,7 @@ typedef struct fq_kv_cache {
 /*
  * The batch: B sequences, and rows of which the last ones of every sequence are the call's (its new tokens).
  *   row_starts  i32 [B + 1]: sequence b has rows row_starts[b] .. row_starts[b + 1] - 1 of the call's row tensors (n_b of them, none is
- *               fine); ascending.  Rows from row_starts[B] on (padding) are neither read nor written.
+ *               fine); ascending.  Rows from row_starts[B] on (padding) are not written, and what they hold does not matter.
  *   lengths     i32 [B]: tokens of the sequence with the new ones.  Row i of sequence b is the token at position lengths[b] - n_b + i;
  *               a row whose position is negative is no token.
  *   page_table  i32 [B, table_width], rows table_stride apart: the page of tokens page_tokens * j .. of the sequence.  A number outside

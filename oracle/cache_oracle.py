@@ -56,7 +56,7 @@ class Pages:
     def __init__(self, pages, H, page, bits, fill=0xA5):
         self.page, self.bits = page, bits
         self.codes = np.full((pages, H, page, D * bits // 8), fill, dtype=np.uint8)
-        self.params = np.full((pages, H, page), fill * 0x01010101, dtype=np.uint32)      # a NaN step and a zero point that is none
+        self.params = np.full((pages, H, page), fill * 0x01010101, dtype=np.uint32)      # a negative step and a zero point that is none
 
     def place(self, table, pos):
         """(page, slot) of a token of the sequence with this table row, or None."""

@@ -14,7 +14,7 @@
 //
 // Softmax in one pass: weights are 2^(score - M), M a reference per row that is raised only where a weight times its step would pass
 // 2^15 (fp16's range) or the weights 2^40: most steps neither reduce a maximum nor touch the accumulators.  When it is raised it is put
-// 2^7 above the largest product, so that products below 2^-14 of it, in fp16's subnormals, lose no more than 2^-32 of that product.
+// so that the largest product is 2^7: those below 2^-21 of it, fp16's subnormals, lose no more than 2^-32 of it.
 //
 // The 4, 8 or 16 waves of a workgroup take its steps in turn and meet in LDS at the end; where the rows are few the axis is split further over
 // workgroups, whose partial results (M, sum, channels, in fp32) a second kernel joins.
@@ -463,7 +463,8 @@ __device__ __forceinline__ void few_rows(const AttnDev& p, unsigned char* smem, 
         for (int k = 0; k <= DEPTH; ++k) pages_of(x + NW * k, pg[k]);
 
     // Rows: queries in the order of the codes, brought up to 2^9 and down by the codes' shifts (a power of two each, and back in `factor`; the sign of the
-    // scale is in the queries), their sums, positions.  Asked for before the first steps: loads return in order.
+    // scale is in the queries), their sums, positions.  A channel that becomes a subnormal fp16 number is rounded by 2^-25 of the row's norm at most, less than
+    // the fp32 sums of its 128 products lose.  Asked for before the first steps: loads return in order.
     half8 raw[NT][4];
     Sight sight[NT];
 #pragma unroll
@@ -929,10 +930,10 @@ __global__ __launch_bounds__(ATT_NT) void balanced_join_kernel(AttnDev p, int wo
 // lane holds) in 16 bytes.  16 bytes of padding a row spread the reads of a fragment over all banks, and leave one address a lane and constants (chunks
 // exchanged by row took 45 registers of addresses, and spilled).
 //
-// Bound by issue: 2048 rows of 64 heads at 8192 tokens take 615 us of a kernel alone (0.78 PFLOP/s), in which the matrix cores are busy for 38 % and the vector
-// units for 45 % (a wave's 16 weights of a tile cost 90 instructions and 16 exponentials, twice what its 16 matrix instructions take): two waves a SIMD, all
-// that the registers allow, overlap the two only in part.  Raised wave priority around the matrix instructions was slower (640), and so was the conversion at
-// the start of a step for half of the waves (635).
+// Bound by issue: 2048 rows of 64 heads at 8192 tokens take 505 us (0.95 PFLOP/s) launch after launch, once the clock has settled, which takes about 70 of them
+// (610 in the first ones after a pause).  The matrix cores are busy for 38 % of it and the vector units for 45 % (a wave's 16 weights of a tile cost 90 instructions and 16 exponentials, twice what its 16 matrix instructions take): two waves a SIMD, all
+// that the registers allow, overlap the two only in part.  Raised wave priority around the matrix instructions was slower (640 / 615, both after a pause), and so
+// was the conversion at the start of a step for half of the waves (635 / 615).
 
 constexpr int SH_ROWS = 32;                // rows per wave
 constexpr int SH_K_PITCH = 2 * ATT_D + 16, SH_V_PITCH = 2 * 64 + 16;

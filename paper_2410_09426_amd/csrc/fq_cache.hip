@@ -210,7 +210,8 @@ static hipError_t rows_launch(const CacheDev& c, const CacheRows& r, hipStream_t
 }
 template <bool WRITE>
 static hipError_t rows_launch(const CacheDev& c, const CacheRows& r, hipStream_t stream) {
-    // 16 or 64 rows a wave?  Keys and values of 2048 x 8 rows and heads written in 6.6 / 10.3 us, of 4096 x 32 in 24.3 / 24.7, of 32768 x 8 in 43.6 / 37.5, of 32768 x 32
+    // 4 or 16 rows a wave?  4096 groups (rows x heads) of keys and values written in 3.5 / 4.5 us and read back in 3.6 / 3.9, 8192 in 4.4 / 4.6 and 4.2 / 4.2, 16384 in
+    // 5.6 / 5.3 and 5.7 / 4.9.  16 or 64?  Keys and values of 2048 x 8 rows and heads written in 6.6 / 10.3 us, of 4096 x 32 in 24.3 / 24.7, of 32768 x 8 in 43.6 / 37.5, of 32768 x 32
     // in 145 / 142; read back in 5.3 / 8.2, 16.7 / 20.6, 28.2 / 31.3, 147 / 152.
     if (c.T * c.H <= 4096) return rows_launch<1, WRITE>(c, r, stream);
     if constexpr (WRITE) {
