@@ -5,8 +5,8 @@
 // by the same wave into one piece; its lanes find the places of a row each, once, and hand them on.  Neighbouring waves and workgroups
 // take the other heads of the same rows.
 //
-// Bound by memory: 16384 rows of 32 heads (268 MB of fp16, 62 MB of codes) are written in 78 us and read back in 62, 4.2 and 5.3 TB/s (a copy of
-// 1 GB 4.73); writing issues 75 vector instructions for the eight values of a lane, which is most of what it lacks (150 took 107 us).  Rows of
+// Bound by memory: 16384 rows of 32 heads (268 MB of fp16, 62 MB of codes) are written in 78 us and read back in 73 to 78, 4.2 to 4.5 TB/s (a copy
+// of 1 GB 4.73), several sets of rows and pages in turn; writing issues 75 vector instructions for the eight values of a lane, which is most of what it lacks (150 took 107 us).  Rows of
 // few tokens (a decode step) are a launch and four loads one after the other: 3.6 us.
 #include "fq_internal.h"
 #include "fq_device.h"
