@@ -314,9 +314,79 @@ fq_status flatquant_cache_tree_attention(const fq_kv_cache* cache, const fq_kv_b
                                          const uint64_t* visible, void* out, int64_t out_stride, void* workspace, int64_t workspace_bytes,
                                          void* stream);
 
-/* Workspace of the two attention calls for this cache and batch, from the host's figures alone (B, T, H, Hq, max_rows, max_length); 0 if they
+/* Workspace of the attention calls for this cache and batch, from the host's figures alone (B, T, H, Hq, max_rows, max_length); 0 if they
  * need none, -1 for arguments they refuse. */
 int64_t fq_cache_attention_workspace(const fq_kv_cache* cache, const fq_kv_batch* batch, int Hq);
+
+/*
+ * The tables of a step.  A serving loop knows, of every sequence, how many tokens its pages hold, how many of them stay and how many rows are new; the
+ * call works out the batch's arrays, takes the pages that are needed from a ring of free ones, gives back those that are not, and says where every row is.
+ *
+ * The ring of free pages (a HOST struct that holds device pointers, like the others):
+ *   ring   i32 [capacity]: pages; the free ones are entries state[0] .. state[1] - 1, each modulo the capacity.  At the start a program puts all of its pages
+ *          in (capacity = pages, ring[i] = i, state = {0, pages}).
+ *   state  i64 [2]: pages that have been taken from the ring, and that have been put into it, since the start
+ *   next   i64 [3]: both behind the call, and how many pages were missing.  next may be state (of three numbers then): the next call goes on from there.
+ */
+typedef struct fq_page_pool {
+    int32_t* ring;
+    const int64_t* state;
+    int64_t* next;
+    int64_t capacity;
+} fq_page_pool;
+
+/*
+ *   held, keep, rows  i32 [B]: tokens whose pages the table holds, how many of them (the first ones) stay, new ones.  held and keep may be batch->lengths, as they
+ *          are read before it is written; rows that drafts took are given up by keep < held, a sequence ends with keep = rows = 0, its place in the batch can get a
+ *          new one in the same call.  Negative numbers count as 0, keep as held at most.
+ * With n_b = rows[b], cut so that all of them are T at most and a length below 2^31, and P(x) = ceil(x / page_tokens), table_width at most:
+ *   batch->row_starts[b]  n_0 + .. + n_(b - 1), and of all in [B];   batch->lengths[b] = keep[b] + n_b
+ *   batch->page_table     entries P(held) .. P(length) - 1 of every sequence: pages from the ring in the order of the sequences and their entries.  If the ring has fewer
+ *          than the call takes, none is taken: the entries become -1 (no page: such tokens are not written and not visible) and next[2] says how many are
+ *          missing; a program gives others back and makes the call again with the same held, keep and rows.
+ *          Entries P(length) .. P(held) - 1 are put into the ring in the same order, but for those that are no page, and can be taken from the next call on.  No entry is
+ *          changed but those that get a page or -1.
+ *   positions  i32 [T], slots i64 [T], either NULL: position of every row, and page * page_tokens + position % page_tokens; -1 for rows behind the last sequence, slots
+ *          also for a token that has no page.
+ * The batch's arrays are written here, max_rows and max_length are not looked at.  page_tokens and pages are those of the cache; page_tokens a power of two, 16 .. 1024.
+ * T == 0 is a step that only gives pages back; B == 0 returns FQ_OK without launching.  Limits as for fq_kv_batch with H = 1, and table_width <= 2^20.
+ */
+fq_status flatquant_cache_advance(const fq_kv_batch* batch, const fq_page_pool* pool, int page_tokens, int64_t pages, const int32_t* held,
+                                  const int32_t* keep, const int32_t* rows, int32_t* positions, int64_t* slots, void* stream);
+
+/*
+ * Queries and keys between their product and the cache, head by head: norm, rotation by the row's position, and for a transformed key cache the matrix of the head
+ * (Sec. 3.2 "Self-Attention": P_h acts on the rotated keys, its inverse transpose on the rotated queries).  Of a row x of 128 channels at position p:
+ *     y = w x / sqrt( mean x^2 + eps )                    (w_q / w_k NULL: y = x)
+ *     (y_a, y_b) -> (y_a cos t_i - y_b sin t_i, y_b cos t_i + y_a sin t_i),  t_i = p * turns[i] * 2^-64 of a turn,   i < rotary / 2:
+ *         interleaved 0: channels a = i, b = i + rotary / 2;   1: a = 2 i, b = 2 i + 1;   channels from rotary on stay as they are
+ *     out = fp16( y ),  or with a matrix  fp16( fp16( y ) P ), fp32 accumulation, as flatquant_head_transform has it.
+ *   q, k, q_out, k_out  fp16 [T, Hq or H, 128], rows a stride of halves apart (multiples of 8, >= 128 Hq or 128 H; both may lie in the rows of one fused product),
+ *              16-byte aligned; outputs overlap nothing.  q or k may be NULL (then nothing of that side is looked at).
+ *   positions  i32 [T]; a row whose position is negative is no token: its outputs are left as they are.
+ *   turns      u64 [rotary / 2], 16-byte aligned (fq_rope_turns makes them); NULL if rotary is 0.  The angle is exact to 2^-32 of a turn at every position.
+ *   rotary     0, 32, 64, 96 or 128.
+ *   w_q, w_k   fp16 [128], 16-byte aligned, shared by the heads, or NULL;  eps > 0.
+ *   P_q, P_k   fp16 [128, 128], or with per_head [Hq, 128, 128] and [H, 128, 128], row-major, 16-byte aligned, or NULL.
+ * T == 0 returns FQ_OK without launching.  T <= 2^29, Hq, H <= 65535 (32767 with per_head), T * Hq and T * H < 2^31 - 256, strides <= 2^40 and T * stride <= 2^48.
+ */
+fq_status flatquant_head_rope(const void* q, int64_t q_stride, int Hq, const void* k, int64_t k_stride, int H, int64_t T, const int32_t* positions,
+                              const uint64_t* turns, int rotary, int interleaved, const void* w_q, const void* w_k, float eps,
+                              const void* P_q, const void* P_k, int per_head, void* q_out, int64_t q_out_stride, void* k_out, int64_t k_out_stride,
+                              void* stream);
+
+/*
+ * flatquant_cache_attention with other scores and one more mask:
+ *     score = scale * q[t, h, :] . k_j,   with cap > 0  cap * tanh(score / cap),   then  score - slopes[h] * |p - j|
+ * for a row at position p.  cap 0 is none, slopes NULL none.
+ *   slopes   fp32 [Hq], finite, 4-byte aligned.
+ *   prefix   i32 [B], 4-byte aligned, or NULL: a row of sequence b also sees every token before prefix[b], those behind it among them, whatever the window.
+ *   visible  u64 [T] or NULL: the masks of flatquant_cache_tree_attention; window and sinks 0, slopes and prefix NULL then.
+ * Everything else, the workspace and what a row that sees nothing or no number gets, as for the other two.
+ */
+fq_status flatquant_cache_scored_attention(const fq_kv_cache* cache, const fq_kv_batch* batch, const void* q, int64_t q_stride, int Hq, float scale,
+                                           float cap, const float* slopes, const int32_t* prefix, int window, int sinks, const uint64_t* visible,
+                                           void* out, int64_t out_stride, void* workspace, int64_t workspace_bytes, void* stream);
 
 /*
  * De-quantization check helper (Sec. 2.1: W^ = s * Pi(W / s)).
@@ -365,6 +435,10 @@ fq_status fq_choose_factors(int64_t n, int* n1, int* n2);
  * `max_residual` is not NULL it receives max |P^T out - I| of the rounded result, in fp64.  Returns FQ_INVALID_ARG
  * for null pointers, n out of range or a singular matrix (a pivot below 1e-12 times the largest entry). */
 fq_status fq_inverse_transpose(const void* P, int n, void* out, double* max_residual);
+
+/* Host helper of flatquant_head_rope: turns[i] = round( frequencies[i] / (2 pi) * 2^64 ) modulo 2^64, the angle that a position adds (radians,
+ * any sign) in units of 2^-64 of a turn.  FQ_INVALID_ARG for null pointers, n < 0 or a frequency that is not finite.  Host pointers. */
+fq_status fq_rope_turns(const double* frequencies, int n, uint64_t* turns);
 
 /* On-chip footprint test of App. "Detailed Design of Kernel Fusion": returns 1
  * when (n1*n1 + 2*n1*n2)*2 < m and (n2*n2 + 2*n1*n2)*2 < m for m bytes of

@@ -6,7 +6,7 @@ tensors); nothing is computed in Python.  There is no fallback for the
 kernels: if the library is missing, loading raises.
 
 All entry points have the parameters of their C counterparts, plus ``stream=None, check=True`` where they launch.  Those of a model's
-forward pass (``NATIVE`` and, on the paged key/value cache, ``CACHE_CALLS``) are functions of the extension module ``_fqcall`` (csrc/fq_python.cpp), which calls the library that
+forward pass (``NATIVE``, on the paged key/value cache ``CACHE_CALLS`` and around it ``STEP_CALLS``) are functions of the extension module ``_fqcall`` (csrc/fq_python.cpp), which calls the library that
 ``lib()`` has loaded.  The module is compiled for one interpreter; under another one, or where it has not been built, the same functions
 call through ctypes like the rest (2.6 us of host time for a product's arguments instead of 0.5).
 """
@@ -30,6 +30,7 @@ EXPORTS = (
     "fq_supported", "fq_choose_factors", "fq_default_design_fits", "fq_lds_bytes",
     "fq_status_string", "fq_last_hip_error", "fq_abi_version", "fq_set_tuning",
     "flatquant_cache_write", "flatquant_cache_read", "flatquant_cache_attention", "flatquant_cache_tree_attention", "fq_cache_attention_workspace",
+    "flatquant_cache_advance", "flatquant_head_rope", "fq_rope_turns", "flatquant_cache_scored_attention",
 )
 
 # parameters of the launching entry points without the stream, and their C types: pointer, int, long (int64_t), float
@@ -56,7 +57,17 @@ _CACHE_PARAMS = {
     "flatquant_cache_tree_attention": ("cache batch q q_stride Hq scale visible out out_stride workspace workspace_bytes", "ppplifpplpl"),
 }
 CACHE_CALLS = tuple(_CACHE_PARAMS)
-_PARAMS = {**_NATIVE_PARAMS, **_CACHE_PARAMS}
+
+# a step around it: `pool` is a PagePool
+_STEP_PARAMS = {
+    "flatquant_cache_advance": ("batch pool page_tokens pages held keep rows positions slots", "ppilppppp"),
+    "flatquant_head_rope": ("q q_stride Hq k k_stride H T positions turns rotary interleaved w_q w_k eps P_q P_k per_head q_out q_out_stride k_out k_out_stride",
+                            "pliplilppiippfppiplpl"),
+    "flatquant_cache_scored_attention": ("cache batch q q_stride Hq scale cap slopes prefix window sinks visible out out_stride workspace workspace_bytes",
+                                         "pppliffppiipplpl"),
+}
+STEP_CALLS = tuple(_STEP_PARAMS)
+_PARAMS = {**_NATIVE_PARAMS, **_CACHE_PARAMS, **_STEP_PARAMS}
 
 _lib = None
 _fqcall = None
@@ -83,6 +94,8 @@ def lib() -> ctypes.CDLL:
             getattr(L, name).restype = i32
         L.fq_cache_attention_workspace.argtypes = [vp, vp, i32]
         L.fq_cache_attention_workspace.restype = i64
+        L.fq_rope_turns.argtypes = [vp, i32, vp]
+        L.fq_rope_turns.restype = i32
         L.fq_mxfp4_tiled_scale_bytes.argtypes = [i64, i64]
         L.fq_mxfp4_tiled_scale_bytes.restype = i64
         L.flatquant_dequant_mxfp4.argtypes = [vp, vp, i64, i32, vp, vp]
@@ -195,6 +208,16 @@ class KvBatch(_HostStruct):
                          table_stride=table_stride, max_rows=max_rows, max_length=max_length)
 
 
+class PagePool(_HostStruct):
+    """fq_page_pool: the ring of free pages (i32 [capacity]), its state (i64 [2]) and what it becomes (i64 [3]; may be the state, of three numbers then)."""
+
+    class _Fields(ctypes.Structure):
+        _fields_ = [("ring", ctypes.c_void_p), ("state", ctypes.c_void_p), ("next", ctypes.c_void_p), ("capacity", ctypes.c_int64)]
+
+    def __init__(self, ring, state, next, capacity: int):
+        super().__init__(ring=ring, state=state, next=next, capacity=capacity)
+
+
 def fq_cache_attention_workspace(cache, batch, Hq: int) -> int:
     """Bytes of workspace of the attention calls; raises for arguments that they refuse."""
     n = int(lib().fq_cache_attention_workspace(_ptr(cache), _ptr(batch), int(Hq)))
@@ -250,6 +273,19 @@ def fq_inverse_transpose(P):
     if st != FQ_OK:
         raise FlatQuantError(st, "fq_inverse_transpose")
     return out, res.value
+
+
+def fq_rope_turns(frequencies):
+    """Host helper of flatquant_head_rope: float64 [n] radians a position -> uint64 [n], the angle that a position adds in units of 2^-64 of a turn."""
+    import numpy as np
+    f = np.ascontiguousarray(frequencies, dtype=np.float64)
+    if f.ndim != 1:
+        raise ValueError("fq_rope_turns expects a vector")
+    turns = np.empty(f.shape, dtype=np.uint64)
+    st = lib().fq_rope_turns(f.ctypes.data, len(f), turns.ctypes.data)
+    if st != FQ_OK:
+        raise FlatQuantError(st, "fq_rope_turns")
+    return turns
 
 
 def flatquant_stream_probe(x, T: int, n: int, x_stride: int, out, stream=None, check: bool = True) -> int:

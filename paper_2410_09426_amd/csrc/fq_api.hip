@@ -351,9 +351,101 @@ fq_status flatquant_cache_read(const fq_kv_cache* cache, const fq_kv_batch* batc
     return fq::finish(fq::cache_read_launch(d, r, static_cast<hipStream_t>(stream)));
 }
 
+namespace {
+struct Bytes {                // of an argument; null: left out
+    const void* p;
+    int64_t n;
+};
+bool meet(const Bytes& a, const Bytes& b) { return a.p && b.p && a.n > 0 && b.n > 0 && fq::overlap(a.p, a.n, b.p, b.n); }
+bool off(const void* p, int align) { return (reinterpret_cast<uintptr_t>(p) & (align - 1)) != 0; }
+}  // namespace
+
+fq_status flatquant_cache_advance(const fq_kv_batch* batch, const fq_page_pool* pool, int page_tokens, int64_t pages, const int32_t* held,
+                                  const int32_t* keep, const int32_t* rows, int32_t* positions, int64_t* slots, void* stream) {
+    if (!batch || !pool || page_tokens < 1 || pages < 1 || pool->capacity < 1) return FQ_INVALID_ARG;
+    if (batch->B < 0 || batch->T < 0 || batch->table_width < 0 || batch->table_stride < batch->table_width) return FQ_INVALID_ARG;
+    if (page_tokens < 16 || page_tokens > 1024 || (page_tokens & (page_tokens - 1)) || pages > 0x7fffffffLL || pool->capacity > 0x7fffffffLL) return FQ_UNSUPPORTED_SHAPE;
+    if (batch->T > (1LL << 29) || batch->B > 0xffffff || batch->table_width > (1 << 20) || batch->table_width > 0x7fff0000LL / page_tokens ||
+        (batch->B > 1 && batch->table_stride > (1LL << 48) / batch->B))
+        return FQ_UNSUPPORTED_SHAPE;
+    if (batch->B == 0) return FQ_OK;
+    if (!batch->row_starts || !batch->lengths || (!batch->page_table && batch->table_width > 0) || !pool->ring || !pool->state || !pool->next || !held ||
+        !keep || !rows)
+        return FQ_INVALID_ARG;
+    if (off(batch->row_starts, 4) || off(batch->lengths, 4) || off(batch->page_table, 4) || off(pool->ring, 4) || off(pool->state, 8) || off(pool->next, 8) ||
+        off(held, 4) || off(keep, 4) || off(rows, 4) || off(positions, 4) || off(slots, 8))
+        return FQ_MISALIGNED;
+    const int64_t B = batch->B, table = batch->table_width > 0 ? ((B - 1) * batch->table_stride + batch->table_width) * 4 : 0;
+    const Bytes written[] = {{batch->row_starts, (B + 1) * 4}, {batch->lengths, B * 4}, {batch->page_table, table}, {pool->ring, pool->capacity * 4},
+                             {pool->next, 24}, {positions, batch->T * 4}, {slots, batch->T * 8}};
+    const Bytes read[] = {{held, B * 4}, {keep, B * 4}, {rows, B * 4}, {pool->state, 16}};
+    for (const Bytes& a : written) {
+        for (const Bytes& b : written)
+            if (&a != &b && meet(a, b)) return FQ_INVALID_ARG;
+        for (const Bytes& b : read) {
+            const bool in_place = (a.p == batch->lengths && (b.p == held || b.p == keep) && a.p == b.p) || (a.p == pool->next && b.p == pool->state && a.p == b.p);
+            if (!in_place && meet(a, b)) return FQ_INVALID_ARG;
+        }
+    }
+    fq::AdvanceDev a;
+    a.held = held; a.keep = keep; a.rows = rows;
+    a.row_starts = const_cast<int32_t*>(batch->row_starts); a.lengths = const_cast<int32_t*>(batch->lengths);
+    a.page_table = const_cast<int32_t*>(batch->page_table);
+    a.ring = pool->ring; a.state = pool->state; a.next = pool->next; a.positions = positions; a.slots = slots;
+    a.table_stride = batch->table_stride; a.T = batch->T; a.capacity = pool->capacity;
+    a.B = (int)B; a.pages = (int)pages; a.table_width = (int)batch->table_width; a.page_shift = __builtin_ctz((unsigned)page_tokens);
+    return fq::finish(fq::advance_launch(a, static_cast<hipStream_t>(stream)));
+}
+
+fq_status flatquant_head_rope(const void* q, int64_t q_stride, int Hq, const void* k, int64_t k_stride, int H, int64_t T, const int32_t* positions,
+                              const uint64_t* turns, int rotary, int interleaved, const void* w_q, const void* w_k, float eps,
+                              const void* P_q, const void* P_k, int per_head, void* q_out, int64_t q_out_stride, void* k_out, int64_t k_out_stride,
+                              void* stream) {
+    if (T < 0 || rotary < 0 || (interleaved != 0 && interleaved != 1) || (per_head != 0 && per_head != 1)) return FQ_INVALID_ARG;
+    if (rotary > 128 || rotary % 32 != 0 || T > (1LL << 29)) return FQ_UNSUPPORTED_SHAPE;
+    fq::RopeDev d;
+    const void *in[2] = {q, k}, *w[2] = {w_q, w_k}, *P[2] = {P_q, P_k};
+    void* out[2] = {q_out, k_out};
+    const int64_t stride[2] = {q_stride, k_stride}, to_stride[2] = {q_out_stride, k_out_stride};
+    const int heads[2] = {Hq, H};
+    Bytes read[8], written[2];
+    int reads = 0;
+    bool any = false;
+    for (int x = 0; x < 2; ++x) {
+        d.rows[x] = static_cast<const _Float16*>(in[x]); d.out[x] = static_cast<_Float16*>(out[x]);
+        d.w[x] = static_cast<const _Float16*>(w[x]); d.P[x] = static_cast<const _Float16*>(P[x]);
+        d.stride[x] = stride[x]; d.out_stride[x] = to_stride[x]; d.heads[x] = heads[x];
+        written[x] = Bytes{nullptr, 0};
+        if (!in[x]) continue;
+        const int64_t row = 128LL * heads[x];
+        if (heads[x] < 1 || stride[x] < row || to_stride[x] < row || (w[x] && !(eps > 0.0f && std::isfinite(eps)))) return FQ_INVALID_ARG;
+        if (heads[x] > (per_head ? 32767 : 65535) || T > 0x7fffff00LL / heads[x]) return FQ_UNSUPPORTED_SHAPE;
+        const int64_t most = T > 256 ? (1LL << 48) / T : 1LL << 40;
+        if (stride[x] > most || to_stride[x] > most) return FQ_UNSUPPORTED_SHAPE;
+        if (!out[x] && T > 0) return FQ_INVALID_ARG;
+        if (off(in[x], 16) || off(out[x], 16) || off(w[x], 16) || off(P[x], 16) || (stride[x] & 7) || (to_stride[x] & 7)) return FQ_MISALIGNED;
+        read[reads++] = Bytes{in[x], ((T - 1) * stride[x] + row) * 2};
+        read[reads++] = Bytes{w[x], 256};
+        read[reads++] = Bytes{P[x], 32768LL * (per_head ? heads[x] : 1)};
+        written[x] = Bytes{out[x], ((T - 1) * to_stride[x] + row) * 2};
+        any = true;
+    }
+    if (T == 0 || !any) return FQ_OK;
+    if (!positions || (rotary > 0 && !turns)) return FQ_INVALID_ARG;
+    if (off(positions, 4) || off(turns, 16)) return FQ_MISALIGNED;
+    read[reads++] = Bytes{positions, T * 4};
+    read[reads++] = Bytes{turns, rotary * 4LL};
+    if (meet(written[0], written[1])) return FQ_INVALID_ARG;
+    for (const Bytes& a : written)
+        for (int r = 0; r < reads; ++r)
+            if (meet(a, read[r])) return FQ_INVALID_ARG;
+    d.positions = positions; d.turns = turns; d.T = T; d.rotary = rotary; d.interleaved = interleaved; d.per_head = per_head; d.eps = eps;
+    return fq::finish(fq::rope_launch(d, static_cast<hipStream_t>(stream)));
+}
+
 static fq_status cache_attention(const fq_kv_cache* cache, const fq_kv_batch* batch, const void* q, int64_t q_stride, int Hq, float scale,
-                                 int window, int sinks, const uint64_t* visible, bool tree, void* out, int64_t out_stride, void* workspace,
-                                 int64_t workspace_bytes, void* stream) {
+                                 int window, int sinks, const uint64_t* visible, bool tree, const fq::ScoreArgs* scores, void* out, int64_t out_stride,
+                                 void* workspace, int64_t workspace_bytes, void* stream) {
     fq::CacheDev d;
     bool empty;
     fq_status st = cache_args(cache, batch, d, empty);
@@ -384,18 +476,38 @@ static fq_status cache_attention(const fq_kv_cache* cache, const fq_kv_batch* ba
     a.q = static_cast<const _Float16*>(q); a.out = static_cast<_Float16*>(out); a.q_stride = q_stride; a.out_stride = out_stride;
     a.Hq = Hq; a.scale = scale; a.window = window; a.sinks = sinks; a.visible = visible; a.workspace = static_cast<float*>(workspace);
     a.max_rows = max_rows;
+    if (scores) return fq::finish(fq::scored_attention_launch(d, a, *scores, plan, static_cast<hipStream_t>(stream)));
     return fq::finish(fq::attention_launch(d, a, plan, static_cast<hipStream_t>(stream)));
 }
 
 fq_status flatquant_cache_attention(const fq_kv_cache* cache, const fq_kv_batch* batch, const void* q, int64_t q_stride, int Hq, float scale,
                                     int window, int sinks, void* out, int64_t out_stride, void* workspace, int64_t workspace_bytes, void* stream) {
-    return cache_attention(cache, batch, q, q_stride, Hq, scale, window, sinks, nullptr, false, out, out_stride, workspace, workspace_bytes, stream);
+    return cache_attention(cache, batch, q, q_stride, Hq, scale, window, sinks, nullptr, false, nullptr, out, out_stride, workspace, workspace_bytes, stream);
 }
 
 fq_status flatquant_cache_tree_attention(const fq_kv_cache* cache, const fq_kv_batch* batch, const void* q, int64_t q_stride, int Hq, float scale,
                                          const uint64_t* visible, void* out, int64_t out_stride, void* workspace, int64_t workspace_bytes,
                                          void* stream) {
-    return cache_attention(cache, batch, q, q_stride, Hq, scale, 0, 0, visible, true, out, out_stride, workspace, workspace_bytes, stream);
+    return cache_attention(cache, batch, q, q_stride, Hq, scale, 0, 0, visible, true, nullptr, out, out_stride, workspace, workspace_bytes, stream);
+}
+
+fq_status flatquant_cache_scored_attention(const fq_kv_cache* cache, const fq_kv_batch* batch, const void* q, int64_t q_stride, int Hq, float scale,
+                                           float cap, const float* slopes, const int32_t* prefix, int window, int sinks, const uint64_t* visible,
+                                           void* out, int64_t out_stride, void* workspace, int64_t workspace_bytes, void* stream) {
+    if (!(cap >= 0.0f) || !std::isfinite(cap) || (visible && (slopes || prefix || window != 0 || sinks != 0))) return FQ_INVALID_ARG;
+    if (off(slopes, 4) || off(prefix, 4)) return FQ_MISALIGNED;
+    if (batch && batch->B > 0 && batch->T > 0 && Hq > 0 && Hq <= (1 << 24) && batch->T <= 0x7fffff00LL / Hq && batch->B <= 0xffffff && out) {
+        const Bytes read[] = {{slopes, Hq * 4LL}, {prefix, batch->B * 4}};
+        const int64_t row = 128LL * Hq, most = (1LL << 48) / batch->T;
+        const Bytes written[] = {{out, out_stride >= row && out_stride <= most ? ((batch->T - 1) * out_stride + row) * 2 : 0},
+                                 {workspace, workspace_bytes > 0 ? workspace_bytes : 0}};
+        for (const Bytes& a : written)
+            for (const Bytes& b : read)
+                if (meet(a, b)) return FQ_INVALID_ARG;
+    }
+    const fq::ScoreArgs scores{cap, slopes, prefix};
+    return cache_attention(cache, batch, q, q_stride, Hq, scale, window, sinks, visible, visible != nullptr, &scores, out, out_stride, workspace,
+                           workspace_bytes, stream);
 }
 
 int64_t fq_cache_attention_workspace(const fq_kv_cache* cache, const fq_kv_batch* batch, int Hq) {
@@ -505,6 +617,20 @@ fq_status fq_inverse_transpose(const void* P, int n, void* out, double* max_resi
                 worst = std::fmax(worst, std::fabs(acc - (i == j ? 1.0 : 0.0)));
             }
         *max_residual = worst;
+    }
+    return FQ_OK;
+}
+
+fq_status fq_rope_turns(const double* frequencies, int n, uint64_t* turns) {
+    if (!frequencies || !turns || n < 0) return FQ_INVALID_ARG;
+    for (int i = 0; i < n; ++i)
+        if (!std::isfinite(frequencies[i])) return FQ_INVALID_ARG;
+    for (int i = 0; i < n; ++i) {
+        const long double pi2 = 6.283185307179586476925286766559005768L;
+        long double turn = fmodl((long double)frequencies[i], pi2) / pi2;      // (64 bits of fraction)
+        if (turn < 0) turn += 1.0L;
+        const long double whole = rintl(turn * 0x1p64L);
+        turns[i] = whole >= 0x1p64L ? 0 : (uint64_t)whole;
     }
     return FQ_OK;
 }

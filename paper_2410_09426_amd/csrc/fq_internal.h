@@ -168,6 +168,40 @@ struct CacheRows {            // row tensors of a write or a read; a null pointe
 hipError_t cache_write_launch(const CacheDev& c, const CacheRows& r, hipStream_t stream);
 hipError_t cache_read_launch(const CacheDev& c, const CacheRows& r, hipStream_t stream);
 hipError_t kv_paged_launch(const CacheDev& c, const CacheRows& r, int x, hipStream_t stream);
+// The tables of a step (fq_advance.hip; flatquant.h says what the fields are).
+struct AdvanceDev {
+    const int32_t* held;
+    const int32_t* keep;
+    const int32_t* rows;
+    int32_t* row_starts;
+    int32_t* lengths;
+    int32_t* page_table;
+    int32_t* ring;
+    const int64_t* state;     // pages taken from the ring so far, pages put into it
+    int64_t* next;            // the same behind the call, and how many were missing
+    int32_t* positions;
+    int64_t* slots;
+    int64_t table_stride, T, capacity;
+    int32_t B, pages, table_width, page_shift;
+};
+hipError_t advance_launch(const AdvanceDev& a, hipStream_t stream);
+
+// Norm, rotation and matrix of queries (0) and keys (1), head by head (fq_rope.hip; flatquant.h says what the fields are).
+struct RopeDev {
+    const _Float16* rows[2];  // null: not there
+    _Float16* out[2];
+    int64_t stride[2], out_stride[2];
+    const _Float16* w[2];     // null: no norm
+    const _Float16* P[2];     // null: no matrix
+    const int32_t* positions;
+    const uint64_t* turns;
+    int64_t T;
+    int32_t heads[2];
+    int32_t rotary, interleaved, per_head;
+    float eps;
+};
+hipError_t rope_launch(const RopeDev& d, hipStream_t stream);
+
 struct AttnArgs {
     const _Float16* q;
     _Float16* out;
@@ -188,6 +222,12 @@ struct AttnPlan {
 };
 AttnPlan attention_plan(int64_t B, int64_t T, int H, int Hq, int64_t max_rows, int64_t length, int64_t seen);
 hipError_t attention_launch(const CacheDev& c, const AttnArgs& a, const AttnPlan& plan, hipStream_t stream);
+struct ScoreArgs {
+    float cap;                // 0: none
+    const float* slopes;      // null: none
+    const int32_t* prefix;    // null: none
+};
+hipError_t scored_attention_launch(const CacheDev& c, const AttnArgs& a, const ScoreArgs& s, const AttnPlan& plan, hipStream_t stream);
 
 hipError_t dequant_mxfp4_launch(const uint8_t* codes, const uint8_t* exps, int64_t rows, int n, float* out, hipStream_t stream);
 hipError_t dequant_bits_launch(const uint8_t* codes, const _Float16* scales, const _Float16* zeros,

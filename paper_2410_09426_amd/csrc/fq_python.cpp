@@ -17,7 +17,7 @@
 
 namespace {
 
-enum Entry { TRANSFORM, MX, MX_TILED, WEIGHT, W4A4, MX_GEMM, KV, KV_BITS, HEAD, CACHE_WRITE, CACHE_READ, CACHE_ATTENTION, CACHE_TREE, COUNT };
+enum Entry { TRANSFORM, MX, MX_TILED, WEIGHT, W4A4, MX_GEMM, KV, KV_BITS, HEAD, CACHE_WRITE, CACHE_READ, CACHE_ATTENTION, CACHE_TREE, CACHE_ADVANCE, HEAD_ROPE, CACHE_SCORED, COUNT };
 void* g_entry[COUNT];                 // addresses in the loaded library; null until then
 PyObject* g_error = nullptr;          // binding.FlatQuantError(status, where)
 PyObject* g_load = nullptr;           // binding.lib: loads the library and binds its addresses, or raises
@@ -76,7 +76,7 @@ struct Reader {                       // reads arguments in order; after a failu
     }
 };
 
-constexpr int kMaxArgs = 16;
+constexpr int kMaxArgs = 24;
 
 // Positional and keyword arguments into out[0 .. n - 1] by the names of a signature whose last two are optional: stream, check.
 struct Signature {
@@ -211,7 +211,14 @@ Signature kCacheAttention{CACHE_ATTENTION, "flatquant_cache_attention",
                           {"cache", "batch", "q", "q_stride", "Hq", "scale", "window", "sinks", "out", "out_stride", "workspace", "workspace_bytes", "stream", "check"}};
 Signature kCacheTree{CACHE_TREE, "flatquant_cache_tree_attention",
                      {"cache", "batch", "q", "q_stride", "Hq", "scale", "visible", "out", "out_stride", "workspace", "workspace_bytes", "stream", "check"}};
-Signature* const kAll[COUNT] = {&kTransform, &kMx, &kMxTiled, &kWeight, &kW4a4, &kMxGemm, &kKv, &kKvBits, &kHead, &kCacheWrite, &kCacheRead, &kCacheAttention, &kCacheTree};
+Signature kCacheAdvance{CACHE_ADVANCE, "flatquant_cache_advance", {"batch", "pool", "page_tokens", "pages", "held", "keep", "rows", "positions", "slots", "stream", "check"}};
+Signature kHeadRope{HEAD_ROPE, "flatquant_head_rope",
+                    {"q", "q_stride", "Hq", "k", "k_stride", "H", "T", "positions", "turns", "rotary", "interleaved", "w_q", "w_k", "eps", "P_q", "P_k", "per_head",
+                     "q_out", "q_out_stride", "k_out", "k_out_stride", "stream", "check"}};
+Signature kCacheScored{CACHE_SCORED, "flatquant_cache_scored_attention",
+                       {"cache", "batch", "q", "q_stride", "Hq", "scale", "cap", "slopes", "prefix", "window", "sinks", "visible", "out", "out_stride", "workspace",
+                        "workspace_bytes", "stream", "check"}};
+Signature* const kAll[COUNT] = {&kTransform, &kMx, &kMxTiled, &kWeight, &kW4a4, &kMxGemm, &kKv, &kKvBits, &kHead, &kCacheWrite, &kCacheRead, &kCacheAttention, &kCacheTree, &kCacheAdvance, &kHeadRope, &kCacheScored};
 
 #define ARGS PyObject*, PyObject *const *a, Py_ssize_t n, PyObject *kw
 #define TYPE(entry) decltype(&entry)
@@ -332,6 +339,81 @@ PyObject* cache_attention(const Signature& s, PyObject* const* args, Py_ssize_t 
 }
 PyObject* py_cache_attention(ARGS) { return cache_attention<false>(kCacheAttention, a, n, kw); }
 PyObject* py_cache_tree(ARGS) { return cache_attention<true>(kCacheTree, a, n, kw); }
+// a step around the cache
+PyObject* py_cache_advance(ARGS) {
+    PyObject* v[kMaxArgs];
+    TYPE(flatquant_cache_advance) fn;
+    if (!collect(kCacheAdvance, a, n, kw, v)) return nullptr;
+    Reader r{v};
+    const void *batch = r.ptr(), *pool = r.ptr();
+    const int page_tokens = r.i32();
+    const int64_t pages = r.i64();
+    const void *held = r.ptr(), *keep = r.ptr(), *rows = r.ptr();
+    void *positions = r.ptr(), *slots = r.ptr(), *stream = r.stream();
+    if (!r.ok || !entry(kCacheAdvance.entry, fn)) return nullptr;
+    fq_status st;
+    Py_BEGIN_ALLOW_THREADS
+    st = fn((const fq_kv_batch*)batch, (const fq_page_pool*)pool, page_tokens, pages, (const int32_t*)held, (const int32_t*)keep, (const int32_t*)rows,
+            (int32_t*)positions, (int64_t*)slots, stream);
+    Py_END_ALLOW_THREADS
+    return finish(kCacheAdvance, st, v[kCacheAdvance.n - 1]);
+}
+PyObject* py_head_rope(ARGS) {
+    PyObject* v[kMaxArgs];
+    TYPE(flatquant_head_rope) fn;
+    if (!collect(kHeadRope, a, n, kw, v)) return nullptr;
+    Reader r{v};
+    const void* q = r.ptr();
+    const int64_t q_stride = r.i64();
+    const int Hq = r.i32();
+    const void* k = r.ptr();
+    const int64_t k_stride = r.i64();
+    const int H = r.i32();
+    const int64_t T = r.i64();
+    const void *positions = r.ptr(), *turns = r.ptr();
+    const int rotary = r.i32(), interleaved = r.i32();
+    const void *w_q = r.ptr(), *w_k = r.ptr();
+    const float eps = r.f32();
+    const void *P_q = r.ptr(), *P_k = r.ptr();
+    const int per_head = r.i32();
+    void* q_out = r.ptr();
+    const int64_t q_out_stride = r.i64();
+    void* k_out = r.ptr();
+    const int64_t k_out_stride = r.i64();
+    void* stream = r.stream();
+    if (!r.ok || !entry(kHeadRope.entry, fn)) return nullptr;
+    fq_status st;
+    Py_BEGIN_ALLOW_THREADS
+    st = fn(q, q_stride, Hq, k, k_stride, H, T, (const int32_t*)positions, (const uint64_t*)turns, rotary, interleaved, w_q, w_k, eps, P_q, P_k, per_head,
+            q_out, q_out_stride, k_out, k_out_stride, stream);
+    Py_END_ALLOW_THREADS
+    return finish(kHeadRope, st, v[kHeadRope.n - 1]);
+}
+PyObject* py_cache_scored(ARGS) {
+    PyObject* v[kMaxArgs];
+    TYPE(flatquant_cache_scored_attention) fn;
+    if (!collect(kCacheScored, a, n, kw, v)) return nullptr;
+    Reader r{v};
+    const void *cache = r.ptr(), *batch = r.ptr(), *q = r.ptr();
+    const int64_t q_stride = r.i64();
+    const int Hq = r.i32();
+    const float scale = r.f32(), cap = r.f32();
+    const void *slopes = r.ptr(), *prefix = r.ptr();
+    const int window = r.i32(), sinks = r.i32();
+    const void* visible = r.ptr();
+    void* out = r.ptr();
+    const int64_t out_stride = r.i64();
+    void* workspace = r.ptr();
+    const int64_t bytes = r.i64();
+    void* stream = r.stream();
+    if (!r.ok || !entry(kCacheScored.entry, fn)) return nullptr;
+    fq_status st;
+    Py_BEGIN_ALLOW_THREADS
+    st = fn((const fq_kv_cache*)cache, (const fq_kv_batch*)batch, q, q_stride, Hq, scale, cap, (const float*)slopes, (const int32_t*)prefix, window, sinks,
+            (const uint64_t*)visible, out, out_stride, workspace, bytes, stream);
+    Py_END_ALLOW_THREADS
+    return finish(kCacheScored, st, v[kCacheScored.n - 1]);
+}
 // connect(load, error): `load` is called when an entry point is needed whose address is not known; `error` is what is raised
 PyObject* py_connect(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (n != 2) {
@@ -380,6 +462,9 @@ PyMethodDef kMethods[] = {
     FN("flatquant_cache_read", py_cache_read, "(cache, batch, k, k_stride, v, v_stride, stream=None, check=True)"),
     FN("flatquant_cache_attention", py_cache_attention, "(cache, batch, q, q_stride, Hq, scale, window, sinks, out, out_stride, workspace, workspace_bytes, stream=None, check=True)"),
     FN("flatquant_cache_tree_attention", py_cache_tree, "(cache, batch, q, q_stride, Hq, scale, visible, out, out_stride, workspace, workspace_bytes, stream=None, check=True)"),
+    FN("flatquant_cache_advance", py_cache_advance, "(batch, pool, page_tokens, pages, held, keep, rows, positions, slots, stream=None, check=True)"),
+    FN("flatquant_head_rope", py_head_rope, "(q, q_stride, Hq, k, k_stride, H, T, positions, turns, rotary, interleaved, w_q, w_k, eps, P_q, P_k, per_head, q_out, q_out_stride, k_out, k_out_stride, stream=None, check=True)"),
+    FN("flatquant_cache_scored_attention", py_cache_scored, "(cache, batch, q, q_stride, Hq, scale, cap, slopes, prefix, window, sinks, visible, out, out_stride, workspace, workspace_bytes, stream=None, check=True)"),
     {"connect", (PyCFunction)(void (*)(void))py_connect, METH_FASTCALL, nullptr},
     {"bind", py_bind, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};

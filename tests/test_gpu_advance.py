@@ -1,0 +1,223 @@
+"""The tables of a step (flatquant_cache_advance) against the oracle's loops: every number equal, nothing else written."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import step_oracle as so
+from paper_2410_09426_amd import binding as fq
+
+pytestmark = pytest.mark.gpu
+GUARD = 64
+
+
+def _i32(a):
+    return torch.from_numpy(np.ascontiguousarray(a, dtype=np.int32)).cuda()
+
+
+class Step:
+    """Sequences' figures, a table with pages in an order of their own, and a ring that has gone round before; the ring and rows sit between guards."""
+
+    def __init__(self, seed, held, keep, rows, page=16, T=None, width=None, stride_pad=3, spare=5, taken=None, holes=0.0):
+        r = np.random.Generator(np.random.PCG64(seed))
+        self.held, self.keep, self.rows, self.page = [list(map(int, x)) for x in (held, keep, rows)] + [page]
+        self.B = len(held)
+        total = sum(max(0, n) for n in rows)
+        self.T = total + 3 if T is None else T
+        cut = [min(max(0, k), max(0, h)) for h, k in zip(held, keep)]
+        most = max([1] + [-(-x // page) for x in held] + [-(-(k + max(0, n)) // page) for k, n in zip(cut, rows)])
+        self.width = most if width is None else width
+        have = [min(-(-max(0, h) // page), self.width) for h in held]
+        need = [min(-(-(k + max(0, n)) // page), self.width) for k, n in zip(cut, rows)]
+        want = sum(max(0, n - h) for n, h in zip(need, have))
+        self.pages = sum(have) + max(1, want + spare)
+        order = r.permutation(self.pages).astype(np.int32)
+        self.table = np.full((self.B, self.width + stride_pad), -7, dtype=np.int32)
+        at = 0
+        for b, n in enumerate(have):
+            self.table[b, :n] = order[at:at + n]
+            for j in np.flatnonzero(r.random(n) < holes):        # entries that are no page, in kinds
+                self.table[b, j] = (-1, self.pages, -2 ** 31, 2 ** 31 - 1)[(b + j) % 4]
+            at += n
+        self.taken = int(r.integers(0, 10 * self.pages)) if taken is None else taken
+        free = order[at:]
+        self.given = self.taken + len(free)
+        self.ring = np.full(self.pages, -3, dtype=np.int32)
+        for i, p in enumerate(free):
+            self.ring[(self.taken + i) % self.pages] = p
+
+    def expect(self):
+        table = [list(map(int, row)) for row in self.table]
+        ring = list(map(int, self.ring))
+        return so.advance(self.held, self.keep, self.rows, table, self.width, self.page, self.pages, ring, self.taken, self.given, self.T) + (table, ring)
+
+    def run(self, in_place=False, maps="ps", stream=None):
+        st = stream or torch.cuda.current_stream()
+        big = lambda n, t: torch.full((GUARD + n + GUARD,), -99, dtype=t, device="cuda")      # noqa: E731
+        starts, lengths, ring = big(self.B + 1, torch.int32), big(self.B, torch.int32), big(self.pages, torch.int32)
+        positions, slots, nxt = big(self.T, torch.int32), big(self.T, torch.int64), big(3, torch.int64)
+        view = lambda x: x[GUARD:-GUARD]                                                      # noqa: E731
+        view(ring).copy_(_i32(self.ring))
+        table, held, keep, rows = _i32(self.table), _i32(self.held), _i32(self.keep), _i32(self.rows)
+        state = torch.tensor([self.taken, self.given], device="cuda")
+        if in_place:
+            view(lengths).copy_(held)
+            view(nxt)[:2].copy_(state)
+            held, state = view(lengths), view(nxt)
+            if self.keep == self.held:
+                keep = held
+        batch = fq.KvBatch(view(starts), view(lengths), table, self.B, self.T, self.width, self.table.shape[1], 1, 1)
+        pool = fq.PagePool(view(ring), state, view(nxt), self.pages)
+        fq.flatquant_cache_advance(batch, pool, self.page, self.pages, held, keep, rows, view(positions) if "p" in maps else None,
+                                   view(slots) if "s" in maps else None, stream=st)
+        torch.cuda.synchronize()
+        for x in (starts, lengths, ring, positions, slots, nxt):
+            assert bool((x[:GUARD] == -99).all()) and bool((x[-GUARD:] == -99).all()), "written beside an output"
+        return [view(x).tolist() for x in (starts, lengths, nxt, positions, slots)] + [table.tolist(), view(ring).tolist()]
+
+    def check(self, **how):
+        maps = how.get("maps", "ps")
+        got, want = self.run(**how), list(self.expect())
+        want[2] = list(want[2])
+        if "p" not in maps:
+            want[3] = [-99] * self.T
+        if "s" not in maps:
+            want[4] = [-99] * self.T
+        for name, g, w in zip(("row_starts", "lengths", "next", "positions", "slots", "table", "ring"), got, want):
+            assert g == w, (name, [(i, a, b) for i, (a, b) in enumerate(zip(g, w)) if a != b][:5])
+
+
+def _mixed(seed, B, most=3000, chunk=200):
+    r = np.random.Generator(np.random.PCG64(seed))
+    held = r.integers(0, most, B)
+    keep, rows = held.copy(), np.ones(B, dtype=int)
+    what = r.integers(0, 6, B)
+    keep[what == 0], rows[what == 0] = 0, 0                                    # has ended
+    keep[what == 1] -= np.minimum(held[what == 1], r.integers(0, 60, (what == 1).sum()))      # drafted tokens given up
+    rows[what == 2] = r.integers(0, chunk, (what == 2).sum())                  # a chunk of a prompt
+    keep[what == 3], rows[what == 3] = 0, r.integers(0, chunk, (what == 3).sum())             # a new sequence in its place
+    rows[what == 4] = 0
+    return held, keep, rows
+
+
+@pytest.mark.parametrize("B", [1, 2, 63, 64, 65, 1000, 1024, 1025, 2500])
+@pytest.mark.parametrize("page", [16, 64])
+def test_mixed_steps(B, page):
+    print(f"[case] mixed B={B} page={page}", flush=True)
+    Step(B, *_mixed(B + page, B, chunk=200 if B < 500 else 12), page=page).check()
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("page,length", [(16, 15), (16, 16), (16, 17), (64, 4096), (1024, 1023), (1024, 1024)])
+def test_decode_at_page_borders(page, length, in_place):
+    print(f"[case] decode page={page} length={length}", flush=True)
+    held = [length, length + 1, length - 1, 0, 5]
+    Step(7, held, held, [1] * 5, page=page).check(in_place=in_place)
+
+
+@pytest.mark.parametrize("T", [0, 1, 100, 4096, 4097, 20000])
+def test_rows_that_do_not_fit_are_cut(T):
+    print(f"[case] cut T={T}", flush=True)
+    held = [40, 0, 16, 100, 3]
+    Step(9, held, held, [300, 0, 9000, 700, 1], T=T).check()
+    Step(10, held, [40, 0, 0, 2, 0], [0, 0, 0, 0, 0], T=T).check()             # only gives pages back
+
+
+@pytest.mark.parametrize("B", [3, 1500])
+def test_long_prompts_and_many_pages(B):
+    print(f"[case] long B={B}", flush=True)
+    rows = [30000, 0, 12345] if B == 3 else [3] * 700 + [20000] + [2] * (B - 701)
+    Step(11, [0] * B, [0] * B, rows).check()
+    Step(12, rows, [0] * B, [0] * (B - 1) + [5]).check()                       # and back
+
+
+@pytest.mark.parametrize("maps", ["", "p", "s"])
+@pytest.mark.parametrize("rows", [5, 3000])
+def test_maps_that_are_left_out(maps, rows):
+    print(f"[case] maps={maps} rows={rows}", flush=True)
+    Step(13, [10, 20], [10, 18], [rows, 2 * rows]).check(maps=maps)
+
+
+def test_entries_that_are_no_page():
+    print("[case] holes", flush=True)
+    Step(14, *_mixed(14, 200), holes=0.3).check()
+
+
+def test_tables_that_are_too_narrow():
+    """Tokens behind the table's width have no page, and nothing is taken or given back for them."""
+    print("[case] narrow", flush=True)
+    Step(15, [100, 30, 0, 64], [100, 30, 0, 10], [100, 1, 500, 0], width=4).check()
+    Step(16, [100, 30], [100, 30], [4, 1], width=0).check()
+
+
+def test_numbers_out_of_range():
+    """Negative counts, more kept than held, lengths beyond 32 bits."""
+    print("[case] out of range", flush=True)
+    Step(17, [-5, 40, 33, 2 ** 31 - 1, 2 ** 31 - 3], [7, 90, -4, 2 ** 31 - 1, 2 ** 31 - 3], [3, -2, -2 ** 31, 9, 9], width=5).check()
+
+
+@pytest.mark.parametrize("B", [4, 1100])
+def test_a_ring_that_has_too_few_pages(B):
+    """None is handed out: -1 in every new entry, the number that is missing, pages given back all the same; with them the same step again goes through."""
+    print(f"[case] shortage B={B}", flush=True)
+    held, keep, rows = [100] * B, [100] * (B - 2) + [0, 20], [40] * (B - 2) + [0, 0]
+    s = Step(18, held, keep, rows, spare=-1)
+    got = s.expect()
+    assert got[2][2] == 1
+    s.check()
+    s.given -= 1
+    s.check()
+    s = Step(19, held, keep, rows, spare=0)                                    # just enough
+    assert s.expect()[2][2] == 0
+    s.check()
+
+
+def test_a_state_that_is_none_stays_inside_the_ring():
+    print("[case] bad state", flush=True)
+    for taken, given in ((-5, -2), (50, 10), (0, 2 ** 62), (-2 ** 62, 2 ** 62), (2 ** 63 - 1, -2 ** 63)):
+        s = Step(20, [100, 50, 0], [100, 0, 0], [40, 0, 60], taken=0)
+        s.taken, s.given = taken, given
+        got = s.run()                                                          # (guards are looked at there)
+        assert got[0] == [0, 40, 40, 100] and got[1] == [140, 0, 60]
+
+
+def test_no_sequences_with_rows():
+    print("[case] nothing", flush=True)
+    Step(21, [5, 6], [5, 6], [0, 0]).check()
+    Step(22, [0], [0], [0]).check()
+
+
+def test_steps_on_end_in_one_graph():
+    """The state and the lengths in place: a captured step replayed, with other figures every time, against the oracle's steps."""
+    print("[case] graph", flush=True)
+    r = np.random.Generator(np.random.PCG64(23))
+    B, page, pages, width, T = 40, 16, 700, 40, 600
+    table, ring = [[-7] * width for _ in range(B)], list(range(pages))
+    state = (0, pages)
+    d = {"table": _i32(table), "ring": _i32(ring), "lengths": torch.zeros(B, dtype=torch.int32, device="cuda"), "keep": torch.zeros(B, dtype=torch.int32, device="cuda"),
+         "rows": torch.zeros(B, dtype=torch.int32, device="cuda"), "starts": torch.zeros(B + 1, dtype=torch.int32, device="cuda"),
+         "state": torch.tensor([0, pages, 0], device="cuda"), "positions": torch.zeros(T, dtype=torch.int32, device="cuda"),
+         "slots": torch.zeros(T, dtype=torch.int64, device="cuda")}
+    batch = fq.KvBatch(d["starts"], d["lengths"], d["table"], B, T, width, width, 1, 1)
+    pool = fq.PagePool(d["ring"], d["state"], d["state"], pages)
+    call = lambda: fq.flatquant_cache_advance(batch, pool, page, pages, d["lengths"], d["keep"], d["rows"], d["positions"], d["slots"],      # noqa: E731
+                                              stream=torch.cuda.current_stream())
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        call()
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    held = [0] * B
+    for step in range(12):
+        keep = [h if r.random() < 0.7 else int(r.integers(0, h + 1)) for h in held]
+        rows = [int(r.integers(0, 15)) if k < 550 else 0 for k in keep]
+        d["keep"].copy_(_i32(keep))
+        d["rows"].copy_(_i32(rows))
+        graph.replay()
+        torch.cuda.synchronize()
+        starts, lengths, nxt, positions, slots = so.advance(held, keep, rows, table, width, page, pages, ring, *state, T)
+        assert nxt[2] == 0
+        state, held = nxt[:2], lengths
+        for name, want in (("starts", starts), ("lengths", lengths), ("state", list(nxt)), ("positions", positions), ("slots", slots), ("table", table), ("ring", ring)):
+            assert d[name].tolist() == want, (step, name)
