@@ -93,7 +93,7 @@ def rope64(x, w, eps, positions, frequencies, interleaved, P=None):
 def scored64(q, k, v, seen, scale, positions, cap, slope, k_step, v_step, k_bits=4):
     """One head: q [n, 128], k, v [L, 128], seen [n, L], positions [n], the tokens' steps [L].  Returns out [n, 128] (zeros for a row that sees nothing) and for
     the bound A = sum_j w_j |v_j|, S = sum_j w_j v_step_j, and what errors of the scores do, E = sum_j w_j d_j (|v_j| + |out|).  The error d_j of a score:
-    of the product as for plain scores (cache_oracle.attention64; tanh's slope is at most one); of the cap 2^-21 of it, where it is beyond 40 2^-19
+    of the product as for plain scores (cache_oracle.attention64; tanh's slope is at most one); of the cap 2^-21 of it, where it is beyond 177 2^-19
     of the score; of the score and its distance's part, base 2, a product and a sum of each 2^-22."""
     q = np.asarray(q, dtype=np.float64)
     n, L = seen.shape
@@ -107,7 +107,7 @@ def scored64(q, k, v, seen, scale, positions, cap, slope, k_step, v_step, k_bits
         d = abs(scale) * k_step[j].max() * (280 * 2.0 ** -24 * (2 ** k_bits - 1) * a.sum() + 132 * 2.0 ** -18 * a.max()) + np.zeros(len(j))
         if cap:
             s = cap * np.tanh(s / cap)
-            d = d + (cap * 2.0 ** -21 if cap < 40 else np.abs(s) * 2.0 ** -19 + 2.0 ** -22)
+            d = d + (cap * 2.0 ** -21 if cap < 177 else np.abs(s) * 2.0 ** -19 + 2.0 ** -22)
         low = slope * np.abs(positions[i] - j)
         d = d + (np.abs(s) + abs(low)) * 2.0 ** -22
         s = s - low

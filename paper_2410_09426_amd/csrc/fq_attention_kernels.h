@@ -56,17 +56,27 @@ struct AttnDev {
 
 // With scores that are capped, lowered by a distance, or seen through a prefix (flatquant_cache_scored_attention), in the exponent's base 2.
 struct ScoredDev : AttnDev {
-    float cap;                // 0: none
-    float per_cap;            // 1 / cap
+    int bend;                 // 0: no cap, 1: scale2 takes scores to exponents of tanh, whose results are in units of 2 cap, 2: a large cap
+    float cap, per_cap;       // of a large one, and its reciprocal
+    float unit;               // what scores are in
     const float* slopes;      // of a query head; null: none
     const int32_t* prefix;    // of a sequence; null: none
 };
 template <typename DEV>
 constexpr bool kScored = std::is_same_v<DEV, ScoredDev>;
+// x, or none if it is infinite.  (tanh would make a number of a score whose key's step is none.)
+__device__ __forceinline__ float if_finite(float x) { return __builtin_fmaf(x, 0.0f, x); }
 // A sum over values.  An infinite one has a step that is none, or its negative, among them: no number.
 template <typename DEV>
 __device__ __forceinline__ float outcome(float x) {
-    if constexpr (kScored<DEV>) return __builtin_fmaf(x, 0.0f, x);
+    if constexpr (kScored<DEV>) return if_finite(x);
+    return x;
+}
+// Step x of a span of `steps`, in the order that the scores ask for: with slopes the last one first, where the scores are highest, so that references need not be raised
+// at every step (2048 rows at 8192 tokens 1110 -> 560 us).
+template <typename DEV>
+__device__ __forceinline__ int in_order(const DEV& p, int steps, int x) {
+    if constexpr (kScored<DEV>) return p.slopes ? steps - 1 - x : x;
     return x;
 }
 // Tokens of sequence b that all of its rows see, wherever they are.
@@ -331,6 +341,20 @@ __device__ __forceinline__ T across_groups(T x, T (*op)(T, T)) {               /
 __device__ __forceinline__ float fmax_op(float a, float b) { return __builtin_fmaxf(a, b); }
 __device__ __forceinline__ float fadd_op(float a, float b) { return a + b; }
 
+// What the scores of a row are in, by the time that they are weighed.
+template <typename DEV>
+__device__ __forceinline__ float unit_of(const DEV& p, float factor) {
+    if constexpr (kScored<DEV>) return p.unit;
+    else return factor;
+}
+
+// What a key's step makes of a score, or no number if it is none.
+template <typename DEV>
+__device__ __forceinline__ float key_factor(const DEV& p, float step) {
+    if constexpr (kScored<DEV>) return if_finite(step) * p.scale2;
+    return step * p.scale2;
+}
+
 // The tokens that a tile of rows goes through: whole steps over the first tokens [0, 32 first_steps), then from `begin` (a multiple of 32) to `end`.
 struct Span {
     int first_steps, begin, end, steps;
@@ -414,44 +438,33 @@ __device__ __forceinline__ float zero_sum(uint32_t pair, uint32_t params, float 
     else asm("v_fma_mix_f32 %0, %1, %2, %0 op_sel:[0,1,0] op_sel_hi:[1,1,0]" : "+v"(sum) : "v"(pair), "v"(params));
     return sum;
 }
-// A score x (factor taken in, base 2), capped: cap tanh(x / cap) = cap - 2 cap / (1 + e^(2 x / cap)), which is off by 2^-22 of the cap, whatever the score.  Large caps
-// (CLOSE) take the series of tanh below a quarter instead, so that the error is 2^-21 of the score there too.  A score that is no number stays
-// none, and so does an infinite one, which comes from a step that is no number.
-constexpr float kLargeCap = 64.0f;
-template <bool CLOSE>
-__device__ __forceinline__ float capped(float x, float cap, float per_cap) {
-    const float y = x * per_cap;
-    const float e = __builtin_amdgcn_exp2f(y * 2.8853900817779268f);           // 2 log2(e)
-    const float far = __builtin_fmaf(-2.0f * cap, __builtin_amdgcn_rcpf(1.0f + e), cap);
-    float r = far;
-    if constexpr (CLOSE) {
-        const float y2 = y * y;
-        const float near = __builtin_fmaf(__builtin_fmaf(__builtin_fmaf(-17.0f / 315, y2, 2.0f / 15), y2, -1.0f / 3) * y2, x, x);
-        r = y2 < 0.0625f ? near : far;
-    }
-    return __builtin_fmaf(x, 0.0f, r);
-}
-// Scores of N tokens, capped and lowered: `distance(k)` is the token's position less the row's.
+// Scores of N tokens (all factors taken in; none infinite), capped and lowered; `distance(k)` is the token's position less the row's.  What is no number stays none.
+//   cap tanh(x / cap) = cap - 2 cap / (1 + e^(2 x / cap)): the exponent of 2 is what comes in, the cap alone is a constant of the row, which weights do not depend on, and the
+//   rest goes on in units of 2 cap: an exponential, an addition and a reciprocal.  It is off by 2^-21 of the cap, whatever the score.
+//   Caps beyond kLargeCap take the series of tanh below a quarter instead, so that the error is 2^-19 of the score there.  That takes twice the time of all the rest of a
+//   step (2048 rows at 8192 tokens 670 / 930 us), and up to there the error is below 2^-13, a quarter of what the weights are rounded by.
+constexpr float kLargeCap = 256.0f;        // base 2
 template <int N, typename Distance>
 __device__ __forceinline__ void rescore(const ScoredDev& p, float (&score)[N], float slope, Distance distance) {
-    if (p.cap > 0.0f) {
-        if (p.cap > kLargeCap)
+    if (p.bend == 1) {
 #pragma unroll
-            for (int k = 0; k < N; ++k) score[k] = capped<true>(score[k], p.cap, p.per_cap);
-        else
+        for (int k = 0; k < N; ++k) score[k] = __builtin_amdgcn_rcpf(-1.0f - __builtin_amdgcn_exp2f(score[k]));
+    } else if (p.bend == 2) {
 #pragma unroll
-            for (int k = 0; k < N; ++k) score[k] = capped<false>(score[k], p.cap, p.per_cap);
-    } else {
-#pragma unroll
-        for (int k = 0; k < N; ++k) score[k] = __builtin_fmaf(score[k], 0.0f, score[k]);
+        for (int k = 0; k < N; ++k) {
+            const float x = score[k], y = x * p.per_cap, y2 = y * y;
+            const float far = __builtin_fmaf(-2.0f * p.cap, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(y * 2.8853900817779268f)), p.cap);
+            const float near = __builtin_fmaf(__builtin_fmaf(__builtin_fmaf(-17.0f / 315, y2, 2.0f / 15), y2, -1.0f / 3) * y2, x, x);
+            score[k] = y2 < 0.0625f ? near : far;
+        }
     }
     if (p.slopes)
 #pragma unroll
         for (int k = 0; k < N; ++k) score[k] = __builtin_fmaf(-slope, __builtin_fabsf(distance(k)), score[k]);
 }
-// Slope of a query head, in base 2.  (Beyond 2^80, where a token further on has no weight either, it is held there: sums stay finite.)
+// Slope of a query head, in the units of the scores.  (Beyond 2^60, where a token further on has no weight either, it is held there: sums stay finite.)
 __device__ __forceinline__ float slope_of(const ScoredDev& p, int hq) {
-    return p.slopes ? __builtin_fminf(__builtin_fmaxf(p.slopes[hq] * 1.44269504088896340736f, -0x1p80f), 0x1p80f) : 0.0f;
+    return p.slopes ? __builtin_fminf(__builtin_fmaxf(p.slopes[hq] * 1.44269504088896340736f, -0x1p60f), 0x1p60f) / p.unit : 0.0f;
 }
 
 // Weights 2^(factor score - ref), their products with the values' steps and the weights' sum; true if a lane of the wave needs a higher reference.
@@ -496,7 +509,10 @@ struct FewRows {
 };
 // Rows row0 .. row_end - 1 (16 NT at most) of head `head` of sequence b over steps [x_begin, x_end) of their span.  The result is the output, or (partial) what
 // the join needs, rows from partial_at on.
-template <int KB, int VB, int NT, int NW, typename DEV>
+// V > 1 (scores that cost more than the products: ScoredDev): there are 16 / V rows at most, each is in V of the 16 columns, and each of these columns takes the scores of
+// one V-th of the tokens, with a reference and sums of its own, weights of zero for the others: the work of a score is done by all lanes instead of those that
+// have a row.  The columns meet behind the last step.
+template <int KB, int VB, int NT, int NW, int V, typename DEV>
 __device__ __forceinline__ void few_rows(const DEV& p, unsigned char* smem, int b, int head, const Sequence& seq, int row0, int row_end, const Span& span,
                                          int x_begin, int x_end, bool partial, int64_t partial_at) {
     typedef Ring<KB, VB> R;
@@ -515,7 +531,7 @@ __device__ __forceinline__ void few_rows(const DEV& p, unsigned char* smem, int 
 
     // (a step behind the last one: no harm, what its table entries say is checked before it is followed)
     auto pages_of = [&](int x, int (&pg)[2]) {
-        const int k0 = span.token(x);
+        const int k0 = span.token(in_order(p, span.steps, x));
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             const unsigned j = (unsigned)(k0 + 16 * t) >> p.c.page_shift;
@@ -524,7 +540,7 @@ __device__ __forceinline__ void few_rows(const DEV& p, unsigned char* smem, int 
     };
     auto load = [&](int x, const int (&pg)[2], int slot) {
         const int ok[2] = {(unsigned)pg[0] < (unsigned)p.c.pages ? pg[0] : 0, (unsigned)pg[1] < (unsigned)p.c.pages ? pg[1] : 0};
-        load_step<KB, VB>(p.c, head, span.token(x), ok, l, ring + slot * R::SLOT);
+        load_step<KB, VB>(p.c, head, span.token(in_order(p, span.steps, x)), ok, l, ring + slot * R::SLOT);
     };
     int x = x_begin + w;
     int pg[DEPTH + 1][2];
@@ -541,7 +557,7 @@ __device__ __forceinline__ void few_rows(const DEV& p, unsigned char* smem, int 
     float slope[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        int r = row0 + 16 * n + i;
+        int r = row0 + 16 * n + (V > 1 ? i % (16 / V) : i);
         r = r < row_end ? r : row_end - 1;
         const int token = r / p.G, sub = r - token * p.G;
         const _Float16* src = p.q + (seq.first + token) * p.q_stride + (head * p.G + sub) * ATT_D + 32 * g;
@@ -599,7 +615,7 @@ __device__ __forceinline__ void few_rows(const DEV& p, unsigned char* smem, int 
     }
 
     auto work = [&](int x, const int (&pg)[2], const unsigned char* slot) {
-        const int k0 = span.token(x);
+        const int k0 = span.token(in_order(p, span.steps, x));
         f32x4 sc[NT][2];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
@@ -617,75 +633,129 @@ __device__ __forceinline__ void few_rows(const DEV& p, unsigned char* smem, int 
             }
         }
         __builtin_amdgcn_sched_barrier(0);
-        // sum_d q_d (c_d - z) = (sum_d q_d c_d) - z sum_d q_d
-        uint32_t vp[8];
+        half8 pw[NT];
+        // whether all rows see all of the step (called behind the sums: what it takes is not kept over them)
+        auto whole = [&] {
+            const bool pages_ok = (unsigned)pg[0] < (unsigned)p.c.pages && (unsigned)pg[1] < (unsigned)p.c.pages;
+            const int all_see = p.visible ? before - 1 : last_of(pos_lo, prefix);      // every row sees the tokens up to here, but for the window
+            return pages_ok && k0 + ATT_STEP - 1 <= all_see && k0 + ATT_STEP <= span.end && (p.window <= 0 || p.visible || k0 > pos_hi - p.window);
+        };
+        if constexpr (V > 1) {
+            constexpr int N = 8 / V;                                           // tokens of a lane, one behind the other
+            const int part = i / (16 / V), tile = V == 2 ? part : part >> 1, first = 16 * tile + 4 * g + (V == 2 ? 0 : 2 * (part & 1));
+            typedef uint32_t words __attribute__((ext_vector_type(N)));
+            const words kp = *reinterpret_cast<const words*>(slot + R::P_AT + 4 * first), v = *reinterpret_cast<const words*>(slot + R::P_AT + 128 + 4 * first);
+            float s[N], prod[N], sum;
+            uint32_t vp[N];
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const u32x4 kp = *reinterpret_cast<const u32x4*>(slot + R::P_AT + 64 * t + 16 * g), v4 = *reinterpret_cast<const u32x4*>(slot + R::P_AT + 128 + 64 * t + 16 * g);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-                    sc[n][t][r] = times_step(kp[r], __builtin_fmaf((float)zero_bits(kp[r]), q_sum[n], sc[n][t][r]));
-                vp[4 * t + r] = v4[r];
+            for (int k = 0; k < N; ++k) {
+                float x = tile ? sc[0][1][k] : sc[0][0][k];
+                if constexpr (V == 4) x = part & 1 ? (tile ? sc[0][1][2 + k] : sc[0][0][2 + k]) : x;
+                s[k] = if_finite(times_step(kp[k], __builtin_fmaf((float)zero_bits(kp[k]), q_sum[0], x)) * factor[0]);
+                vp[k] = v[k];
             }
-        }
-        const bool pages_ok = (unsigned)pg[0] < (unsigned)p.c.pages && (unsigned)pg[1] < (unsigned)p.c.pages;
-        if constexpr (kScored<DEV>)
+            const float from = (float)(k0 + first - sight[0].hi);              // (no slopes in trees: hi is the row's position)
+            rescore(p, s, slope[0], [&](int k) { return from + (float)k; });
+            if (!whole()) {
+                const bool page_ok = (unsigned)(tile ? pg[1] : pg[0]) < (unsigned)p.c.pages;
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                const float from = (float)(k0 + 4 * g - sight[n].hi);          // (no slopes in trees: hi is the row's position)
-                float s8[8];
-#pragma unroll
-                for (int k = 0; k < 8; ++k) s8[k] = sc[n][k >> 2][k & 3] * factor[n];
-                rescore(p, s8, slope[n], [&](int k) { return from + (float)(16 * (k >> 2) + (k & 3)); });
-#pragma unroll
-                for (int k = 0; k < 8; ++k) sc[n][k >> 2][k & 3] = s8[k];
-            }
-        const int all_see = p.visible ? before - 1 : last_of(pos_lo, prefix);        // every row sees the tokens up to here, but for the window
-        if (!(pages_ok && k0 + ATT_STEP - 1 <= all_see && k0 + ATT_STEP <= span.end && (p.window <= 0 || p.visible || k0 > pos_hi - p.window))) {
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const bool page_ok = (unsigned)pg[t] < (unsigned)p.c.pages;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int k = k0 + 16 * t + 4 * g + r;
-                    const bool held = page_ok & (k < span.end);
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        bool ok = sees(sight[n], k);
-                        if (p.visible) ok |= sees_drafted(sight[n], before, k);
-                        sc[n][t][r] = (ok & held) ? if_number(vp[4 * t + r], sc[n][t][r]) : -__builtin_inff();
-                    }
-                    vp[4 * t + r] = usable_parameters(vp[4 * t + r]);
+                for (int k = 0; k < N; ++k) {
+                    const int at = k0 + first + k;
+                    bool ok = sees(sight[0], at);
+                    if (p.visible) ok |= sees_drafted(sight[0], before, at);
+                    s[k] = (ok & page_ok & (at < span.end)) ? if_number(vp[k], s[k]) : -__builtin_inff();
+                    vp[k] = usable_parameters(vp[k]);
                 }
             }
-        }
-        half8 pw[NT];
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            float s8[8], prod[8], sum;
-            auto by = [&](int) { return kScored<DEV> ? 1.0f : factor[n]; };
+            auto by = [&](int) { return unit_of(p, factor[0]); };
             auto step = [&](int k) { return (float)step_bits(vp[k]); };
+            if (weigh<N, false>(s, by, step, ref[0], prod, sum)) {
+                const float f = raise_reference<N>(s, by, step, ref[0], [](float top) { return across_groups(top, fmax_op); });
+                total[0] *= f;
+                zeros[0] *= f;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) s8[k] = sc[n][k >> 2][k & 3];
-            if (weigh<8, false>(s8, by, step, ref[n], prod, sum)) {
-                const float f = raise_reference<8>(s8, by, step, ref[n], [](float top) { return across_groups(top, fmax_op); });
-                total[n] *= f;
-                zeros[n] *= f;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) acc[n][j] *= f;
-                weigh<8, true>(s8, by, step, ref[n], prod, sum);
+                for (int j = 0; j < 8; ++j) acc[0][j] *= f;
+                weigh<N, true>(s, by, step, ref[0], prod, sum);
             }
-            total[n] += sum;
+            total[0] += sum;
             u32x4 pp;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                pp[k] = as_u32(half2v{(_Float16)prod[2 * k], (_Float16)prod[2 * k + 1]});
-                zeros[n] = zero_sum<0>(pp[k], vp[2 * k], zeros[n]);
-                zeros[n] = zero_sum<1>(pp[k], vp[2 * k + 1], zeros[n]);
+            for (int k = 0; k < N / 2; ++k) {
+                const uint32_t two = as_u32(half2v{(_Float16)prod[2 * k], (_Float16)prod[2 * k + 1]});
+                zeros[0] = zero_sum<0>(two, vp[2 * k], zeros[0]);
+                zeros[0] = zero_sum<1>(two, vp[2 * k + 1], zeros[0]);
+#pragma unroll
+                for (int m = 0; m < V; ++m) pp[N / 2 * m + k] = part == m ? two : 0u;
             }
-            pw[n] = __builtin_bit_cast(half8, pp);
+            pw[0] = __builtin_bit_cast(half8, pp);
+        } else {
+            // sum_d q_d (c_d - z) = (sum_d q_d c_d) - z sum_d q_d
+            uint32_t vp[8];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const u32x4 kp = *reinterpret_cast<const u32x4*>(slot + R::P_AT + 64 * t + 16 * g), v4 = *reinterpret_cast<const u32x4*>(slot + R::P_AT + 128 + 64 * t + 16 * g);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+                        sc[n][t][r] = times_step(kp[r], __builtin_fmaf((float)zero_bits(kp[r]), q_sum[n], sc[n][t][r]));
+                    vp[4 * t + r] = v4[r];
+                }
+            }
+            if constexpr (kScored<DEV>)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const float from = (float)(k0 + 4 * g - sight[n].hi);          // (no slopes in trees: hi is the row's position)
+                    float s8[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) s8[k] = if_finite(sc[n][k >> 2][k & 3] * factor[n]);
+                    rescore(p, s8, slope[n], [&](int k) { return from + (float)(16 * (k >> 2) + (k & 3)); });
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) sc[n][k >> 2][k & 3] = s8[k];
+                }
+            if (!whole()) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    const bool page_ok = (unsigned)pg[t] < (unsigned)p.c.pages;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int k = k0 + 16 * t + 4 * g + r;
+                        const bool held = page_ok & (k < span.end);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            bool ok = sees(sight[n], k);
+                            if (p.visible) ok |= sees_drafted(sight[n], before, k);
+                            sc[n][t][r] = (ok & held) ? if_number(vp[4 * t + r], sc[n][t][r]) : -__builtin_inff();
+                        }
+                        vp[4 * t + r] = usable_parameters(vp[4 * t + r]);
+                    }
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                float s8[8], prod[8], sum;
+                auto by = [&](int) { return unit_of(p, factor[n]); };
+                auto step = [&](int k) { return (float)step_bits(vp[k]); };
+#pragma unroll
+                for (int k = 0; k < 8; ++k) s8[k] = sc[n][k >> 2][k & 3];
+                if (weigh<8, false>(s8, by, step, ref[n], prod, sum)) {
+                    const float f = raise_reference<8>(s8, by, step, ref[n], [](float top) { return across_groups(top, fmax_op); });
+                    total[n] *= f;
+                    zeros[n] *= f;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) acc[n][j] *= f;
+                    weigh<8, true>(s8, by, step, ref[n], prod, sum);
+                }
+                total[n] += sum;
+                u32x4 pp;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    pp[k] = as_u32(half2v{(_Float16)prod[2 * k], (_Float16)prod[2 * k + 1]});
+                    zeros[n] = zero_sum<0>(pp[k], vp[2 * k], zeros[n]);
+                    zeros[n] = zero_sum<1>(pp[k], vp[2 * k + 1], zeros[n]);
+                }
+                pw[n] = __builtin_bit_cast(half8, pp);
+            }
         }
         uint32_t vc[8];
 #pragma unroll
@@ -728,6 +798,24 @@ __device__ __forceinline__ void few_rows(const DEV& p, unsigned char* smem, int 
         }
     }
 
+    if constexpr (V > 1) {                                                     // the columns of a row meet
+        float top = __builtin_fmaxf(ref[0], dpp_move<0x128>(ref[0]));          // row_ror:8
+        if constexpr (V == 4) top = __builtin_fmaxf(top, dpp_move<0x124>(top));
+        const float f = __builtin_amdgcn_exp2f(ref[0] - top);
+        ref[0] = top;
+        auto meet = [&](float x) {
+            x *= f;
+            x += dpp_move<0x128>(x);
+            if constexpr (V == 4) x += dpp_move<0x124>(x);                     // row_ror:4
+            return x;
+        };
+        total[0] = meet(total[0]);
+        zeros[0] = meet(zeros[0]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[0][j][r] = meet(acc[0][j][r]);
+    }
     // ---- the waves meet
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -810,15 +898,16 @@ __device__ __forceinline__ Tile tile_of(const AttnDev& p, const Sequence& seq, i
 }
 
 // blockIdx: (sequence and head, tile of rows).
-template <int KB, int VB, int NT, int NW, typename DEV>
+template <int KB, int VB, int NT, int NW, typename DEV, int V = 1>
 __global__ __launch_bounds__(64 * NW, NW > 4 ? 4 : NT == 1 ? 3 : 2) void whole_attention_kernel(DEV p) {
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     const int b = blockIdx.x / p.c.H, head = blockIdx.x - b * p.c.H;
     const Sequence seq = sequence_of(p.c, b);
-    const int tiles = (seq.rows * p.G + 16 * NT - 1) / (16 * NT);
+    constexpr int ROWS = 16 * NT / V;
+    const int tiles = (seq.rows * p.G + ROWS - 1) / ROWS;
     for (int tile = blockIdx.y; tile < tiles; tile += gridDim.y) {
-        const Tile t = tile_of<16 * NT>(p, seq, tiles - 1 - tile, prefix_of(p, b));    // the last rows, which see most, first
-        few_rows<KB, VB, NT, NW>(p, smem, b, head, seq, t.row0, t.row_end, t.span, 0, t.span.steps, false, 0);
+        const Tile t = tile_of<ROWS>(p, seq, tiles - 1 - tile, prefix_of(p, b));       // the last rows, which see most, first
+        few_rows<KB, VB, NT, NW, V>(p, smem, b, head, seq, t.row0, t.row_end, t.span, 0, t.span.steps, false, 0);
     }
 }
 
@@ -894,10 +983,10 @@ __device__ __forceinline__ int sequence_at(const Cut& c, int B, int u) {
     return n - 1;
 }
 
-template <int KB, int VB, int NT, int NW, typename DEV>
+template <int KB, int VB, int NT, int NW, typename DEV, int V = 1>
 __global__ __launch_bounds__(64 * NW, NT == 1 ? 3 : 2) void balanced_attention_kernel(DEV p) {
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    constexpr int ROWS = 16 * NT;
+    constexpr int ROWS = 16 * NT / V;
     Cut& cut = *reinterpret_cast<Cut*>(smem + FewRows<KB, VB, NT, NW>::LDS);
     make_cut<ROWS>(p, gridDim.x, cut);
     const int wg = blockIdx.x, per = uniform(cut.per), begin = wg * per, end = min(begin + per, uniform(cut.all));
@@ -929,16 +1018,16 @@ __global__ __launch_bounds__(64 * NW, NT == 1 ? 3 : 2) void balanced_attention_k
         const Sequence seq = sequence_of(cut, b);
         const Tile t = tile_of<ROWS>(p, seq, tile, prefix_of(p, b));
         tile += !units;
-        few_rows<KB, VB, NT, NW>(p, smem, b, head, seq, t.row0, t.row_end, t.span, 4 * from, min(t.span.steps, 4 * to), partial, at);
+        few_rows<KB, VB, NT, NW, V>(p, smem, b, head, seq, t.row0, t.row_end, t.span, 4 * from, min(t.span.steps, 4 * to), partial, at);
     }
 }
 
 // Joins the partial results of the (sequence, head) pairs that more than one workgroup had: blockIdx (pair, part of its rows).  Up to 16 workgroups: a wave a row;
 // more: a row at a time, its workgroups dealt out to the waves.
-template <int NT, typename DEV>
+template <int NT, typename DEV, int V = 1>
 __global__ __launch_bounds__(ATT_NT) void balanced_join_kernel(DEV p, int workgroups) {
     __shared__ float tops[ATT_WAVES], totals[ATT_WAVES], sums[ATT_WAVES][ATT_D];
-    constexpr int ROWS = 16 * NT;
+    constexpr int ROWS = 16 * NT / V;
     const int l = threadIdx.x & 63;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int b = blockIdx.x / p.c.H, head = blockIdx.x - b * p.c.H;
@@ -1101,11 +1190,12 @@ __global__ __launch_bounds__(64 * NW, 2) void shared_attention_kernel(DEV p) {
         float ref = ATT_NONE, total = 0.0f, slope = 0.0f;
         if constexpr (kScored<DEV>) slope = slope_of(p, head * p.G + sub);
 
+        const int lower = in_order(p, 1, 0) == in_order(p, 2, 0) ? 0 : 1;      // which of two steps has the lower tokens
         // codes of steps x and x + 1 of the span, 32 tokens each, which need not follow each other
         // The page of tokens 16 n .. of the step from x on, by every lane n of NW: looked up in all lanes at once (a scalar look-up each took more time than the
         // conversion), a step before the loads that follow it, in whose queue it stands.
         auto page_of = [&](int x) {
-            const int n = again(l) % NW, y = x + (n >> 1);
+            const int n = again(l) % NW, y = in_order(p, span.steps, x + (n >> 1));
             const unsigned token = (unsigned)((y < span.first_steps ? ATT_STEP * y : span.begin + ATT_STEP * (y - span.first_steps)) + 16 * (n & 1));
             const unsigned j = token >> p.c.page_shift, last = (unsigned)p.c.table_width - 1u;
             return p.c.page_table[b * p.c.table_stride + (j < last ? j : last)];           // (behind the width: behind the end)
@@ -1115,7 +1205,7 @@ __global__ __launch_bounds__(64 * NW, 2) void shared_attention_kernel(DEV p) {
             s.pages = (int)__ballot(ok) & ((1 << NW) - 1);
             const int held = ok ? page : 0, mine = 2 * (2 * part + w % 2);
             const int pg[2] = {__builtin_amdgcn_readlane(held, mine), __builtin_amdgcn_readlane(held, mine + 1)};      // of this wave's 32 tokens
-            const int k0 = span.token(x + 2 * part + w % 2);
+            const int k0 = span.token(in_order(p, span.steps, x + 2 * part + w % 2));
             const int mask = (1 << p.c.page_shift) - 1;
             const int lane = again(l);
             u32x4 words[2] = {}, parameters[2] = {};
@@ -1179,7 +1269,7 @@ __global__ __launch_bounds__(64 * NW, 2) void shared_attention_kernel(DEV p) {
                         *reinterpret_cast<u32x4*>(base + tok * SH_K_PITCH + 16 * chunk) = o;
                     });
                 }
-                if (h == 0) steps[tok] = step_of(s.params(0)) * p.scale2;
+                if (h == 0) steps[tok] = key_factor(p, step_of(s.params(0)));
             } else {
                 const int i = l & 15, g = l >> 4, chunk = 4 * (role - 2) + g;
                 const Masks<VB> masks;
@@ -1231,13 +1321,17 @@ __global__ __launch_bounds__(64 * NW, 2) void shared_attention_kernel(DEV p) {
                 for (int e = 0; e < 4; ++e) f[4 * k + e] = v[e];
             }
         };
+        auto factor_of = [&](const float (&fk)[16], int k) {
+            if constexpr (kScored<DEV>) return p.unit;                         // (the keys' steps are in the scores by then)
+            else return fk[k];
+        };
         // scores of tokens that a row does not see: -infinity (the factors are one then), and steps of zero: a weight of zero times what the page holds, an
         // infinity of either sign or a NaN, need not be zero
         auto mask = [&](int x, int t, int pages, f32x16& sc, float (&fk)[16], float (&vs)[16]) {
-            const int k0 = span.token(x + t);
+            const int k0 = span.token(in_order(p, span.steps, x + t));
             const int pages_ok = pages >> (2 * t) & 3, all_see = p.visible ? before - 1 : last_of(pos_lo, prefix);
             if (pages_ok == 3 && k0 + 31 <= all_see && k0 + 32 <= span.end && x + t < x_end && (p.window <= 0 || p.visible || k0 > pos_hi - p.window)) return;
-            const int end = x + t < x_end ? span.end : 0;
+            const int end = x + t < x_end ? span.end : kScored<DEV> ? -0x7fffffff : 0;        // (in the other order tokens behind the last step are below zero)
             const int row = again(token);
             const Sight sight = sight_of(p, before, row, seq.first + row, prefix);
 #pragma unroll
@@ -1246,13 +1340,17 @@ __global__ __launch_bounds__(64 * NW, 2) void shared_attention_kernel(DEV p) {
                 bool ok = sees(sight, kk);
                 if (p.visible) ok |= sees_drafted(sight, before, kk);
                 ok = ok & (kk < end) & (pages_ok >> (k >> 3) & 1);
-                sc[k] = ok ? sc[k] * fk[k] : -__builtin_inff();
-                fk[k] = 1.0f;
+                if constexpr (kScored<DEV>) {
+                    sc[k] = ok ? sc[k] : -__builtin_inff();
+                } else {
+                    sc[k] = ok ? sc[k] * fk[k] : -__builtin_inff();
+                    fk[k] = 1.0f;
+                }
                 vs[k] = ok ? vs[k] : 0.0f;
             }
         };
         auto raise = [&](const f32x16& sc, const float (&fk)[16], const float (&vs)[16], float (&prod)[16], float& sum) {
-            auto by = [&](int k) { return fk[k]; };
+            auto by = [&](int k) { return factor_of(fk, k); };
             auto step = [&](int k) { return vs[k]; };
             const float f = raise_reference<16>(sc, by, step, ref, [](float top) { return __builtin_fmaxf(top, __shfl_xor(top, 32)); });
             total *= f;
@@ -1292,26 +1390,23 @@ __global__ __launch_bounds__(64 * NW, 2) void shared_attention_kernel(DEV p) {
                 for (int y = 0; y < PARTS; ++y) {
                     const unsigned char* base = sh_smem + (PARTS * buf + y) * SH_BUFFER;
                     // (the first tokens lie before everything else)
-                    if (!busy || x + 2 * y >= x_end || !(p.visible || span.token(x + 2 * y) <= last_of(pos_hi, prefix))) continue;
+                    if (!busy || x + 2 * y >= x_end || !(p.visible || span.token(in_order(p, span.steps, x + 2 * y + lower)) <= last_of(pos_hi, prefix))) continue;
 #pragma unroll
                     for (int t = 0; t < 2; ++t) {
                         if (halved && t != my_half) continue;
                         f32x16 sc;
                         float fk[16], vs[16], prod[16], sum;
                         half8 pw[2];
-                        auto by = [&](int k) { return fk[k]; };
+                        auto by = [&](int k) { return factor_of(fk, k); };
                         auto step = [&](int k) { return vs[k]; };
                         scores(base, t, sc);
                         factors(base, 32 * t, fk);
                         factors(base, 64 + 32 * t, vs);
                         if constexpr (kScored<DEV>) {
-                            const float from = (float)(span.token(x + 2 * y + t) + 4 * h - before - again(token));
+                            const float from = (float)(span.token(in_order(p, span.steps, x + 2 * y + t)) + 4 * h - before - again(token));
                             float s16[16];
 #pragma unroll
-                            for (int k = 0; k < 16; ++k) {
-                                s16[k] = sc[k] * fk[k];
-                                fk[k] = 1.0f;
-                            }
+                            for (int k = 0; k < 16; ++k) s16[k] = sc[k] * fk[k];
                             rescore(p, s16, slope, [&](int k) { return from + (float)(8 * (k >> 2) + (k & 3)); });
 #pragma unroll
                             for (int k = 0; k < 16; ++k) sc[k] = s16[k];
@@ -1451,40 +1546,55 @@ __global__ __launch_bounds__(ATT_NT) void attention_join_kernel(DEV p) {
 // Compute units of the card: the plan (and with it the workspace) follows from the host's figures alone.
 constexpr int64_t kPlanCus = 256;
 
-template <int KB, int VB, typename DEV>
-static hipError_t attention_launch_bits(const DEV& d, const AttnPlan& plan, int64_t max_rows, hipStream_t stream) {
-    const int64_t tiles = (max_rows * d.G + plan.tile_rows - 1) / plan.tile_rows;
-    const dim3 pairs((unsigned)(d.c.B * d.c.H), (unsigned)(tiles < 1 ? 1 : tiles > 65535 ? 65535 : tiles), (unsigned)d.splits);
-    auto go = [&](auto kernel, dim3 grid, int threads, int lds, OccCache& cache) {
-        int occ = 0;
-        const hipError_t e = kernel_occupancy(reinterpret_cast<const void*>(kernel), threads, lds, cache, occ);
-        return e == hipSuccess ? launch(kernel, grid, dim3((unsigned)threads), lds, stream, d) : e;
-    };
-    static OccCache caches[8];
-    hipError_t e;
+// A kernel whose dynamic LDS may be more than the default.
+template <typename Kernel, typename DEV>
+static hipError_t large_launch(Kernel kernel, dim3 grid, int threads, int lds, OccCache& cache, hipStream_t stream, const DEV& d) {
+    int occ = 0;
+    const hipError_t e = kernel_occupancy(reinterpret_cast<const void*>(kernel), threads, lds, cache, occ);
+    return e == hipSuccess ? launch(kernel, grid, dim3((unsigned)threads), lds, stream, d) : e;
+}
+// Tiles of 16 NT rows (of 16 / V).
+template <int KB, int VB, int NT, int V, typename DEV>
+static hipError_t few_rows_launch(const DEV& d, const AttnPlan& plan, int64_t max_rows, hipStream_t stream) {
+    static OccCache caches[4];
+    constexpr int ROWS = 16 * NT / V;
+    const int64_t rows = max_rows * d.G, tiles = (rows + ROWS - 1) / ROWS;
+    const dim3 pairs((unsigned)(d.c.B * d.c.H), (unsigned)(tiles < 1 ? 1 : tiles > 65535 ? 65535 : tiles));
     if (plan.workgroups > 0) {
-        const dim3 grid((unsigned)plan.workgroups);
-        if (plan.tile_rows == 16) e = go(balanced_attention_kernel<KB, VB, 1, 4, DEV>, grid, 256, FewRows<KB, VB, 1, 4>::LDS + (int)sizeof(Cut), caches[0]);
-        else e = go(balanced_attention_kernel<KB, VB, 2, 4, DEV>, grid, 256, FewRows<KB, VB, 2, 4>::LDS + (int)sizeof(Cut), caches[1]);
+        const hipError_t e = large_launch(balanced_attention_kernel<KB, VB, NT, 4, DEV, V>, dim3((unsigned)plan.workgroups), 256,
+                                          FewRows<KB, VB, NT, 4>::LDS + (int)sizeof(Cut), caches[0], stream, d);
         if (e != hipSuccess) return e;
-        const int64_t rows = max_rows * d.G;
         // a workgroup a row where there are few pairs and so many partial results of each, else one for four rows
         const int64_t parts = pairs.x < kPlanCus ? rows : (rows + ATT_WAVES - 1) / ATT_WAVES;
-        const dim3 join(pairs.x, (unsigned)(parts < 1 ? 1 : parts < plan.tile_rows ? parts : plan.tile_rows));
-        if (plan.tile_rows == 16) return launch(balanced_join_kernel<1, DEV>, join, dim3(ATT_NT), 0, stream, d, plan.workgroups);
-        return launch(balanced_join_kernel<2, DEV>, join, dim3(ATT_NT), 0, stream, d, plan.workgroups);
+        const dim3 join(pairs.x, (unsigned)(parts < 1 ? 1 : parts < 16 * NT ? parts : 16 * NT));
+        return launch(balanced_join_kernel<NT, DEV, V>, join, dim3(ATT_NT), 0, stream, d, plan.workgroups);
     }
-    if (plan.tile_rows == 16 && plan.waves == 16) return go(whole_attention_kernel<KB, VB, 1, 16, DEV>, pairs, 1024, FewRows<KB, VB, 1, 16>::LDS, caches[2]);
-    if (plan.tile_rows == 16 && plan.waves == 8) return go(whole_attention_kernel<KB, VB, 1, 8, DEV>, pairs, 512, FewRows<KB, VB, 1, 8>::LDS, caches[6]);
-    if (plan.tile_rows == 16) return go(whole_attention_kernel<KB, VB, 1, 4, DEV>, pairs, 256, FewRows<KB, VB, 1, 4>::LDS, caches[3]);
-    if (plan.tile_rows == 32) return go(whole_attention_kernel<KB, VB, 2, 4, DEV>, pairs, 256, FewRows<KB, VB, 2, 4>::LDS, caches[4]);
-    if (plan.waves == 8) return go(shared_attention_kernel<KB, VB, 8, DEV>, pairs, 512, 4 * SH_BUFFER, caches[7]);
-    e = go(shared_attention_kernel<KB, VB, 4, DEV>, pairs, ATT_NT, 2 * SH_BUFFER, caches[5]);
+    if constexpr (NT == 1) {
+        if (plan.waves == 16) return large_launch(whole_attention_kernel<KB, VB, NT, 16, DEV, V>, pairs, 1024, FewRows<KB, VB, NT, 16>::LDS, caches[1], stream, d);
+        if (plan.waves == 8) return large_launch(whole_attention_kernel<KB, VB, NT, 8, DEV, V>, pairs, 512, FewRows<KB, VB, NT, 8>::LDS, caches[2], stream, d);
+    }
+    return large_launch(whole_attention_kernel<KB, VB, NT, 4, DEV, V>, pairs, 256, FewRows<KB, VB, NT, 4>::LDS, caches[3], stream, d);
+}
+template <int KB, int VB, typename DEV>
+static hipError_t attention_launch_bits(const DEV& d, const AttnPlan& plan, int64_t max_rows, hipStream_t stream) {
+    if (plan.tile_rows == 16) {
+        if constexpr (kScored<DEV>) {
+            const int64_t rows = max_rows * d.G;
+            if (rows <= 4) return few_rows_launch<KB, VB, 1, 4>(d, plan, max_rows, stream);
+            if (rows <= 8) return few_rows_launch<KB, VB, 1, 2>(d, plan, max_rows, stream);
+        }
+        return few_rows_launch<KB, VB, 1, 1>(d, plan, max_rows, stream);
+    }
+    if (plan.tile_rows == 32) return few_rows_launch<KB, VB, 2, 1>(d, plan, max_rows, stream);
+    static OccCache caches[2];
+    const int64_t tiles = (max_rows * d.G + plan.tile_rows - 1) / plan.tile_rows;
+    const dim3 pairs((unsigned)(d.c.B * d.c.H), (unsigned)(tiles < 1 ? 1 : tiles > 65535 ? 65535 : tiles), (unsigned)d.splits);
+    if (plan.waves == 8) return large_launch(shared_attention_kernel<KB, VB, 8, DEV>, pairs, 512, 4 * SH_BUFFER, caches[0], stream, d);
+    const hipError_t e = large_launch(shared_attention_kernel<KB, VB, 4, DEV>, pairs, ATT_NT, 2 * SH_BUFFER, caches[1], stream, d);
     if (e != hipSuccess || d.splits == 1) return e;
     const int64_t rows = (max_rows * d.G + ATT_WAVES - 1) / ATT_WAVES;
     return launch(attention_join_kernel<SH_ROWS * ATT_WAVES, DEV>, dim3(pairs.x, (unsigned)(rows < 1 ? 1 : rows > 65535 ? 65535 : rows)), dim3(ATT_NT), 0, stream, d);
 }
-
 
 // What every launch has of the arguments and the plan.
 inline void fill_attention(AttnDev& d, const CacheDev& c, const AttnArgs& a, const AttnPlan& plan) {
