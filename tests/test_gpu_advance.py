@@ -180,6 +180,18 @@ def test_a_state_that_is_none_stays_inside_the_ring():
         assert got[0] == [0, 40, 40, 100] and got[1] == [140, 0, 60]
 
 
+@pytest.mark.parametrize("B,rows", [(64, 100), (65, 100), (1000, 7), (1025, 9), (5000, 2), (66, 70), (200, 0)])
+def test_rows_of_many_sequences(B, rows):
+    """More rows than the one workgroup writes; runs of sequences without any, so that a wave's rows have one to hundreds of sequences between them."""
+    print(f"[case] rows of many B={B} rows={rows}", flush=True)
+    r = np.random.Generator(np.random.PCG64(B))
+    n = np.where(r.random(B) < 0.3, 0, r.integers(0, 2 * rows + 1, B))
+    n[B // 2] = 5000
+    n[B // 3:B // 3 + B // 5] = 0
+    held = r.integers(0, 40, B)
+    Step(24, held, held, n).check()
+
+
 def test_no_sequences_with_rows():
     print("[case] nothing", flush=True)
     Step(21, [5, 6], [5, 6], [0, 0]).check()
