@@ -7,9 +7,11 @@
 // 32 bits, a whole number of quarter turns taken off, is below an eighth of a turn, where few terms of the series give both functions to 2^-24.
 //
 // Without a matrix: 16 lanes a (row, head) group, eight channels each; a wave takes four rows and some of the heads, so that the angles are worked out
-// once for all of them, and the weights go into the cosines and sines.  Bound by memory.
+// once for all of them, four pairs a lane (the lane that holds the pairs' other numbers has the other four), and the weights go into the cosines and sines.  Bound by memory:
+// 16384 rows of 40 heads (336 MB) in 60 us; 64 rows in 3.4, a launch and two loads one after the other.  Stores past the caches: 4096 rows of 40 heads 22.5 -> 16.9 us.
 // With one: 32 groups a wave as the columns of v_mfma_f32_32x32x16_f16, as they come from memory: a lane holds 8 channels of every 16 of its group, both of
-// every pair, so that it turns them in its registers before they are the right operand.
+// every pair, so that it turns them in its registers before they are the right operand.  8192 rows of 32 + 8 heads (168 MB, 8.6 GFLOP) through one matrix in 46 us, 33 of
+// them memory at a copy's rate; through one each 76, as every group's angles are worked out for it alone, 32 a lane, which takes more than the products.
 #include "fq_internal.h"
 #include "fq_device.h"
 #include "fq_cache_device.h"
@@ -51,13 +53,12 @@ __device__ __forceinline__ float row16_sum(float x) {
 
 // ---- without a matrix
 
-// blockIdx: (four rows, heads); a wave has `per` heads, queries first.
+// Rows 4 block .. + 3 of heads `first` .. + per - 1, queries first, by one wave.
 template <int AHEAD>
-__global__ __launch_bounds__(RP_NT) void rope_kernel(RopeDev d, int per) {
+__device__ __forceinline__ void turn_rows(const RopeDev& d, int64_t block, int first, int per) {
     const int l = threadIdx.x & 63, i = l & 15, g = l >> 4;
-    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t row = 4 * (int64_t)blockIdx.x + g, t = row < d.T ? row : d.T - 1;
-    const int all = d.heads[0] + d.heads[1], first = ((int)blockIdx.y * RP_WAVES + w) * per, last = min(first + per, all);
+    const int64_t row = 4 * block + g, t = row < d.T ? row : d.T - 1;
+    const int all = d.heads[0] + d.heads[1], last = min(first + per, all);
     if (first >= last) return;
     const int position = d.positions[t];
     const bool live = row < d.T && position >= 0;
@@ -76,36 +77,43 @@ __global__ __launch_bounds__(RP_NT) void rope_kernel(RopeDev d, int per) {
     // cosines, and sines with the sign that the pair's other number has in this one
     const int half = d.rotary >> 1, ch = 8 * i;
     const bool turned = ch < d.rotary, second = ch >= half;
+    // the lane that has the other numbers (of those that are not turned: itself)
+    const int other = 4 * (!d.interleaved && turned ? l + (second ? -(half >> 3) : half >> 3) : l);
+    const bool across = !d.interleaved && d.rotary == 2 * 64;
+    auto exchange = [&](uint32_t x) {
+        return (uint32_t)(across ? __builtin_amdgcn_mov_dpp((int)x, 0x128, 0xF, 0xF, true) : __builtin_amdgcn_ds_bpermute(other, (int)x));     // row_ror:8
+    };
     float cs[8], sn[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         cs[e] = 1.0f;
         sn[e] = 0.0f;
     }
-    if (turned) {
+    if (d.rotary > 0) {
+        // four pairs a lane: all that its neighbours have, or half of those that it shares with the other lane
         const uint32_t p = position < 0 ? 0u : (uint32_t)position;
+        const int pair = !turned ? 0 : d.interleaved ? 4 * i : second ? ch - half + 4 : ch;
+        float c[4], s[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) cos_sin(angle_of(p, d.turns[pair + e]), c[e], s[e]);
         if (d.interleaved) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                float c, s;
-                cos_sin(angle_of(p, d.turns[4 * i + e]), c, s);
-                cs[2 * e] = cs[2 * e + 1] = c;
-                sn[2 * e] = -s;
-                sn[2 * e + 1] = s;
+                cs[2 * e] = cs[2 * e + 1] = turned ? c[e] : 1.0f;
+                sn[2 * e] = turned ? -s[e] : 0.0f;
+                sn[2 * e + 1] = turned ? s[e] : 0.0f;
             }
         } else {
-            const uint64_t* from = d.turns + ch - (second ? half : 0);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                float s;
-                cos_sin(angle_of(p, from[e]), cs[e], s);
-                sn[e] = second ? s : -s;
+            for (int e = 0; e < 4; ++e) {
+                const float co = __builtin_bit_cast(float, exchange(__builtin_bit_cast(uint32_t, c[e]))), so = __builtin_bit_cast(float, exchange(__builtin_bit_cast(uint32_t, s[e])));
+                cs[e] = !turned ? 1.0f : second ? co : c[e];
+                cs[4 + e] = !turned ? 1.0f : second ? c[e] : co;
+                sn[e] = !turned ? 0.0f : second ? so : -s[e];
+                sn[4 + e] = !turned ? 0.0f : second ? s[e] : -so;
             }
         }
     }
-    // the lane that has the other numbers (of those that are not turned: itself)
-    const int other = 4 * (!d.interleaved && turned ? l + (second ? -(half >> 3) : half >> 3) : l);
-    const bool across = !d.interleaved && d.rotary == 2 * 64;
 
     int role = -1;
     float cw[8], sw[8];
@@ -140,12 +148,9 @@ __global__ __launch_bounds__(RP_NT) void rope_kernel(RopeDev d, int per) {
             if (d.interleaved) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[e] = __builtin_amdgcn_alignbit(v[e], v[e], 16);
-            } else if (across) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[e] = (uint32_t)__builtin_amdgcn_mov_dpp((int)v[e], 0x128, 0xF, 0xF, true);      // row_ror:8
             } else {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[e] = (uint32_t)__builtin_amdgcn_ds_bpermute(other, (int)v[e]);
+                for (int e = 0; e < 4; ++e) o[e] = exchange(v[e]);
             }
             if (d.rotary < RP_D)
 #pragma unroll
@@ -160,9 +165,15 @@ __global__ __launch_bounds__(RP_NT) void rope_kernel(RopeDev d, int per) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) r[e] = (_Float16)__builtin_fmaf((float)y[k][e], cw[e], (float)z[e] * sw[e]);
             }
-            if (live) *reinterpret_cast<half8*>(d.out[role] + row * d.out_stride[role] + (at - (role ? d.heads[0] : 0)) * RP_D + ch) = r;
+            if (live) __builtin_nontemporal_store(r, reinterpret_cast<half8*>(d.out[role] + row * d.out_stride[role] + (at - (role ? d.heads[0] : 0)) * RP_D + ch));
         }
     }
+}
+
+// blockIdx: (four rows, heads); a wave has `per` heads.
+template <int AHEAD>
+__global__ __launch_bounds__(RP_NT) void rope_kernel(RopeDev d, int per) {
+    turn_rows<AHEAD>(d, blockIdx.x, ((int)blockIdx.y * RP_WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * per, per);
 }
 
 // ---- with a matrix
@@ -174,24 +185,40 @@ constexpr int RM_FLAT_BYTES = RP_D * (RP_D + 8) * 2;
 constexpr int RM_OUT_PITCH = 2 * RP_D + 16;
 constexpr int RM_STAGE_BYTES = RP_WAVES * RM_GROUPS * RM_OUT_PITCH;
 constexpr int RM_LOOP_AT = RM_FRAG_BYTES, RM_TABLE_AT = RM_LOOP_AT + (RM_FLAT_BYTES > RM_STAGE_BYTES ? RM_FLAT_BYTES : RM_STAGE_BYTES);
-constexpr int RM_LDS = RM_TABLE_AT + 64 * 8 + RP_D * 4;
+constexpr int RM_ANGLES_AT = RM_TABLE_AT + 64 * 8 + RP_D * 4;
 
-// Angles of a position and weights, in LDS.
+// Weights, and what the lanes need of the angles, in LDS: either the turns, and a lane works its 32 angles out, or cosines and sines of all the rows that the
+// groups have, which are few where the heads follow each other: 32 groups of 32 heads have one row, and its 64 angles take a lane one where they would
+// take it 32.
+constexpr int RM_ANGLES = 64 + 2;          // pairs of a row in the table, two of padding
+constexpr int RM_ROWS = 4;                 // rows of a wave's table
+constexpr int RM_LDS_DIRECT = RM_ANGLES_AT, RM_LDS_TABLE = RM_ANGLES_AT + RP_WAVES * RM_ROWS * RM_ANGLES * 8;
 struct RopeTable {
     const uint64_t* turns;
     const float* weights;
+    float2* angles;
 };
-__device__ __forceinline__ RopeTable make_table(const RopeDev& d, int role, unsigned char* smem) {
-    uint64_t* turns = reinterpret_cast<uint64_t*>(smem);
-    float* weights = reinterpret_cast<float*>(smem + 64 * 8);
+__device__ __forceinline__ void fill_table(const RopeDev& d, int role, uint64_t* turns, float* weights) {
     if ((int)threadIdx.x < d.rotary / 2) turns[threadIdx.x] = d.turns[threadIdx.x];
     if (threadIdx.x < RP_D) weights[threadIdx.x] = d.w[role] ? (float)d.w[role][threadIdx.x] : 1.0f;
-    return RopeTable{turns, weights};
+}
+// Angles of rows first .. last, by `threads` threads of which this is number n.
+__device__ __forceinline__ void fill_angles(const RopeDev& d, const uint64_t* turns, float2* angles, int64_t first, int64_t last, int n, int threads) {
+    const int pairs = d.rotary / 2, all = (int)(last - first + 1) * 64;
+    for (int k = n; k < all; k += threads) {
+        const int row = k >> 6, pair = k & 63;
+        if (pair >= pairs) continue;
+        const int position = d.positions[first + row];
+        float2 a;
+        cos_sin(angle_of(position < 0 ? 0u : (uint32_t)position, turns[pair]), a.x, a.y);
+        angles[row * RM_ANGLES + pair] = a;
+    }
 }
 
 // Channels 16 kb + 8 h .. + 7 of a group in rows[kb]: norm and rotation, each number rounded to fp16, which the matrix instructions take.  R: rotary / 32.
-template <int R, bool PAIRS>
-__device__ __forceinline__ void turn_group(u32x4 (&rows)[RM_KB], const RopeTable& table, bool norm, float eps, uint32_t position, int h) {
+// `angles`: of the group's row, or null, and the position says.
+template <int R, bool PAIRS, bool DIRECT>
+__device__ __forceinline__ void turn_group(u32x4 (&rows)[RM_KB], const RopeTable& table, bool norm, float eps, uint32_t position, const float2* angles, int h) {
     float by = 1.0f;
     if (norm) {
         float sum = 0.0f;
@@ -204,6 +231,15 @@ __device__ __forceinline__ void turn_group(u32x4 (&rows)[RM_KB], const RopeTable
         const float* w = table.weights + 16 * kb + 8 * h;
 #pragma unroll
         for (int e = 0; e < 8; ++e) y[e] = norm ? (float)x[e] * w[e] * by : (float)x[e];
+    };
+    auto turn = [&](int pair, float& c, float& s) {
+        if constexpr (DIRECT) {
+            cos_sin(angle_of(position, table.turns[pair]), c, s);
+        } else {
+            const float2 a = angles[pair];
+            c = a.x;
+            s = a.y;
+        }
     };
     auto put = [&](int kb, const float (&y)[8]) {
         half8 o;
@@ -219,7 +255,7 @@ __device__ __forceinline__ void turn_group(u32x4 (&rows)[RM_KB], const RopeTable
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 float c, s;
-                cos_sin(angle_of(position, table.turns[8 * kb + 4 * h + e]), c, s);
+                turn(8 * kb + 4 * h + e, c, s);
                 z[2 * e] = __builtin_fmaf(y[2 * e], c, -y[2 * e + 1] * s);
                 z[2 * e + 1] = __builtin_fmaf(y[2 * e + 1], c, y[2 * e] * s);
             }
@@ -234,7 +270,7 @@ __device__ __forceinline__ void turn_group(u32x4 (&rows)[RM_KB], const RopeTable
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 float c, s;
-                cos_sin(angle_of(position, table.turns[16 * kb + 8 * h + e]), c, s);
+                turn(16 * kb + 8 * h + e, c, s);
                 const float x = a[e], y = b[e];
                 a[e] = __builtin_fmaf(x, c, -y * s);
                 b[e] = __builtin_fmaf(y, c, x * s);
@@ -276,7 +312,7 @@ struct RopeGroups {
     }
 };
 
-template <int R, bool PAIRS>
+template <int R, bool PAIRS, bool DIRECT>
 __global__ __launch_bounds__(RP_NT) __attribute__((amdgpu_waves_per_eu(2))) void rope_matrix_kernel(RopeDev d) {
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     u32x4* Pf = reinterpret_cast<u32x4*>(smem);                                // fragment table
@@ -291,7 +327,7 @@ __global__ __launch_bounds__(RP_NT) __attribute__((amdgpu_waves_per_eu(2))) void
     // A group's row, or the last one's behind the end, and where its output starts (below zero: nowhere)
     struct Block {
         u32x4 rows[RM_KB];
-        int position;
+        int position, from_first;          // rows behind the first group's
         int64_t to;
     };
     auto issue = [&](int64_t block, Block& b) {
@@ -303,6 +339,7 @@ __global__ __launch_bounds__(RP_NT) __attribute__((amdgpu_waves_per_eu(2))) void
 #pragma unroll
         for (int kb = 0; kb < RM_KB; ++kb) b.rows[kb] = from[2 * kb + h];
         b.position = d.positions[row];
+        if constexpr (!DIRECT) b.from_first = (int)(row - __shfl((long long)row, 0));
         b.to = mine < groups.count ? row * d.out_stride[groups.role] + of * RP_D : -1;
     };
 
@@ -314,7 +351,10 @@ __global__ __launch_bounds__(RP_NT) __attribute__((amdgpu_waves_per_eu(2))) void
     u32x4 v[CHUNKS / RP_NT];
 #pragma unroll
     for (int k = 0; k < CHUNKS / RP_NT; ++k) v[k] = reinterpret_cast<const u32x4*>(P)[tid + k * RP_NT];
-    const RopeTable table = make_table(d, groups.role, smem + RM_TABLE_AT);
+    uint64_t* turns = reinterpret_cast<uint64_t*>(smem + RM_TABLE_AT);
+    float* weights = reinterpret_cast<float*>(smem + RM_TABLE_AT + 64 * 8);
+    const RopeTable table{turns, weights, reinterpret_cast<float2*>(smem + RM_ANGLES_AT) + w * RM_ROWS * RM_ANGLES};
+    fill_table(d, groups.role, turns, weights);
 #pragma unroll
     for (int k = 0; k < CHUNKS / RP_NT; ++k) {
         const int q = tid + k * RP_NT;
@@ -338,7 +378,21 @@ __global__ __launch_bounds__(RP_NT) __attribute__((amdgpu_waves_per_eu(2))) void
     auto work = [&](int64_t at, Block& b, Block& far) {
         issue(at + step < blocks ? at + step : blocks - 1, far);
         __builtin_amdgcn_sched_barrier(0);
-        turn_group<R, PAIRS>(b.rows, table, d.w[groups.role] != nullptr, d.eps, b.position < 0 ? 0u : (uint32_t)b.position, h);
+        const uint32_t position = b.position < 0 ? 0u : (uint32_t)b.position;
+        if constexpr (!DIRECT && R > 0) {                                      // a pair a lane, row by row
+            const int rows = __builtin_amdgcn_readlane(b.from_first, RM_GROUPS - 1) + 1;
+            for (int k = 0; k < rows; ++k) {
+                const uint64_t has = __ballot(b.from_first == k && h == 0);    // (rows follow each other: every k has a lane)
+                const uint32_t p = (uint32_t)__builtin_amdgcn_readlane((int)position, has ? __builtin_ctzll(has) : 0);
+                float2 a;
+                cos_sin(angle_of(p, turns[l < 16 * R ? l : 0]), a.x, a.y);
+                if (l < 16 * R && k < RM_ROWS) table.angles[k * RM_ANGLES + l] = a;
+            }
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        }
+        turn_group<R, PAIRS, DIRECT>(b.rows, table, d.w[groups.role] != nullptr, d.eps, position, table.angles + (DIRECT ? 0 : b.from_first) * RM_ANGLES, h);
         f32x16 acc[RM_MT];
 #pragma unroll
         for (int mt = 0; mt < RM_MT; ++mt)
@@ -370,7 +424,7 @@ __global__ __launch_bounds__(RP_NT) __attribute__((amdgpu_waves_per_eu(2))) void
             const int r = (l >> 4) + 4 * k;
             const u32x4 y = *reinterpret_cast<const u32x4*>(stage + r * RM_OUT_PITCH + 16 * (l & 15));
             const int64_t dst = __shfl((long long)to, r);
-            if (dst >= 0) *reinterpret_cast<u32x4*>(out + dst + 8 * (l & 15)) = y;
+            if (dst >= 0) __builtin_nontemporal_store(y, reinterpret_cast<u32x4*>(out + dst + 8 * (l & 15)));
         }
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();                                       // read before the next block overwrites it
@@ -384,15 +438,23 @@ __global__ __launch_bounds__(RP_NT) __attribute__((amdgpu_waves_per_eu(2))) void
     }
 }
 
-// Few groups: a workgroup takes 32 of them, each of its waves 32 of the 128 outputs; its quarter of P goes through a part of LDS of its own.  Same arithmetic
-// in the same order as above: the same bits.
+// Few groups: a workgroup takes 32 of them, each of its waves 32 of the 128 outputs; its quarter of P goes through a part of LDS of its own, the angles of the
+// groups' rows are worked out by all.  Same arithmetic in the same order as above: the same bits.  The workgroups behind those (blockIdx.y = matrices) have the
+// side without a matrix, a head a wave: one launch for both.
 template <int R, bool PAIRS>
-__global__ __launch_bounds__(RP_NT) void rope_matrix_few_kernel(RopeDev d) {
+__global__ __launch_bounds__(RP_NT) void rope_matrix_few_kernel(RopeDev d, RopeDev plain, int matrices) {
     constexpr int PITCH = 32 + 8;
     __shared__ __attribute__((aligned(16))) _Float16 Pw_all[RP_WAVES * RP_D * PITCH];
-    __shared__ __attribute__((aligned(16))) unsigned char tables[64 * 8 + RP_D * 4];
+    __shared__ __attribute__((aligned(16))) uint64_t turns[64];
+    __shared__ __attribute__((aligned(16))) float weights[RP_D];
+    __shared__ __attribute__((aligned(16))) float2 angles[RM_GROUPS * RM_ANGLES];
     const int l = threadIdx.x & 63, c = l & 31, h = l >> 5;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if ((int)blockIdx.y == matrices) {
+        const int heads = plain.heads[0] + plain.heads[1], waves = (heads + RP_WAVES - 1) / RP_WAVES;
+        for (int64_t k = blockIdx.x; k < (plain.T + 3) / 4 * waves; k += gridDim.x) turn_rows<1>(plain, k / waves, (int)(k % waves) * RP_WAVES + w, 1);
+        return;
+    }
     const RopeGroups groups(d, blockIdx.y);
     if ((int64_t)blockIdx.x * RM_GROUPS >= groups.count) return;
     const _Float16* P = groups.matrix() + 32 * w;
@@ -408,11 +470,13 @@ __global__ __launch_bounds__(RP_NT) void rope_matrix_few_kernel(RopeDev d) {
     const u32x4* from = reinterpret_cast<const u32x4*>(d.rows[groups.role] + row * d.stride[groups.role] + of * RP_D);
 #pragma unroll
     for (int kb = 0; kb < RM_KB; ++kb) rows[kb] = from[2 * kb + h];
-    const RopeTable table = make_table(d, groups.role, tables);
+    const int64_t first = __shfl((long long)row, 0), last = __shfl((long long)row, RM_GROUPS - 1);
+    fill_table(d, groups.role, turns, weights);
+    if constexpr (R > 0) fill_angles(d, d.turns, angles, first, last, threadIdx.x, RP_NT);
 #pragma unroll
     for (int k = 0; k < 8; ++k) *reinterpret_cast<u32x4*>(Pw + (16 * k + (l >> 2)) * PITCH + 8 * (l & 3)) = v[k];
     __syncthreads();
-    turn_group<R, PAIRS>(rows, table, d.w[groups.role] != nullptr, d.eps, position < 0 ? 0u : (uint32_t)position, h);
+    turn_group<R, PAIRS, false>(rows, RopeTable{turns, weights, angles}, d.w[groups.role] != nullptr, d.eps, 0u, angles + (int)(row - first) * RM_ANGLES, h);
     f32x16 acc;
 #pragma unroll
     for (int r = 0; r < 16; ++r) acc[r] = 0.0f;
@@ -430,22 +494,41 @@ __global__ __launch_bounds__(RP_NT) void rope_matrix_few_kernel(RopeDev d) {
     }
 }
 
+// Rows of 32 groups at most.
+static int rows_of_groups(const RopeDev& d) {
+    if (d.per_head) return RM_GROUPS;
+    int heads = 1 << 30;
+    for (int x = 0; x < 2; ++x)
+        if (d.rows[x] && d.heads[x] < heads) heads = d.heads[x];
+    return RM_GROUPS % heads == 0 ? RM_GROUPS / heads : (RM_GROUPS - 1) / heads + 2;
+}
+// `done`: whether the side without a matrix went along.
 template <int R, bool PAIRS>
-static hipError_t rope_matrix_launch(const RopeDev& d, hipStream_t stream) {
+static hipError_t rope_matrix_launch(const RopeDev& d, const RopeDev& plain, bool& done, hipStream_t stream) {
     const unsigned matrices = d.per_head ? (unsigned)(d.heads[0] + d.heads[1]) : (unsigned)((d.rows[0] != nullptr) + (d.rows[1] != nullptr));
     const int64_t most = d.per_head ? d.T : d.T * (d.heads[0] > d.heads[1] ? d.heads[0] : d.heads[1]);
     const int64_t blocks = (most + RM_GROUPS - 1) / RM_GROUPS;
-    if (blocks * matrices <= 2 * cu_count())
-        return launch(rope_matrix_few_kernel<R, PAIRS>, dim3((unsigned)blocks, matrices), dim3(RP_NT), 0, stream, d);
-    static OccCache cache;
-    int occ = 0;
-    const hipError_t e = kernel_occupancy(reinterpret_cast<const void*>(rope_matrix_kernel<R, PAIRS>), RP_NT, RM_LDS, cache, occ);
-    if (e != hipSuccess) return e;
-    const int64_t need = (blocks + RP_WAVES - 1) / RP_WAVES;
-    int64_t gx = ((int64_t)cu_count() * occ + matrices - 1) / matrices;
-    const int64_t rounds = (need + gx - 1) / gx;
-    gx = (need + rounds - 1) / rounds;
-    return launch(rope_matrix_kernel<R, PAIRS>, dim3((unsigned)gx, matrices), dim3(RP_NT), RM_LDS, stream, d);
+    // Up to two workgroups a CU (one where each head has a matrix and its rows' angles for itself) the kernel for few.  us, few / many: 300 rows of 32 + 8 heads through one matrix
+    // 8.9 / 11.6, 500 10.9 / 12.0, 777 17.1 / 13.8; through one each 64 8.1 / -, 200 11.7 / 9.9, 300 12.0 / 10.7.
+    done = blocks * matrices <= (d.per_head ? 1 : 2) * cu_count();
+    if (done) {
+        const bool both = plain.heads[0] + plain.heads[1] > 0;
+        return launch(rope_matrix_few_kernel<R, PAIRS>, dim3((unsigned)blocks, matrices + both), dim3(RP_NT), 0, stream, d, plain, (int)matrices);
+    }
+    auto many = [&](auto kernel, int lds, OccCache& cache) {
+        int occ = 0;
+        const hipError_t e = kernel_occupancy(reinterpret_cast<const void*>(kernel), RP_NT, lds, cache, occ);
+        if (e != hipSuccess) return e;
+        const int64_t need = (blocks + RP_WAVES - 1) / RP_WAVES;
+        int64_t gx = ((int64_t)cu_count() * occ + matrices - 1) / matrices;
+        const int64_t rounds = (need + gx - 1) / gx;
+        gx = (need + rounds - 1) / rounds;
+        return launch(kernel, dim3((unsigned)gx, matrices), dim3(RP_NT), lds, stream, d);
+    };
+    static OccCache caches[2];
+    // (8192 rows of 32 + 8 heads: 52.7 us with the table, 58.0 without)
+    if (rows_of_groups(d) <= RM_ROWS) return many(rope_matrix_kernel<R, PAIRS, false>, RM_LDS_TABLE, caches[0]);
+    return many(rope_matrix_kernel<R, PAIRS, true>, RM_LDS_DIRECT, caches[1]);
 }
 
 hipError_t rope_launch(const RopeDev& all, hipStream_t stream) {
@@ -459,25 +542,28 @@ hipError_t rope_launch(const RopeDev& all, hipStream_t stream) {
     if (through.rows[0] || through.rows[1]) {
         const int r = all.rotary / 32;
         const bool pairs = all.interleaved && r > 0;
+        bool done = false;
         hipError_t e = hipErrorInvalidValue;
         switch (2 * r + pairs) {
-            case 0: e = rope_matrix_launch<0, false>(through, stream); break;
-            case 2: e = rope_matrix_launch<1, false>(through, stream); break;
-            case 3: e = rope_matrix_launch<1, true>(through, stream); break;
-            case 4: e = rope_matrix_launch<2, false>(through, stream); break;
-            case 5: e = rope_matrix_launch<2, true>(through, stream); break;
-            case 6: e = rope_matrix_launch<3, false>(through, stream); break;
-            case 7: e = rope_matrix_launch<3, true>(through, stream); break;
-            case 8: e = rope_matrix_launch<4, false>(through, stream); break;
-            case 9: e = rope_matrix_launch<4, true>(through, stream); break;
+            case 0: e = rope_matrix_launch<0, false>(through, plain, done, stream); break;
+            case 2: e = rope_matrix_launch<1, false>(through, plain, done, stream); break;
+            case 3: e = rope_matrix_launch<1, true>(through, plain, done, stream); break;
+            case 4: e = rope_matrix_launch<2, false>(through, plain, done, stream); break;
+            case 5: e = rope_matrix_launch<2, true>(through, plain, done, stream); break;
+            case 6: e = rope_matrix_launch<3, false>(through, plain, done, stream); break;
+            case 7: e = rope_matrix_launch<3, true>(through, plain, done, stream); break;
+            case 8: e = rope_matrix_launch<4, false>(through, plain, done, stream); break;
+            case 9: e = rope_matrix_launch<4, true>(through, plain, done, stream); break;
         }
-        if (e != hipSuccess) return e;
+        if (e != hipSuccess || done) return e;
     }
     const int heads = plain.heads[0] + plain.heads[1];
     if (heads == 0) return hipSuccess;
     const int64_t blocks = (plain.T + 3) / 4;
+    // Heads of a wave, which works the angles of its four rows out for all of them: as many as leave 2048 waves, two a SIMD, and 8 at most.  us with 1024 / 2048 / 4096 waves left:
+    // 777 rows of 40 heads 7.6 / 6.8 / 7.3, 1500 14.1 / 10.9 / 10.3, 512 of 64 8.6 / 7.5 / 7.4; with 4 / 8 / 16 heads at most: 16384 of 40 64.7 / 59.7 / 66.9, 4096 18.3 / 16.9 / 16.6.
     int per = 1;
-    while (per < 16 && blocks * ((heads + 2 * per - 1) / (2 * per)) >= 4096) per *= 2;
+    while (per < 8 && blocks * ((heads + 2 * per - 1) / (2 * per)) >= 2048) per *= 2;
     const dim3 grid((unsigned)blocks, (unsigned)((heads + RP_WAVES * per - 1) / (RP_WAVES * per)));
     if (per == 1) return launch(rope_kernel<1>, grid, dim3(RP_NT), 0, stream, plain, per);
     if (per == 2) return launch(rope_kernel<2>, grid, dim3(RP_NT), 0, stream, plain, per);
