@@ -8,8 +8,9 @@
 // counted in memory.  Entries that change are dealt out to its threads evenly (a thread finds the sequence of its entry by bisection in LDS), as
 // one sequence may have most of them.
 //
-// Bound by latency: loads of a chunk, one running sum in LDS, ring to table, rows.  Rows of more than a few thousand tokens are worked out by a second
-// kernel on all CUs, whose stores bound it.
+// Bound by latency, and on its one CU by the instructions of an entry: 64 decoding sequences 4.7 us (replayed; a launch, the sequences' loads, three running sums, rows), 512 in mixed states
+// (1150 pages taken, 15800 given back) 10.5 and 4 for their 18500 rows, 16 prompts of 65536 tokens (42900 pages, 686000 rows) 11.5 and 6.  Rows of more than a few
+// thousand tokens are worked out by a second kernel on all CUs.
 #include "fq_internal.h"
 #include "fq_cache_device.h"
 
@@ -208,6 +209,7 @@ __global__ __launch_bounds__(ADV_NT) void advance_kernel(AdvanceDev a) {
                         if (x0 + 64 * k + l < takes) a.page_table[place[k]] = page[k];
                 }
             };
+            // 1200 entries 6.7 us one at a time by a thread, 7.9 eight at a time; 2700 7.5 / 8.1, 5700 8.7 / 8.7, 42900 23.4 / 17.7
             if (takes <= 4 * ADV_NT) take(std::integral_constant<int, 1>{});
             else take(std::integral_constant<int, 8>{});
             taken_before += enough ? takes : 0;
@@ -244,8 +246,9 @@ __global__ __launch_bounds__(ADV_NT) void advance_kernel(AdvanceDev a) {
                     released += all;
                 }
             };
+            // (of 2000 entries 9.9 us one at a time by a thread, 8.3 four, 11.7 sixteen; of 15800 23.7, 14.9 and 14.6)
             if (gone <= ADV_NT) give(std::integral_constant<int, 1>{});
-            else give(std::integral_constant<int, 16>{});
+            else give(std::integral_constant<int, 4>{});
         }
         rows_before = rows_behind;
         if constexpr (ROWS) {
@@ -332,6 +335,7 @@ __global__ __launch_bounds__(256) void advance_rows_kernel(AdvanceDev a) {
 
 hipError_t advance_launch(const AdvanceDev& a, hipStream_t stream) {
     const bool maps = (a.positions || a.slots) && a.T > 0;
+    // The rows in the same kernel, or in one of their own?  us: 64 sequences of a row 4.7 / 6.1, 8 of 300 rows 5.1 / 6.7, of 600 5.9 / 7.2, of 2000 11.1 / 6.6, of 6000 24.5 / 6.9.
     if (maps && a.B <= ADV_NT && a.T <= 4 * ADV_NT) return launch(advance_kernel<true>, dim3(1), dim3(ADV_NT), 0, stream, a);
     const hipError_t e = launch(advance_kernel<false>, dim3(1), dim3(ADV_NT), 0, stream, a);
     if (e != hipSuccess || !maps) return e;

@@ -509,8 +509,8 @@ struct FewRows {
 };
 // Rows row0 .. row_end - 1 (16 NT at most) of head `head` of sequence b over steps [x_begin, x_end) of their span.  The result is the output, or (partial) what
 // the join needs, rows from partial_at on.
-// V > 1 (scores that cost more than the products: ScoredDev): there are 16 / V rows at most, each is in V of the 16 columns, and each of these columns takes the scores of
-// one V-th of the tokens, with a reference and sums of its own, weights of zero for the others: the work of a score is done by all lanes instead of those that
+// V = 2 (scores that cost more than the products: ScoredDev): there are 8 rows at most, each is in two of the 16 columns, and each of these takes the scores of
+// half of the tokens, with a reference and sums of its own and weights of zero for the others: the work of a score is done by all lanes instead of those that
 // have a row.  The columns meet behind the last step.
 template <int KB, int VB, int NT, int NW, int V, typename DEV>
 __device__ __forceinline__ void few_rows(const DEV& p, unsigned char* smem, int b, int head, const Sequence& seq, int row0, int row_end, const Span& span,
@@ -641,16 +641,15 @@ __device__ __forceinline__ void few_rows(const DEV& p, unsigned char* smem, int 
             return pages_ok && k0 + ATT_STEP - 1 <= all_see && k0 + ATT_STEP <= span.end && (p.window <= 0 || p.visible || k0 > pos_hi - p.window);
         };
         if constexpr (V > 1) {
-            constexpr int N = 8 / V;                                           // tokens of a lane, one behind the other
-            const int part = i / (16 / V), tile = V == 2 ? part : part >> 1, first = 16 * tile + 4 * g + (V == 2 ? 0 : 2 * (part & 1));
-            typedef uint32_t words __attribute__((ext_vector_type(N)));
-            const words kp = *reinterpret_cast<const words*>(slot + R::P_AT + 4 * first), v = *reinterpret_cast<const words*>(slot + R::P_AT + 128 + 4 * first);
+            static_assert(V == 2 && NT == 1, "columns 8 further on have the second 16 tokens");
+            constexpr int N = 4;                                               // tokens of a lane, one behind the other
+            const int tile = i / 8, first = 16 * tile + 4 * g;
+            const u32x4 kp = *reinterpret_cast<const u32x4*>(slot + R::P_AT + 4 * first), v = *reinterpret_cast<const u32x4*>(slot + R::P_AT + 128 + 4 * first);
             float s[N], prod[N], sum;
             uint32_t vp[N];
 #pragma unroll
             for (int k = 0; k < N; ++k) {
-                float x = tile ? sc[0][1][k] : sc[0][0][k];
-                if constexpr (V == 4) x = part & 1 ? (tile ? sc[0][1][2 + k] : sc[0][0][2 + k]) : x;
+                const float x = tile ? sc[0][1][k] : sc[0][0][k];
                 s[k] = if_finite(times_step(kp[k], __builtin_fmaf((float)zero_bits(kp[k]), q_sum[0], x)) * factor[0]);
                 vp[k] = v[k];
             }
@@ -684,8 +683,8 @@ __device__ __forceinline__ void few_rows(const DEV& p, unsigned char* smem, int 
                 const uint32_t two = as_u32(half2v{(_Float16)prod[2 * k], (_Float16)prod[2 * k + 1]});
                 zeros[0] = zero_sum<0>(two, vp[2 * k], zeros[0]);
                 zeros[0] = zero_sum<1>(two, vp[2 * k + 1], zeros[0]);
-#pragma unroll
-                for (int m = 0; m < V; ++m) pp[N / 2 * m + k] = part == m ? two : 0u;
+                pp[k] = tile ? 0u : two;
+                pp[2 + k] = tile ? two : 0u;
             }
             pw[0] = __builtin_bit_cast(half8, pp);
         } else {
@@ -799,15 +798,12 @@ __device__ __forceinline__ void few_rows(const DEV& p, unsigned char* smem, int 
     }
 
     if constexpr (V > 1) {                                                     // the columns of a row meet
-        float top = __builtin_fmaxf(ref[0], dpp_move<0x128>(ref[0]));          // row_ror:8
-        if constexpr (V == 4) top = __builtin_fmaxf(top, dpp_move<0x124>(top));
+        const float top = __builtin_fmaxf(ref[0], dpp_move<0x128>(ref[0]));    // row_ror:8
         const float f = __builtin_amdgcn_exp2f(ref[0] - top);
         ref[0] = top;
         auto meet = [&](float x) {
             x *= f;
-            x += dpp_move<0x128>(x);
-            if constexpr (V == 4) x += dpp_move<0x124>(x);                     // row_ror:4
-            return x;
+            return x + dpp_move<0x128>(x);
         };
         total[0] = meet(total[0]);
         zeros[0] = meet(zeros[0]);
@@ -1580,7 +1576,8 @@ static hipError_t attention_launch_bits(const DEV& d, const AttnPlan& plan, int6
     if (plan.tile_rows == 16) {
         if constexpr (kScored<DEV>) {
             const int64_t rows = max_rows * d.G;
-            if (rows <= 4) return few_rows_launch<KB, VB, 1, 4>(d, plan, max_rows, stream);
+            // us, one column a row / two: 64 sequences of 4096, 8 heads of 1, 4 and 8 queries, capped 54.1 / 49.5, 52.5 / 48.5, 52.7 / 49.3, with slopes 51.4 / 47.5, 51.9 / 47.7,
+            // 52.5 / 48.5; 1 of 1000 11.8 / 11.0 and 10.8 / 10.1.  (Four columns for four rows: as two.)
             if (rows <= 8) return few_rows_launch<KB, VB, 1, 2>(d, plan, max_rows, stream);
         }
         return few_rows_launch<KB, VB, 1, 1>(d, plan, max_rows, stream);
