@@ -344,8 +344,8 @@ typedef struct fq_page_pool {
  *   batch->page_table     entries P(held) .. P(length) - 1 of every sequence: pages from the ring in the order of the sequences and their entries.  If the ring has fewer
  *          than the call takes, none is taken: the entries become -1 (no page: such tokens are not written and not visible) and next[2] says how many are
  *          missing; a program gives others back and makes the call again with the same held, keep and rows.
- *          Entries P(length) .. P(held) - 1 are put into the ring in the same order, but for those that are no page, and can be taken from the next call on.  No entry is
- *          changed but those that get a page or -1.
+ *          Entries P(length) .. P(held) - 1 are put into the ring in the same order, but for those that are no page, and can be taken from the next call on (so they have to be
+ *          the sequence's own: pages that it shares are for the program to give back).  No entry is changed but those that get a page or -1.
  *   positions  i32 [T], slots i64 [T], either NULL: position of every row, and page * page_tokens + position % page_tokens; -1 for rows behind the last sequence, slots
  *          also for a token that has no page.
  * The batch's arrays are written here, max_rows and max_length are not looked at.  page_tokens and pages are those of the cache; page_tokens a power of two, 16 .. 1024.
@@ -362,7 +362,7 @@ fq_status flatquant_cache_advance(const fq_kv_batch* batch, const fq_page_pool* 
  *         interleaved 0: channels a = i, b = i + rotary / 2;   1: a = 2 i, b = 2 i + 1;   channels from rotary on stay as they are
  *     out = fp16( y ),  or with a matrix  fp16( fp16( y ) P ), fp32 accumulation, as flatquant_head_transform has it.
  *   q, k, q_out, k_out  fp16 [T, Hq or H, 128], rows a stride of halves apart (multiples of 8, >= 128 Hq or 128 H; both may lie in the rows of one fused product),
- *              16-byte aligned; outputs overlap nothing.  q or k may be NULL (then nothing of that side is looked at).
+ *              16-byte aligned; outputs overlap nothing, nor do their rows lie between rows of another tensor.  q or k may be NULL (then nothing of that side is looked at).
  *   positions  i32 [T]; a row whose position is negative is no token: its outputs are left as they are.
  *   turns      u64 [rotary / 2], 16-byte aligned (fq_rope_turns makes them); NULL if rotary is 0.  The angle is exact to 2^-32 of a turn at every position.
  *   rotary     0, 32, 64, 96 or 128.

@@ -472,6 +472,9 @@ static fq_status cache_attention(const fq_kv_cache* cache, const fq_kv_batch* ba
     if (plan.workspace > 0 && (fq::overlap(workspace, plan.workspace, out, obytes) || fq::overlap(workspace, plan.workspace, q, qbytes) ||
                                in_cache(cache, batch, workspace, plan.workspace) || (tree && fq::overlap(visible, batch->T * 8, workspace, plan.workspace))))
         return FQ_INVALID_ARG;
+    if (scores)
+        for (const Bytes& x : {Bytes{scores->slopes, Hq * 4LL}, Bytes{scores->prefix, batch->B * 4}})
+            if (meet(x, Bytes{out, obytes}) || meet(x, Bytes{workspace, plan.workspace})) return FQ_INVALID_ARG;
     fq::AttnArgs a;
     a.q = static_cast<const _Float16*>(q); a.out = static_cast<_Float16*>(out); a.q_stride = q_stride; a.out_stride = out_stride;
     a.Hq = Hq; a.scale = scale; a.window = window; a.sinks = sinks; a.visible = visible; a.workspace = static_cast<float*>(workspace);
@@ -496,15 +499,6 @@ fq_status flatquant_cache_scored_attention(const fq_kv_cache* cache, const fq_kv
                                            void* out, int64_t out_stride, void* workspace, int64_t workspace_bytes, void* stream) {
     if (!(cap >= 0.0f) || !std::isfinite(cap) || (visible && (slopes || prefix || window != 0 || sinks != 0))) return FQ_INVALID_ARG;
     if (off(slopes, 4) || off(prefix, 4)) return FQ_MISALIGNED;
-    if (batch && batch->B > 0 && batch->T > 0 && Hq > 0 && Hq <= (1 << 24) && batch->T <= 0x7fffff00LL / Hq && batch->B <= 0xffffff && out) {
-        const Bytes read[] = {{slopes, Hq * 4LL}, {prefix, batch->B * 4}};
-        const int64_t row = 128LL * Hq, most = (1LL << 48) / batch->T;
-        const Bytes written[] = {{out, out_stride >= row && out_stride <= most ? ((batch->T - 1) * out_stride + row) * 2 : 0},
-                                 {workspace, workspace_bytes > 0 ? workspace_bytes : 0}};
-        for (const Bytes& a : written)
-            for (const Bytes& b : read)
-                if (meet(a, b)) return FQ_INVALID_ARG;
-    }
     const fq::ScoreArgs scores{cap, slopes, prefix};
     return cache_attention(cache, batch, q, q_stride, Hq, scale, window, sinks, visible, visible != nullptr, &scores, out, out_stride, workspace,
                            workspace_bytes, stream);

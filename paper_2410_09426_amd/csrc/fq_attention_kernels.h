@@ -72,13 +72,15 @@ __device__ __forceinline__ float outcome(float x) {
     if constexpr (kScored<DEV>) return if_finite(x);
     return x;
 }
-// Step x of a span of `steps`, in the order that the scores ask for: with slopes the last one first, where the scores are highest, so that references need not be raised
-// at every step (2048 rows at 8192 tokens 1110 -> 560 us).
+// Whether a span's steps are gone through from the last one on: with slopes, whose scores are highest there, so that references need not be raised at every step
+// (2048 rows at 8192 tokens 1110 -> 560 us).  A step behind the last one in this order has tokens below zero.
 template <typename DEV>
-__device__ __forceinline__ int in_order(const DEV& p, int steps, int x) {
-    if constexpr (kScored<DEV>) return p.slopes ? steps - 1 - x : x;
-    return x;
+__device__ __forceinline__ bool backwards(const DEV& p) {
+    if constexpr (kScored<DEV>) return p.slopes != nullptr;
+    return false;
 }
+template <typename DEV>
+__device__ __forceinline__ int in_order(const DEV& p, int steps, int x) { return backwards(p) ? steps - 1 - x : x; }
 // Tokens of sequence b that all of its rows see, wherever they are.
 template <typename DEV>
 __device__ __forceinline__ int prefix_of(const DEV& p, int b) {
@@ -441,8 +443,8 @@ __device__ __forceinline__ float zero_sum(uint32_t pair, uint32_t params, float 
 // Scores of N tokens (all factors taken in; none infinite), capped and lowered; `distance(k)` is the token's position less the row's.  What is no number stays none.
 //   cap tanh(x / cap) = cap - 2 cap / (1 + e^(2 x / cap)): the exponent of 2 is what comes in, the cap alone is a constant of the row, which weights do not depend on, and the
 //   rest goes on in units of 2 cap: an exponential, an addition and a reciprocal.  It is off by 2^-21 of the cap, whatever the score.
-//   Caps beyond kLargeCap take the series of tanh below a quarter instead, so that the error is 2^-19 of the score there.  That takes twice the time of all the rest of a
-//   step (2048 rows at 8192 tokens 670 / 930 us), and up to there the error is below 2^-13, a quarter of what the weights are rounded by.
+//   Caps beyond kLargeCap take the series of tanh below a quarter instead, so that the error is 2^-19 of the score there (2048 rows at 8192 tokens 670 us, so 930); up to
+//   there it is below 2^-13, a quarter of what the weights are rounded by.
 constexpr float kLargeCap = 256.0f;        // base 2
 template <int N, typename Distance>
 __device__ __forceinline__ void rescore(const ScoredDev& p, float (&score)[N], float slope, Distance distance) {
@@ -1186,7 +1188,7 @@ __global__ __launch_bounds__(64 * NW, 2) void shared_attention_kernel(DEV p) {
         float ref = ATT_NONE, total = 0.0f, slope = 0.0f;
         if constexpr (kScored<DEV>) slope = slope_of(p, head * p.G + sub);
 
-        const int lower = in_order(p, 1, 0) == in_order(p, 2, 0) ? 0 : 1;      // which of two steps has the lower tokens
+        const int lower = backwards(p) ? 1 : 0;                                // which of two steps has the lower tokens
         // codes of steps x and x + 1 of the span, 32 tokens each, which need not follow each other
         // The page of tokens 16 n .. of the step from x on, by every lane n of NW: looked up in all lanes at once (a scalar look-up each took more time than the
         // conversion), a step before the loads that follow it, in whose queue it stands.

@@ -173,7 +173,8 @@ __device__ __forceinline__ void turn_rows(const RopeDev& d, int64_t block, int f
 // blockIdx: (four rows, heads); a wave has `per` heads.
 template <int AHEAD>
 __global__ __launch_bounds__(RP_NT) void rope_kernel(RopeDev d, int per) {
-    turn_rows<AHEAD>(d, blockIdx.x, ((int)blockIdx.y * RP_WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * per, per);
+    const int first = ((int)blockIdx.y * RP_WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * per;
+    for (int64_t block = blockIdx.x; 4 * block < d.T; block += gridDim.x) turn_rows<AHEAD>(d, block, first, per);
 }
 
 // ---- with a matrix
@@ -531,6 +532,7 @@ static hipError_t rope_matrix_launch(const RopeDev& d, const RopeDev& plain, boo
     return many(rope_matrix_kernel<R, PAIRS, true>, RM_LDS_DIRECT, caches[1]);
 }
 
+constexpr int64_t kMostBlocks = 1 << 20;   // (a grid has less than 2^32 threads)
 hipError_t rope_launch(const RopeDev& all, hipStream_t stream) {
     RopeDev plain = all, through = all;
     for (int x = 0; x < 2; ++x) {
@@ -564,7 +566,7 @@ hipError_t rope_launch(const RopeDev& all, hipStream_t stream) {
     // 777 rows of 40 heads 7.6 / 6.8 / 7.3, 1500 14.1 / 10.9 / 10.3, 512 of 64 8.6 / 7.5 / 7.4; with 4 / 8 / 16 heads at most: 16384 of 40 64.7 / 59.7 / 66.9, 4096 18.3 / 16.9 / 16.6.
     int per = 1;
     while (per < 8 && blocks * ((heads + 2 * per - 1) / (2 * per)) >= 2048) per *= 2;
-    const dim3 grid((unsigned)blocks, (unsigned)((heads + RP_WAVES * per - 1) / (RP_WAVES * per)));
+    const dim3 grid((unsigned)(blocks < kMostBlocks ? blocks : kMostBlocks), (unsigned)((heads + RP_WAVES * per - 1) / (RP_WAVES * per)));
     if (per == 1) return launch(rope_kernel<1>, grid, dim3(RP_NT), 0, stream, plain, per);
     if (per == 2) return launch(rope_kernel<2>, grid, dim3(RP_NT), 0, stream, plain, per);
     return launch(rope_kernel<4>, grid, dim3(RP_NT), 0, stream, plain, per);

@@ -53,7 +53,7 @@ class Step:
     def run(self, in_place=False, maps="ps", stream=None):
         st = stream or torch.cuda.current_stream()
         big = lambda n, t: torch.full((GUARD + n + GUARD,), -99, dtype=t, device="cuda")      # noqa: E731
-        starts, lengths, ring = big(self.B + 1, torch.int32), big(self.B, torch.int32), big(self.pages, torch.int32)
+        starts, lengths, ring = big(self.B + 1, torch.int32), big(self.B, torch.int32), big(len(self.ring), torch.int32)
         positions, slots, nxt = big(self.T, torch.int32), big(self.T, torch.int64), big(3, torch.int64)
         view = lambda x: x[GUARD:-GUARD]                                                      # noqa: E731
         view(ring).copy_(_i32(self.ring))
@@ -66,7 +66,7 @@ class Step:
             if self.keep == self.held:
                 keep = held
         batch = fq.KvBatch(view(starts), view(lengths), table, self.B, self.T, self.width, self.table.shape[1], 1, 1)
-        pool = fq.PagePool(view(ring), state, view(nxt), self.pages)
+        pool = fq.PagePool(view(ring), state, view(nxt), len(self.ring))
         fq.flatquant_cache_advance(batch, pool, self.page, self.pages, held, keep, rows, view(positions) if "p" in maps else None,
                                    view(slots) if "s" in maps else None, stream=st)
         torch.cuda.synchronize()
@@ -168,6 +168,26 @@ def test_a_ring_that_has_too_few_pages(B):
     s.check()
     s = Step(19, held, keep, rows, spare=0)                                    # just enough
     assert s.expect()[2][2] == 0
+    s.check()
+
+
+@pytest.mark.parametrize("more", [1, 7, 5000])
+def test_rings_with_more_places_than_pages(more):
+    print(f"[case] ring + {more}", flush=True)
+    s = Step(25, *_mixed(25, 100))
+    free = [int(s.ring[i % s.pages]) for i in range(s.taken, s.given)]
+    s.ring = np.full(s.pages + more, -3, dtype=np.int32)
+    for i, p in enumerate(free):
+        s.ring[(s.taken + i) % len(s.ring)] = p
+    s.check()
+
+
+def test_a_ring_of_one_page():
+    print("[case] one page", flush=True)
+    s = Step(26, [0], [0], [5], spare=0)
+    assert s.pages == 1
+    s.check()
+    s = Step(27, [5], [0], [0], spare=0)
     s.check()
 
 

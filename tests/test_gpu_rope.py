@@ -181,6 +181,25 @@ def test_launch_forms_give_the_same_rows():
         assert all(np.array_equal(a[:21], b) for a, b in zip(whole, part)), P
 
 
+def test_more_rows_than_a_grid_has():
+    """2^22 rows and more: workgroups take several blocks; the last rows and some others against those of a short call."""
+    print("[case] 2^22 + 77 rows", flush=True)
+    T = 2 ** 22 + 77
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(3)
+    x = torch.randn((T, D), generator=gen, device="cuda", dtype=torch.float16)
+    pos = torch.randint(0, 2 ** 20, (T,), generator=gen, device="cuda", dtype=torch.int32)
+    turns = torch.from_numpy(fq.fq_rope_turns([10000.0 ** (-2 * i / D) for i in range(D // 2)]).view(np.int64)).cuda()
+    out = torch.full((T, D), -7.25, dtype=torch.float16, device="cuda")
+    call = lambda x, pos, out: fq.flatquant_head_rope(x, D, 1, None, 0, 0, len(x), pos, turns, D, 0, None, None, 0.0, None, None, 0, out, D, None, 0,      # noqa: E731
+                                                      stream=torch.cuda.current_stream())
+    call(x, pos, out)
+    for rows in (slice(0, 500), slice(2 ** 22 - 250, 2 ** 22 + 77), slice(2 ** 21, 2 ** 21 + 100)):
+        part = torch.empty_like(out[rows])
+        call(x[rows].contiguous(), pos[rows].contiguous(), part)
+        assert torch.equal(part, out[rows])
+
+
 def test_the_matrix_is_that_of_the_head_transform():
     """Without norm and rotation: the bits of flatquant_head_transform."""
     print("[case] head transform", flush=True)

@@ -105,8 +105,10 @@ def test_scored_attention_refuses():
     assert _scored(batch=dict(max_rows=65), visible=FAR + 0x300000, slopes=None, prefix=None, **work) == fq.FQ_UNSUPPORTED_SHAPE
     for bad in (dict(slopes=FAR + 0x200002), dict(prefix=FAR + 0x201001), dict(visible=FAR + 0x300004, slopes=None, prefix=None), dict(out=FAR + 0x100008)):
         assert _scored(**{**work, **bad}) == fq.FQ_MISALIGNED, bad
+    long = dict(batch=dict(T=16, max_rows=8, max_length=4000, table_width=256, table_stride=256))      # rows that need a workspace
+    assert fq.fq_cache_attention_workspace(fq.KvCache(**CACHE), fq.KvBatch(**{**BATCH, **long["batch"]}), 8) > 4096
     for bad in (dict(slopes=FAR + 0x100010), dict(prefix=FAR + 0x100004), dict(slopes=FAR + 0x800000), dict(prefix=FAR + 0x800004), dict(out=FAR)):
-        assert _scored(**{**work, **bad}) == fq.FQ_INVALID_ARG, bad
+        assert _scored(**{**work, **long, **bad}) == fq.FQ_INVALID_ARG, bad
     assert fq.flatquant_cache_scored_attention(None, fq.KvBatch(**{**BATCH, "T": 3}), FAR, 1024, 8, 0.1, 0.0, None, None, 0, 0, None, FAR, 1024, None, 0,
                                                check=False) == fq.FQ_INVALID_ARG
     assert fq.flatquant_cache_scored_attention(fq.KvCache(**CACHE), None, FAR, 1024, 8, 0.1, 0.0, None, None, 0, 0, None, FAR, 1024, None, 0,
