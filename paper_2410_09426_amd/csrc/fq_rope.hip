@@ -10,8 +10,8 @@
 // once for all of them, four pairs a lane (the lane that holds the pairs' other numbers has the other four), and the weights go into the cosines and sines.  Bound by memory:
 // 16384 rows of 40 heads (336 MB) in 60 us; 64 rows in 3.4, a launch and two loads one after the other.  Stores past the caches: 4096 rows of 40 heads 22.5 -> 16.9 us.
 // With one: 32 groups a wave as the columns of v_mfma_f32_32x32x16_f16, as they come from memory: a lane holds 8 channels of every 16 of its group, both of
-// every pair, so that it turns them in its registers before they are the right operand.  8192 rows of 32 + 8 heads (168 MB, 8.6 GFLOP) through one matrix in 46 us, 33 of
-// them memory at a copy's rate; through one each 76, as every group's angles are worked out for it alone, 32 a lane, which takes more than the products.
+// every pair, so that it turns them in its registers before they are the right operand.  8192 rows of 32 + 8 heads (168 MB, 8.6 GFLOP) through one matrix in 39 us, 33 of
+// them memory at a copy's rate; through one each 77, as every group's angles are worked out for it alone, 32 a lane, which takes more than the products.
 #include "fq_internal.h"
 #include "fq_device.h"
 #include "fq_cache_device.h"
@@ -314,7 +314,7 @@ struct RopeGroups {
 };
 
 template <int R, bool PAIRS, bool DIRECT>
-__global__ __launch_bounds__(RP_NT) __attribute__((amdgpu_waves_per_eu(2))) void rope_matrix_kernel(RopeDev d) {
+__global__ __launch_bounds__(RP_NT) __attribute__((amdgpu_waves_per_eu(2))) void rope_matrix_kernel(RopeDev d, RopeDev plain) {
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     u32x4* Pf = reinterpret_cast<u32x4*>(smem);                                // fragment table
     _Float16* Pflat = reinterpret_cast<_Float16*>(smem + RM_LOOP_AT);          // prologue only
@@ -323,7 +323,21 @@ __global__ __launch_bounds__(RP_NT) __attribute__((amdgpu_waves_per_eu(2))) void
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const RopeGroups groups(d, blockIdx.y);
     const int64_t blocks = (groups.count + RM_GROUPS - 1) / RM_GROUPS, step = (int64_t)gridDim.x * RP_WAVES;
-    if ((int64_t)blockIdx.x * RP_WAVES >= blocks) return;
+    // The side without a matrix goes along, eight heads of four rows at a time by a wave, the last workgroups first, some of which may have nothing else to do: at the start in one
+    // half of the workgroups, at the end in the other, so that what is bound by memory runs beside what has products to do (8192 rows of 32 + 8 heads 38.8 us; in two launches 41.3).
+    const int plain_heads = plain.heads[0] + plain.heads[1], chunks = (plain_heads + 7) / 8;
+    auto turn_plain = [&] {
+        const int64_t all = plain_heads > 0 ? (plain.T + 3) / 4 * chunks : 0;
+        const int64_t waves = (int64_t)gridDim.x * gridDim.y * RP_WAVES;
+        for (int64_t k = waves - 1 - (((int64_t)blockIdx.x * gridDim.y + blockIdx.y) * RP_WAVES + w); k < all; k += waves)
+            turn_rows<4>(plain, k / chunks, (int)(k % chunks) * 8, 8);
+    };
+    const bool plain_first = 2 * blockIdx.x < gridDim.x;
+    if (plain_first) turn_plain();
+    if ((int64_t)blockIdx.x * RP_WAVES >= blocks) {
+        if (!plain_first) turn_plain();
+        return;
+    }
 
     // A group's row, or the last one's behind the end, and where its output starts (below zero: nowhere)
     struct Block {
@@ -437,6 +451,7 @@ __global__ __launch_bounds__(RP_NT) __attribute__((amdgpu_waves_per_eu(2))) void
         work(block, nxt, cur);
         block += step;
     }
+    if (!plain_first) turn_plain();
 }
 
 // Few groups: a workgroup takes 32 of them, each of its waves 32 of the 128 outputs; its quarter of P goes through a part of LDS of its own, the angles of the
@@ -503,16 +518,14 @@ static int rows_of_groups(const RopeDev& d) {
         if (d.rows[x] && d.heads[x] < heads) heads = d.heads[x];
     return RM_GROUPS % heads == 0 ? RM_GROUPS / heads : (RM_GROUPS - 1) / heads + 2;
 }
-// `done`: whether the side without a matrix went along.
 template <int R, bool PAIRS>
-static hipError_t rope_matrix_launch(const RopeDev& d, const RopeDev& plain, bool& done, hipStream_t stream) {
+static hipError_t rope_matrix_launch(const RopeDev& d, const RopeDev& plain, hipStream_t stream) {
     const unsigned matrices = d.per_head ? (unsigned)(d.heads[0] + d.heads[1]) : (unsigned)((d.rows[0] != nullptr) + (d.rows[1] != nullptr));
     const int64_t most = d.per_head ? d.T : d.T * (d.heads[0] > d.heads[1] ? d.heads[0] : d.heads[1]);
     const int64_t blocks = (most + RM_GROUPS - 1) / RM_GROUPS;
-    // Up to two workgroups a CU (one where each head has a matrix and its rows' angles for itself) the kernel for few.  us, few / many: 300 rows of 32 + 8 heads through one matrix
-    // 8.9 / 11.6, 500 10.9 / 12.0, 777 17.1 / 13.8; through one each 64 8.1 / -, 200 11.7 / 9.9, 300 12.0 / 10.7.
-    done = blocks * matrices <= (d.per_head ? 1 : 2) * cu_count();
-    if (done) {
+    // Up to one workgroup a CU the kernel for few.  us, few / many: 32 + 8 heads, the queries through one matrix, 150 rows 7.2 / 8.7, 256 7.5 / 8.8, 400 9.4 / 9.0; 32 + 32
+    // heads, 256 rows 8.0 / 8.9, 300 9.6 / 9.0, 400 13.1 / 9.6; through one each, 32 + 8 heads, 150 rows 9.1 / 10.3, 200 11.7 / 10.4, 256 12.0 / 10.5.
+    if (blocks * matrices <= cu_count()) {
         const bool both = plain.heads[0] + plain.heads[1] > 0;
         return launch(rope_matrix_few_kernel<R, PAIRS>, dim3((unsigned)blocks, matrices + both), dim3(RP_NT), 0, stream, d, plain, (int)matrices);
     }
@@ -523,8 +536,10 @@ static hipError_t rope_matrix_launch(const RopeDev& d, const RopeDev& plain, boo
         const int64_t need = (blocks + RP_WAVES - 1) / RP_WAVES;
         int64_t gx = ((int64_t)cu_count() * occ + matrices - 1) / matrices;
         const int64_t rounds = (need + gx - 1) / gx;
+        const int64_t most = gx, tasks = (plain.T + 3) / 4 * ((plain.heads[0] + plain.heads[1] + 7) / 8), others = (tasks + RP_WAVES * matrices - 1) / (RP_WAVES * matrices);
         gx = (need + rounds - 1) / rounds;
-        return launch(kernel, dim3((unsigned)gx, matrices), dim3(RP_NT), lds, stream, d);
+        if (rounds == 1) gx = gx + others < most ? gx + others : most;         // workgroups for the side without a matrix, where there is room
+        return launch(kernel, dim3((unsigned)gx, matrices), dim3(RP_NT), lds, stream, d, plain);
     };
     static OccCache caches[2];
     // (8192 rows of 32 + 8 heads: 52.7 us with the table, 58.0 without)
@@ -544,20 +559,19 @@ hipError_t rope_launch(const RopeDev& all, hipStream_t stream) {
     if (through.rows[0] || through.rows[1]) {
         const int r = all.rotary / 32;
         const bool pairs = all.interleaved && r > 0;
-        bool done = false;
         hipError_t e = hipErrorInvalidValue;
         switch (2 * r + pairs) {
-            case 0: e = rope_matrix_launch<0, false>(through, plain, done, stream); break;
-            case 2: e = rope_matrix_launch<1, false>(through, plain, done, stream); break;
-            case 3: e = rope_matrix_launch<1, true>(through, plain, done, stream); break;
-            case 4: e = rope_matrix_launch<2, false>(through, plain, done, stream); break;
-            case 5: e = rope_matrix_launch<2, true>(through, plain, done, stream); break;
-            case 6: e = rope_matrix_launch<3, false>(through, plain, done, stream); break;
-            case 7: e = rope_matrix_launch<3, true>(through, plain, done, stream); break;
-            case 8: e = rope_matrix_launch<4, false>(through, plain, done, stream); break;
-            case 9: e = rope_matrix_launch<4, true>(through, plain, done, stream); break;
+            case 0: e = rope_matrix_launch<0, false>(through, plain, stream); break;
+            case 2: e = rope_matrix_launch<1, false>(through, plain, stream); break;
+            case 3: e = rope_matrix_launch<1, true>(through, plain, stream); break;
+            case 4: e = rope_matrix_launch<2, false>(through, plain, stream); break;
+            case 5: e = rope_matrix_launch<2, true>(through, plain, stream); break;
+            case 6: e = rope_matrix_launch<3, false>(through, plain, stream); break;
+            case 7: e = rope_matrix_launch<3, true>(through, plain, stream); break;
+            case 8: e = rope_matrix_launch<4, false>(through, plain, stream); break;
+            case 9: e = rope_matrix_launch<4, true>(through, plain, stream); break;
         }
-        if (e != hipSuccess || done) return e;
+        return e;
     }
     const int heads = plain.heads[0] + plain.heads[1];
     if (heads == 0) return hipSuccess;
