@@ -378,7 +378,7 @@ fq_status flatquant_head_rope(const void* q, int64_t q_stride, int Hq, const voi
 /*
  * flatquant_cache_attention with other scores and one more mask:
  *     score = scale * q[t, h, :] . k_j,   with cap > 0  cap * tanh(score / cap),   then  score - slopes[h] * |p - j|
- * for a row at position p.  cap 0 is none, slopes NULL none.
+ * for a row at position p.  cap 0 is none, slopes NULL none; with neither and no prefix it is that call, or flatquant_cache_tree_attention.
  *   slopes   fp32 [Hq], finite, 4-byte aligned.
  *   prefix   i32 [B], 4-byte aligned, or NULL: a row of sequence b also sees every token before prefix[b], those behind it among them, whatever the window.
  *   visible  u64 [T] or NULL: the masks of flatquant_cache_tree_attention; window and sinks 0, slopes and prefix NULL then.

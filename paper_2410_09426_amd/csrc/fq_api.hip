@@ -479,7 +479,7 @@ static fq_status cache_attention(const fq_kv_cache* cache, const fq_kv_batch* ba
     a.q = static_cast<const _Float16*>(q); a.out = static_cast<_Float16*>(out); a.q_stride = q_stride; a.out_stride = out_stride;
     a.Hq = Hq; a.scale = scale; a.window = window; a.sinks = sinks; a.visible = visible; a.workspace = static_cast<float*>(workspace);
     a.max_rows = max_rows;
-    if (scores) return fq::finish(fq::scored_attention_launch(d, a, *scores, plan, static_cast<hipStream_t>(stream)));
+    if (scores && (scores->cap > 0.0f || scores->slopes || scores->prefix)) return fq::finish(fq::scored_attention_launch(d, a, *scores, plan, static_cast<hipStream_t>(stream)));
     return fq::finish(fq::attention_launch(d, a, plan, static_cast<hipStream_t>(stream)));
 }
 

@@ -212,6 +212,27 @@ def test_rows_of_many_sequences(B, rows):
     Step(24, held, held, n).check()
 
 
+def test_table_rows_far_apart():
+    """Rows of the table 2^30 entries apart: places beyond 2^32 bytes."""
+    print("[case] far rows", flush=True)
+    stride, B, width, pages = 2 ** 30, 3, 6, 20
+    table = torch.empty(2 * stride + width, dtype=torch.int32, device="cuda")
+    rows = [table[b * stride:b * stride + width] for b in range(B)]
+    want, held, keep, new = [], [40, 0, 70], [40, 0, 20], [30, 50, 3]
+    for b, r in enumerate(rows):
+        want.append([10 * b + j if j * 16 < held[b] else -5 for j in range(width)])
+        r.copy_(_i32(want[b]))
+    ring, state = list(range(60, 80)), (3, 20)
+    d = [torch.zeros(n, dtype=t, device="cuda") for n, t in ((B + 1, torch.int32), (B, torch.int32), (90, torch.int32), (90, torch.int64), (3, torch.int64))]
+    dring, dstate = _i32(ring), torch.tensor(state, device="cuda")
+    batch = fq.KvBatch(d[0], d[1], table, B, 90, width, stride, 1, 1)
+    fq.flatquant_cache_advance(batch, fq.PagePool(dring, dstate, d[4], pages), 16, 100, _i32(held), _i32(keep), _i32(new), d[2], d[3], stream=torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    starts, lengths, nxt, positions, slots = so.advance(held, keep, new, want, width, 16, 100, ring, *state, 90)
+    got = [x.tolist() for x in (d[0], d[1], d[4], d[2], d[3], dring)] + [r.tolist() for r in rows]
+    assert got == [starts, lengths, list(nxt), positions, slots, ring] + want
+
+
 def test_no_sequences_with_rows():
     print("[case] nothing", flush=True)
     Step(21, [5, 6], [5, 6], [0, 0]).check()

@@ -200,6 +200,24 @@ def test_more_rows_than_a_grid_has():
         assert torch.equal(part, out[rows])
 
 
+@pytest.mark.parametrize("P", [0, 1, 2])
+def test_rows_far_apart(P):
+    """Rows 2^31 halves apart: offsets beyond 2^32 bytes, into and out of the call."""
+    print(f"[case] far rows P={P}", flush=True)
+    stride, T, H = 2 ** 31, 3, 2
+    c = Rows(14, T, H, 1, norm=True, P=P)
+    near = c.run("q", out_pad=0)[0]
+    x, w, P_dev = torch.empty(2 * stride + H * D, dtype=torch.float16, device="cuda"), c.kept[3][0], c.kept[4][0]
+    out = torch.empty_like(x)
+    for t in range(T):
+        x[t * stride:t * stride + H * D] = c.kept[0][0][t, :H * D]
+    fq.flatquant_head_rope(x, stride, H, None, 0, 0, T, c.kept[5], c.kept[2], D, 0, w, None, c.eps, P_dev, None, c.per_head, out, stride, None, 0,
+                           stream=torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    for t in range(T):
+        assert np.array_equal(host_f16(out[t * stride:t * stride + H * D]).reshape(H, D), near[t])
+
+
 def test_the_matrix_is_that_of_the_head_transform():
     """Without norm and rotation: the bits of flatquant_head_transform."""
     print("[case] head transform", flush=True)

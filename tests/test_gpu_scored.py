@@ -151,14 +151,15 @@ def test_rows_that_see_nothing():
 
 
 def test_plain_scores_are_those_of_the_plain_call():
-    """No cap, no slopes, no prefix: the same launches, weights within a rounding of the factor."""
+    """No cap, no slopes, no prefix: the same bits; a prefix of nothing: weights within a rounding of the factor."""
     print("[case] plain", flush=True)
     for shape in ("one row", "tile of 32", "prompt", "split"):
         rows, lengths, H, G = SHAPES[shape]
         c = Batch(77, rows, lengths, H).upload()
         q, got = check(c, G)
         plain = run_attention(c, q, G, 0.09)
-        n = c.starts[-1]
+        assert np.array_equal(got, plain)
+        got, n = run_scored(c, q, G, 0.09, prefix=[0] * c.B), c.starts[-1]
         assert np.abs(got[:n].astype(float) - plain[:n]).max() <= 2.0 ** -9 * np.abs(plain[:n].astype(float)).max()
 
 
