@@ -203,18 +203,6 @@ __device__ __forceinline__ void fill_table(const RopeDev& d, int role, uint64_t*
     if ((int)threadIdx.x < d.rotary / 2) turns[threadIdx.x] = d.turns[threadIdx.x];
     if (threadIdx.x < RP_D) weights[threadIdx.x] = d.w[role] ? (float)d.w[role][threadIdx.x] : 1.0f;
 }
-// Angles of rows first .. last, by `threads` threads of which this is number n.
-__device__ __forceinline__ void fill_angles(const RopeDev& d, const uint64_t* turns, float2* angles, int64_t first, int64_t last, int n, int threads) {
-    const int pairs = d.rotary / 2, all = (int)(last - first + 1) * 64;
-    for (int k = n; k < all; k += threads) {
-        const int row = k >> 6, pair = k & 63;
-        if (pair >= pairs) continue;
-        const int position = d.positions[first + row];
-        float2 a;
-        cos_sin(angle_of(position < 0 ? 0u : (uint32_t)position, turns[pair]), a.x, a.y);
-        angles[row * RM_ANGLES + pair] = a;
-    }
-}
 
 // Channels 16 kb + 8 h .. + 7 of a group in rows[kb]: norm and rotation, each number rounded to fp16, which the matrix instructions take.  R: rotary / 32.
 // `angles`: of the group's row, or null, and the position says.
@@ -461,7 +449,6 @@ template <int R, bool PAIRS>
 __global__ __launch_bounds__(RP_NT) void rope_matrix_few_kernel(RopeDev d, RopeDev plain, int matrices) {
     constexpr int PITCH = 32 + 8;
     __shared__ __attribute__((aligned(16))) _Float16 Pw_all[RP_WAVES * RP_D * PITCH];
-    __shared__ __attribute__((aligned(16))) uint64_t turns[64];
     __shared__ __attribute__((aligned(16))) float weights[RP_D];
     __shared__ __attribute__((aligned(16))) float2 angles[RM_GROUPS * RM_ANGLES];
     const int l = threadIdx.x & 63, c = l & 31, h = l >> 5;
@@ -479,26 +466,38 @@ __global__ __launch_bounds__(RP_NT) void rope_matrix_few_kernel(RopeDev d, RopeD
     int64_t row;
     int of;
     groups.at(n, row, of);
-    const int position = d.positions[row];
+    // what the angles take first: loads return in order.  Positions of the groups' rows, one a lane; a wave takes every fourth of them, a lane a pair
+    const int64_t first = __shfl((long long)row, 0), last = __shfl((long long)row, RM_GROUPS - 1);
+    const uint64_t turn = R > 0 ? d.turns[l < 16 * R ? l : 0] : 0;
+    const int positions = d.positions[first + c <= last ? first + c : last];
+    const float weight = d.w[groups.role] ? (float)d.w[groups.role][threadIdx.x & (RP_D - 1)] : 1.0f;
+    __builtin_amdgcn_sched_barrier(0);
     u32x4 v[8], rows[RM_KB];
 #pragma unroll
     for (int k = 0; k < 8; ++k) v[k] = *reinterpret_cast<const u32x4*>(P + (16 * k + (l >> 2)) * RP_D + 8 * (l & 3));
     const u32x4* from = reinterpret_cast<const u32x4*>(d.rows[groups.role] + row * d.stride[groups.role] + of * RP_D);
 #pragma unroll
     for (int kb = 0; kb < RM_KB; ++kb) rows[kb] = from[2 * kb + h];
-    const int64_t first = __shfl((long long)row, 0), last = __shfl((long long)row, RM_GROUPS - 1);
-    fill_table(d, groups.role, turns, weights);
-    if constexpr (R > 0) fill_angles(d, d.turns, angles, first, last, threadIdx.x, RP_NT);
+    __builtin_amdgcn_sched_barrier(0);
+    if ((int)threadIdx.x < RP_D) weights[threadIdx.x] = weight;
+    if constexpr (R > 0)
+        for (int k = w; first + k <= last; k += RP_WAVES) {
+            const int p = __builtin_amdgcn_readlane(positions, k);
+            float2 a;
+            cos_sin(angle_of(p < 0 ? 0u : (uint32_t)p, turn), a.x, a.y);
+            if (l < 16 * R) angles[k * RM_ANGLES + l] = a;
+        }
 #pragma unroll
     for (int k = 0; k < 8; ++k) *reinterpret_cast<u32x4*>(Pw + (16 * k + (l >> 2)) * PITCH + 8 * (l & 3)) = v[k];
     __syncthreads();
-    turn_group<R, PAIRS, false>(rows, RopeTable{turns, weights, angles}, d.w[groups.role] != nullptr, d.eps, 0u, angles + (int)(row - first) * RM_ANGLES, h);
+    turn_group<R, PAIRS, false>(rows, RopeTable{nullptr, weights, angles}, d.w[groups.role] != nullptr, d.eps, 0u, angles + (int)(row - first) * RM_ANGLES, h);
     f32x16 acc;
 #pragma unroll
     for (int r = 0; r < 16; ++r) acc[r] = 0.0f;
 #pragma unroll
     for (int kb = 0; kb < RM_KB; ++kb)
         acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(lds_column8<true>(Pw, PITCH, 16 * kb + 8 * h, 4, c & 16, l & 15), __builtin_bit_cast(half8, rows[kb]), acc, 0, 0, 0);
+    const int position = __shfl(positions, (int)(row - first));
     if (mine >= groups.count || position < 0) return;
     _Float16* out = d.out[groups.role] + row * d.out_stride[groups.role] + of * RP_D + 32 * w + 8 * h;
 #pragma unroll
@@ -523,8 +522,8 @@ static hipError_t rope_matrix_launch(const RopeDev& d, const RopeDev& plain, hip
     const unsigned matrices = d.per_head ? (unsigned)(d.heads[0] + d.heads[1]) : (unsigned)((d.rows[0] != nullptr) + (d.rows[1] != nullptr));
     const int64_t most = d.per_head ? d.T : d.T * (d.heads[0] > d.heads[1] ? d.heads[0] : d.heads[1]);
     const int64_t blocks = (most + RM_GROUPS - 1) / RM_GROUPS;
-    // Up to one workgroup a CU the kernel for few.  us, few / many: 32 + 8 heads, the queries through one matrix, 150 rows 7.2 / 8.7, 256 7.5 / 8.8, 400 9.4 / 9.0; 32 + 32
-    // heads, 256 rows 8.0 / 8.9, 300 9.6 / 9.0, 400 13.1 / 9.6; through one each, 32 + 8 heads, 150 rows 9.1 / 10.3, 200 11.7 / 10.4, 256 12.0 / 10.5.
+    // Up to one workgroup a CU the kernel for few.  us, few / many: 32 + 8 heads, the queries through one matrix, 150 rows 6.6 / 8.7, 256 6.9 / 8.8, 400 8.6 / 9.0, 500 10.0 / 9.4;
+    // 32 + 32 heads, 256 rows 7.1 / 8.9, 300 9.4 / 9.0, 400 12.1 / 9.7; through one each, 32 + 8 heads, 150 rows 7.8 / 10.3, 200 10.4 / 10.5, 300 10.7 / 11.2.
     if (blocks * matrices <= cu_count()) {
         const bool both = plain.heads[0] + plain.heads[1] > 0;
         return launch(rope_matrix_few_kernel<R, PAIRS>, dim3((unsigned)blocks, matrices + both), dim3(RP_NT), 0, stream, d, plain, (int)matrices);
