@@ -5,8 +5,8 @@
 // max(0, P(keep + n) - P(held)) and lie in the ring behind those of the sequences before it, and what it gives back, max(0, P(held) - P(keep + n)) entries
 // but those that are no page, is put behind the ring's last in the same order.  All of it follows from running sums over the sequences, so one
 // workgroup works it out, 1024 sequences at a time: the order of the pages is that of the sequences, whatever runs first, and nothing has to be cleared or
-// counted in memory.  Entries that change are dealt out to its threads evenly (a thread finds the sequence of its entry by bisection in LDS), as
-// one sequence may have most of them.
+// counted in memory.  Entries that change are dealt out to its waves evenly, as one sequence may have most of them: a wave looks for the sequences of its first and its
+// last entry, and those between by bisection in LDS.
 //
 // Bound by latency, and on its one CU by the instructions of an entry: 64 decoding sequences 4.7 us (replayed; a launch, the sequences' loads, three running sums, rows), 512 in mixed states
 // (1150 pages taken, 15800 given back) 10.5 and 4 for their 18500 rows, 16 prompts of 65536 tokens (42900 pages, 686000 rows) 11.5 and 6.  Rows of more than a few
@@ -143,7 +143,8 @@ __global__ __launch_bounds__(ADV_NT) void advance_kernel(AdvanceDev a) {
     __shared__ unsigned long long wanted_all;
     int turn = 0;
     const int tid = threadIdx.x, l = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int64_t taken = a.state[0], given = a.state[1];
+    int64_t taken = a.state[0], given = a.state[1];
+    asm volatile("" : "+v"(taken), "+v"(given));                               // (have arrived before the first barrier: the next state may take their place behind the last)
     const int64_t capacity = a.capacity;
     int64_t available = (int64_t)((uint64_t)given - (uint64_t)taken);          // (of a state that is none: what the ring can hold at most)
     available = available < 0 ? 0 : available < capacity ? available : capacity;
@@ -158,7 +159,7 @@ __global__ __launch_bounds__(ADV_NT) void advance_kernel(AdvanceDev a) {
         for (int b0 = 0; b0 < a.B; b0 += ADV_NT) mine += step_of(a, b0 + tid, rows, parts, turn, rows).taken;
 #pragma unroll
         for (int m = 1; m < 64; m *= 2) mine += __shfl_xor((long long)mine, m);
-        if ((tid & 63) == 0) atomicAdd(&wanted_all, (unsigned long long)mine);  // (integers: any order gives the same)
+        if (l == 0) atomicAdd(&wanted_all, (unsigned long long)mine);  // (integers: any order gives the same)
         __syncthreads();
         wanted = (int64_t)wanted_all;
     }
