@@ -488,15 +488,18 @@ __device__ __forceinline__ bool weigh(const Scores& score, Factor factor, Step s
     }
     return __any(big > 32768.0f || sum > 0x1p40f);
 }
-// Raises the reference so that the row's largest product here is at most 2^7 (a step below 2^-25 counts as that), or 2^11 for scores near 2^24: so much lower that
+// Raises the reference so that the row's largest product here is at most 2^7 (a step below 2^-25 counts as that), or 2^4 more for scores near 2^24: so much lower that
 // the largest weight of all scores, however large, is not lost to the reference's rounding.  Returns the factor for what has been summed.
-template <int N, typename Scores, typename Factor, typename Step, typename Row>
+// LARGEST says which power: 7, or for many rows with other scores, which spread over a cap's range and cost more to weigh again, 2, so that it is done less often; products in
+// fp16's subnormals then lose 2^-27 of the row's largest (2048 rows at 8192 tokens capped 742 -> 704 us, 64 at 1500 of 32 sequences 100 -> 92, trees of 13 49.5 -> 46.6; few rows,
+// bound by memory, gain nothing).
+template <int N, int LARGEST, typename Scores, typename Factor, typename Step, typename Row>
 __device__ __forceinline__ float raise_reference(const Scores& score, Factor factor, Step step, float& ref, Row row_max) {
     float top = ATT_NONE;
 #pragma unroll
     for (int k = 0; k < N; ++k) top = __builtin_fmaxf(top, score[k] * factor(k) + __builtin_fmaxf(__builtin_amdgcn_logf(step(k)), -25.0f));
     top = __builtin_fminf(row_max(top), 0x1p120f);
-    const float to = __builtin_fmaxf(ref, top - 7.0f - __builtin_fabsf(top) * 0x1p-22f), f = __builtin_amdgcn_exp2f(ref - to);
+    const float to = __builtin_fmaxf(ref, top - (float)LARGEST - __builtin_fabsf(top) * 0x1p-22f), f = __builtin_amdgcn_exp2f(ref - to);
     ref = to;
     return f;
 }
@@ -671,7 +674,7 @@ __device__ __forceinline__ void few_rows(const DEV& p, unsigned char* smem, int 
             auto by = [&](int) { return unit_of(p, factor[0]); };
             auto step = [&](int k) { return (float)step_bits(vp[k]); };
             if (weigh<N, false>(s, by, step, ref[0], prod, sum)) {
-                const float f = raise_reference<N>(s, by, step, ref[0], [](float top) { return across_groups(top, fmax_op); });
+                const float f = raise_reference<N, 7>(s, by, step, ref[0], [](float top) { return across_groups(top, fmax_op); });
                 total[0] *= f;
                 zeros[0] *= f;
 #pragma unroll
@@ -740,7 +743,7 @@ __device__ __forceinline__ void few_rows(const DEV& p, unsigned char* smem, int 
 #pragma unroll
                 for (int k = 0; k < 8; ++k) s8[k] = sc[n][k >> 2][k & 3];
                 if (weigh<8, false>(s8, by, step, ref[n], prod, sum)) {
-                    const float f = raise_reference<8>(s8, by, step, ref[n], [](float top) { return across_groups(top, fmax_op); });
+                    const float f = raise_reference<8, 7>(s8, by, step, ref[n], [](float top) { return across_groups(top, fmax_op); });
                     total[n] *= f;
                     zeros[n] *= f;
 #pragma unroll
@@ -1350,7 +1353,7 @@ __global__ __launch_bounds__(64 * NW, 2) void shared_attention_kernel(DEV p) {
         auto raise = [&](const f32x16& sc, const float (&fk)[16], const float (&vs)[16], float (&prod)[16], float& sum) {
             auto by = [&](int k) { return factor_of(fk, k); };
             auto step = [&](int k) { return vs[k]; };
-            const float f = raise_reference<16>(sc, by, step, ref, [](float top) { return __builtin_fmaxf(top, __shfl_xor(top, 32)); });
+            const float f = raise_reference<16, kScored<DEV> ? 2 : 7>(sc, by, step, ref, [](float top) { return __builtin_fmaxf(top, __shfl_xor(top, 32)); });
             total *= f;
 #pragma unroll
             for (int dt = 0; dt < 4; ++dt)

@@ -4,7 +4,6 @@ import pytest
 import torch
 
 from cache_util import D, Batch, run_attention
-from oracle import cache_oracle as co
 from oracle import step_oracle as so
 from paper_2410_09426_amd import binding as fq
 
@@ -50,7 +49,7 @@ def expect(c, q, G, scale, cap=0.0, slopes=None, prefix=None, window=0, sinks=0,
         for h in range(c.H * G) if heads is None else heads:
             o, A, S, E = so.scored64(q[t, h], k[h // G], v[h // G], seen, scale, pos, cap, 0.0 if slopes is None else float(slopes[h]), ks[h // G], vs[h // G], c.bits[0])
             out[t, h] = o
-            tol[t, h] = co.attention_bound(o, A, S, np.zeros(n), L, c.bits[1]) + E * (1 + 2.0 ** -6)
+            tol[t, h] = so.scored_bound(o, A, S, E, L, c.bits[1])
     return out, tol
 
 

@@ -254,7 +254,7 @@ def test_oracle_bounds_reject_planted_mistakes():
     seen[0, 100:] = False
     how = dict(scale=0.09, positions=np.array([60, 119]), k_step=ks, v_step=vs)
     out, A_, S, E = so.scored64(q, k, v, seen, cap=2.0, slope=0.1, **how)
-    tol = co.attention_bound(out, A_, S, np.zeros(2), L) + E * 1.01
+    tol = so.scored_bound(out, A_, S, E, L)
     fewer = seen.copy()
     fewer[0, 99] = False
     for z in (so.scored64(q, k, v, seen, cap=1.92, slope=0.1, **how), so.scored64(q, k, v, seen, cap=2.0, slope=0.11, **how),
