@@ -366,7 +366,7 @@ fq_status flatquant_cache_advance(const fq_kv_batch* batch, const fq_page_pool* 
  *   positions  i32 [T]; a row whose position is negative is no token: its outputs are left as they are.
  *   turns      u64 [rotary / 2], 16-byte aligned (fq_rope_turns makes them); NULL if rotary is 0.  The angle is exact to 2^-32 of a turn at every position.
  *   rotary     0, 32, 64, 96 or 128.
- *   w_q, w_k   fp16 [128], 16-byte aligned, shared by the heads, or NULL;  eps > 0.
+ *   w_q, w_k   fp16 [128], 16-byte aligned, shared by the heads, or NULL;  eps > 0, no subnormal number.
  *   P_q, P_k   fp16 [128, 128], or with per_head [Hq, 128, 128] and [H, 128, 128], row-major, 16-byte aligned, or NULL.
  * T == 0 returns FQ_OK without launching.  T <= 2^29, Hq, H <= 65535 (32767 with per_head), T * Hq and T * H < 2^31 - 256, strides <= 2^40 and T * stride <= 2^48.
  */

@@ -418,7 +418,7 @@ fq_status flatquant_head_rope(const void* q, int64_t q_stride, int Hq, const voi
         written[x] = Bytes{nullptr, 0};
         if (!in[x]) continue;
         const int64_t row = 128LL * heads[x];
-        if (heads[x] < 1 || stride[x] < row || to_stride[x] < row || (w[x] && !(eps > 0.0f && std::isfinite(eps)))) return FQ_INVALID_ARG;
+        if (heads[x] < 1 || stride[x] < row || to_stride[x] < row || (w[x] && !(eps > 0.0f && std::isnormal(eps)))) return FQ_INVALID_ARG;   // (the root of a subnormal one is none)
         if (heads[x] > (per_head ? 32767 : 65535) || T > 0x7fffff00LL / heads[x]) return FQ_UNSUPPORTED_SHAPE;
         const int64_t most = T > 256 ? (1LL << 48) / T : 1LL << 40;
         if (stride[x] > most || to_stride[x] > most) return FQ_UNSUPPORTED_SHAPE;

@@ -137,10 +137,11 @@ def test_values_of_all_sizes():
     c.x[0] *= (2.0 ** np.random.default_rng(2).integers(-24, 13, (64, 1, 1))).astype(np.float16)
     c.x[0][5] = 0
     c.check()
-    c = Rows(9, 64, 2, 1, norm=True, eps=1e-5)
-    c.x[0][5], c.x[0][6] = 0, 60000.0
-    got = c.check()
-    assert not got[0][5].any()
+    for eps in (1e-5, 1.2e-38):
+        c = Rows(9, 64, 2, 1, norm=True, eps=eps)
+        c.x[0][5], c.x[0][6] = 0, 60000.0
+        got = c.check()
+        assert not got[0][5].any()
 
 
 @pytest.mark.parametrize("interleaved", [False, True])

@@ -243,3 +243,20 @@ def test_hints_that_are_wrong():
     for rows, length in ((0, 0), (1, 100), (40, 0), (3, 10 ** 6), (10 ** 6, 10 ** 9)):
         got = run_scored(c, q, 4, 0.09, batch=c.batch(max_rows=rows, max_length=length), **how)
         assert (np.abs(got - want) / tol).max() <= 1, (rows, length)
+
+
+@pytest.mark.parametrize("B,H,G,length", [(20, 8, 2, 300), (70, 8, 4, 200), (300, 2, 8, 90)])
+def test_launches_of_many_pairs(B, H, G, length):
+    """160 to 600 pairs, more sequences than the balanced launch holds; some sequences and heads against fp64."""
+    print(f"[case] pairs {B} x {H}", flush=True)
+    r = np.random.default_rng(B)
+    c = Batch(B, [1] * B, [int(n) for n in r.integers(1, length, B)], H, k_bits=3, v_bits=4).upload()
+    check(c, G, heads=[0, H * G - 1], sequences=sorted(set(r.integers(0, B, 12).tolist())), **kind_of("all", c, G))
+
+
+def test_trees_without_a_cap_are_those_of_the_tree_call():
+    print("[case] plain tree", flush=True)
+    c = Batch(17, [13, 1, 30], [300, 40, 90], 2).upload()
+    masks = [int(c.r.integers(0, 2 ** 63)) for _ in range(c.T)]
+    q = c.row_tensor(8)
+    assert np.array_equal(run_scored(c, q, 4, 0.09, masks=masks), run_attention(c, q, 4, 0.09, masks=masks))

@@ -69,7 +69,7 @@ def test_rope_refuses():
     assert _rope(T=0) == fq.FQ_OK and _rope(q=None, k=None) == fq.FQ_OK
     assert _rope(T=0, q=None, Hq=-5, k=None) == fq.FQ_OK
     for bad in (dict(T=-1), dict(rotary=-32), dict(interleaved=2), dict(per_head=-1), dict(Hq=0), dict(H=-1), dict(q_stride=1016), dict(k_stride=504),
-                dict(q_out_stride=1016), dict(k_out_stride=511), dict(eps=0.0), dict(eps=-1.0), dict(eps=float("nan")), dict(eps=float("inf")), dict(q_out=None),
+                dict(q_out_stride=1016), dict(k_out_stride=511), dict(eps=0.0), dict(eps=1e-40), dict(eps=-1.0), dict(eps=float("nan")), dict(eps=float("inf")), dict(q_out=None),
                 dict(k_out=None), dict(positions=None), dict(turns=None)):
         assert _rope(**{**wrong, **bad}) == fq.FQ_INVALID_ARG, bad
     for bad in (dict(rotary=16), dict(rotary=100), dict(rotary=160), dict(T=2 ** 29 + 1), dict(Hq=65536, q_stride=2 ** 23, q_out_stride=2 ** 23),
