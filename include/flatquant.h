@@ -343,9 +343,11 @@ typedef struct fq_page_pool {
  *   batch->row_starts[b]  n_0 + .. + n_(b - 1), and of all in [B];   batch->lengths[b] = keep[b] + n_b
  *   batch->page_table     entries P(held) .. P(length) - 1 of every sequence: pages from the ring in the order of the sequences and their entries.  If the ring has fewer
  *          than the call takes, none is taken: the entries become -1 (no page: such tokens are not written and not visible) and next[2] says how many are
- *          missing; a program gives others back and makes the call again with the same held, keep and rows.
+ *          missing; a program looks at it, gives others back and makes the call again with the same held, keep and rows (so where the ring may run short held and
+ *          keep lie in arrays of their own, not in batch->lengths, which is written all the same).
  *          Entries P(length) .. P(held) - 1 are put into the ring in the same order, but for those that are no page, and can be taken from the next call on (so they have to be
- *          the sequence's own: pages that it shares are for the program to give back).  No entry is changed but those that get a page or -1.
+ *          the sequence's own: pages that it shares are for the program to give back).  They stay as they are, or become -1 where pages are missing: made again, the call
+ *          gives no page back twice.  No other entry is changed.
  *   positions  i32 [T], slots i64 [T], either NULL: position of every row, and page * page_tokens + position % page_tokens; -1 for rows behind the last sequence, slots
  *          also for a token that has no page.
  * The batch's arrays are written here, max_rows and max_length are not looked at.  page_tokens and pages are those of the cache; page_tokens a power of two, 16 .. 1024.

@@ -33,7 +33,11 @@ def advance(held, keep, rows, table, width, page, pages, ring, taken, given, T):
         for j in range(have, need):
             table[b][j] = ring[(taken + len(got)) % len(ring)] if enough else -1
             got.append(j)
-        back += [table[b][j] for j in range(need, have) if 0 <= table[b][j] < pages]
+        for j in range(need, have):
+            if 0 <= table[b][j] < pages:
+                back.append(table[b][j])
+                if not enough:
+                    table[b][j] = -1                                           # the call is made again: it finds no page there
     for i, p in enumerate(back):
         ring[(given + i) % len(ring)] = p
     positions, slots = [-1] * T, [-1] * T

@@ -240,7 +240,10 @@ __global__ __launch_bounds__(ADV_NT) void advance_kernel(AdvanceDev a) {
                         uint32_t r = __builtin_amdgcn_mbcnt_hi((uint32_t)(is[k] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)is[k], at));
                         if (capacity > ADV_NT * PER) r = r >= (uint32_t)capacity ? r - (uint32_t)capacity : r;
                         else r %= (uint32_t)capacity;
-                        if (is[k] >> l & 1) a.ring[r] = page[k];
+                        if (is[k] >> l & 1) {
+                            a.ring[r] = page[k];
+                            if (!enough) a.page_table[place[k]] = -1;          // the call is made again with the same figures: it finds no page there
+                        }
                         at += __builtin_popcountll(is[k]);
                     }
                     tail = (tail + all) % (uint32_t)capacity;
