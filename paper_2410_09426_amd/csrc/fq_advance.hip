@@ -20,7 +20,13 @@ constexpr int ADV_NT = 1024;               // sequences of a chunk, threads
 constexpr int ADV_WAVES = ADV_NT / 64;
 constexpr int kSaturated = 1 << 30;        // of row counts: above every T
 
-__device__ __forceinline__ int saturated_add(int a, int b) { return min(a + b, kSaturated); }
+// (as numbers without a sign: two that are saturated add up to 2^31)
+constexpr __host__ __device__ __forceinline__ int saturated_add(int a, int b) {
+    const uint32_t sum = (uint32_t)a + (uint32_t)b;
+    return sum < (uint32_t)kSaturated ? (int)sum : kSaturated;
+}
+static_assert(saturated_add(kSaturated, kSaturated) == kSaturated && saturated_add(kSaturated - 1, 1) == kSaturated && saturated_add(kSaturated, 0) == kSaturated &&
+                  saturated_add(3, 4) == 7, "sums of row counts");
 // Value of the lane N places before in its row of 16 (SHIFT), or of the last lane of the row or half before; zero where there is none.
 template <int CTRL, int ROWS = 0xF>
 __device__ __forceinline__ uint32_t lane_before(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xF, false); }
