@@ -384,7 +384,8 @@ fq_status flatquant_head_rope(const void* q, int64_t q_stride, int Hq, const voi
  *   slopes   fp32 [Hq], finite, 4-byte aligned.
  *   prefix   i32 [B], 4-byte aligned, or NULL: a row of sequence b also sees every token before prefix[b], those behind it among them, whatever the window.
  *   visible  u64 [T] or NULL: the masks of flatquant_cache_tree_attention; window and sinks 0, slopes and prefix NULL then.
- * Everything else, the workspace and what a row that sees nothing or no number gets, as for the other two.
+ * With any of them a row whose queries are not all finite gets NaN if it sees a token.  Everything else, the workspace and what a row that sees nothing or no number gets,
+ * as for the other two.
  */
 fq_status flatquant_cache_scored_attention(const fq_kv_cache* cache, const fq_kv_batch* batch, const void* q, int64_t q_stride, int Hq, float scale,
                                            float cap, const float* slopes, const int32_t* prefix, int window, int sinks, const uint64_t* visible,

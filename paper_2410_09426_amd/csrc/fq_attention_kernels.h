@@ -1182,6 +1182,20 @@ __global__ __launch_bounds__(64 * NW, 2) void shared_attention_kernel(DEV p) {
                         q[2 * quarter + k][2 * e + 1] = h ? pick(KeyCodes<KB>::second(hi)) : pick(KeyCodes<KB>::second(lo));
                     }
             }
+            // A row with such a channel: none of them, so that every score is none (infinite ones tanh would make numbers of).  Nothing in the loop.
+            if constexpr (kScored<DEV>) {
+                uint32_t none = 0;                                             // bits 15 and 31: of a channel that is an infinity or no number
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) none |= (__builtin_bit_cast(u32x4, q[k])[e] & 0x7C007C00u) + 0x04000400u;
+                none |= __shfl_xor(none, 32);
+                if (__any(none & 0x80008000u)) {
+                    const uint32_t fill = none & 0x80008000u ? 0x7E007E00u : 0u;
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) q[k] = __builtin_bit_cast(half8, __builtin_bit_cast(u32x4, q[k]) | fill);
+                }
+            }
         }
         f32x16 acc[4];
 #pragma unroll
