@@ -123,11 +123,13 @@ def scored64(q, k, v, seen, scale, positions, cap, slope, k_step, v_step, k_bits
     return out, A, S, E
 
 
-def scored_bound(out, A, S, E, tokens, v_bits=4):
-    """As cache_oracle.attention_bound with what errors of the scores do (E, to first order: 2^-6 of it more).  Of many rows references are raised so that the largest product is 2^2
-    there and not 2^7: a product in fp16's subnormals loses 2^-25 at most, 2^-27 of the largest, which is S at most in sum: 2^b - 1 units of a code each."""
+def scored_bound(out, A, S, E, tokens, v_bits=4, capped=True):
+    """As cache_oracle.attention_bound with what errors of the scores do (E, to first order: 2^-6 of it more).  Of many rows with a cap references are raised so that the largest
+    product is 2^2 there and not 2^7, up to 2^14 tokens: a product in fp16's subnormals loses 2^-25 at most, 2^-27 of the largest, which is S at most in sum: 2^b - 1 units of a
+    code each."""
     from oracle.cache_oracle import attention_bound
-    return attention_bound(out, A, S, np.zeros(len(out)), tokens, v_bits) + E * (1 + 2.0 ** -6) + S[:, None] * ((2 ** v_bits - 1) * tokens * (2.0 ** -27 - 2.0 ** -32))
+    lost = tokens * (2.0 ** -27 - 2.0 ** -32) if capped and tokens <= 2 ** 14 else 0.0
+    return attention_bound(out, A, S, np.zeros(len(out)), tokens, v_bits) + E * (1 + 2.0 ** -6) + S[:, None] * ((2 ** v_bits - 1) * lost)
 
 
 def slopes(heads):

@@ -14,7 +14,8 @@
 //
 // Softmax in one pass: weights are 2^(score - M), M a reference per row that is raised only where a weight times its step would pass
 // 2^15 (fp16's range) or the weights 2^40: most steps neither reduce a maximum nor touch the accumulators.  When it is raised it is put
-// so that the largest product is 2^7: those below 2^-21 of it, fp16's subnormals, lose no more than 2^-32 of it.
+// so that the largest product is 2^7: those below 2^-21 of it, fp16's subnormals, lose no more than 2^-32 of it.  (Capped scores of many rows over 2^14 tokens at most: 2^2, 2^-16
+// and 2^-27; see largest_of.)
 //
 // The 4, 8 or 16 waves of a workgroup take its steps in turn and meet in LDS at the end; where the rows are few the axis is split further over
 // workgroups, whose partial results (M, sum, channels, in fp32) a second kernel joins.
@@ -382,6 +383,16 @@ __device__ __forceinline__ Span span_of(const AttnDev& p, int length, int pos_lo
     s.steps = s.first_steps + (s.end > s.begin ? (s.end - s.begin + ATT_STEP - 1) / ATT_STEP : 0);
     return s;
 }
+// The power of 2 of a row's largest product behind a raised reference (many rows).  With a cap scores spread over its range and cost more to weigh again: 2 instead of 7, so that
+// references are raised less often (2048 rows at 8192 tokens capped 742 -> 704 us, 64 at 1500 of 32 sequences 100 -> 92, trees of 13 49.5 -> 46.6; few rows, bound by memory, gain
+// nothing).  Products in fp16's subnormals then lose 2^-27 of the row's largest each, 2^-32 before: up to 2^14 tokens, that is 2^-13 in all, an eighth of what one product in fp16 is
+// rounded by.
+constexpr int kLowReferenceSteps = (1 << 14) / ATT_STEP;
+template <typename DEV>
+__device__ __forceinline__ float largest_of(const DEV& p, const Span& span) {
+    if constexpr (kScored<DEV>) return p.bend && span.steps <= kLowReferenceSteps ? 2.0f : 7.0f;
+    return 7.0f;
+}
 __device__ __forceinline__ int splits_used(const AttnDev& p, int steps) {
     const int per = p.chunk / ATT_STEP, used = (steps + per - 1) / per;
     return used < 1 ? 1 : used < p.splits ? used : p.splits;
@@ -490,16 +501,14 @@ __device__ __forceinline__ bool weigh(const Scores& score, Factor factor, Step s
 }
 // Raises the reference so that the row's largest product here is at most 2^7 (a step below 2^-25 counts as that), or 2^4 more for scores near 2^24: so much lower that
 // the largest weight of all scores, however large, is not lost to the reference's rounding.  Returns the factor for what has been summed.
-// LARGEST says which power: 7, or for many rows with other scores, which spread over a cap's range and cost more to weigh again, 2, so that it is done less often; products in
-// fp16's subnormals then lose 2^-27 of the row's largest (2048 rows at 8192 tokens capped 742 -> 704 us, 64 at 1500 of 32 sequences 100 -> 92, trees of 13 49.5 -> 46.6; few rows,
-// bound by memory, gain nothing).
-template <int N, int LARGEST, typename Scores, typename Factor, typename Step, typename Row>
-__device__ __forceinline__ float raise_reference(const Scores& score, Factor factor, Step step, float& ref, Row row_max) {
+// `largest`: 7, or of many rows 2 where largest_of says so.
+template <int N, typename Scores, typename Factor, typename Step, typename Row>
+__device__ __forceinline__ float raise_reference(const Scores& score, Factor factor, Step step, float& ref, float largest, Row row_max) {
     float top = ATT_NONE;
 #pragma unroll
     for (int k = 0; k < N; ++k) top = __builtin_fmaxf(top, score[k] * factor(k) + __builtin_fmaxf(__builtin_amdgcn_logf(step(k)), -25.0f));
     top = __builtin_fminf(row_max(top), 0x1p120f);
-    const float to = __builtin_fmaxf(ref, top - (float)LARGEST - __builtin_fabsf(top) * 0x1p-22f), f = __builtin_amdgcn_exp2f(ref - to);
+    const float to = __builtin_fmaxf(ref, top - largest - __builtin_fabsf(top) * 0x1p-22f), f = __builtin_amdgcn_exp2f(ref - to);
     ref = to;
     return f;
 }
@@ -674,7 +683,7 @@ __device__ __forceinline__ void few_rows(const DEV& p, unsigned char* smem, int 
             auto by = [&](int) { return unit_of(p, factor[0]); };
             auto step = [&](int k) { return (float)step_bits(vp[k]); };
             if (weigh<N, false>(s, by, step, ref[0], prod, sum)) {
-                const float f = raise_reference<N, 7>(s, by, step, ref[0], [](float top) { return across_groups(top, fmax_op); });
+                const float f = raise_reference<N>(s, by, step, ref[0], 7.0f, [](float top) { return across_groups(top, fmax_op); });
                 total[0] *= f;
                 zeros[0] *= f;
 #pragma unroll
@@ -743,7 +752,7 @@ __device__ __forceinline__ void few_rows(const DEV& p, unsigned char* smem, int 
 #pragma unroll
                 for (int k = 0; k < 8; ++k) s8[k] = sc[n][k >> 2][k & 3];
                 if (weigh<8, false>(s8, by, step, ref[n], prod, sum)) {
-                    const float f = raise_reference<8, 7>(s8, by, step, ref[n], [](float top) { return across_groups(top, fmax_op); });
+                    const float f = raise_reference<8>(s8, by, step, ref[n], 7.0f, [](float top) { return across_groups(top, fmax_op); });
                     total[n] *= f;
                     zeros[n] *= f;
 #pragma unroll
@@ -1367,7 +1376,7 @@ __global__ __launch_bounds__(64 * NW, 2) void shared_attention_kernel(DEV p) {
         auto raise = [&](const f32x16& sc, const float (&fk)[16], const float (&vs)[16], float (&prod)[16], float& sum) {
             auto by = [&](int k) { return factor_of(fk, k); };
             auto step = [&](int k) { return vs[k]; };
-            const float f = raise_reference<16, kScored<DEV> ? 2 : 7>(sc, by, step, ref, [](float top) { return __builtin_fmaxf(top, __shfl_xor(top, 32)); });
+            const float f = raise_reference<16>(sc, by, step, ref, largest_of(p, span), [](float top) { return __builtin_fmaxf(top, __shfl_xor(top, 32)); });
             total *= f;
 #pragma unroll
             for (int dt = 0; dt < 4; ++dt)
