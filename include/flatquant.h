@@ -383,6 +383,8 @@ fq_status flatquant_head_rope(const void* q, int64_t q_stride, int Hq, const voi
  * for a row at position p.  cap 0 is none, slopes NULL none; with neither and no prefix it is that call, or flatquant_cache_tree_attention.
  *   slopes   fp32 [Hq], finite, 4-byte aligned.
  *   prefix   i32 [B], 4-byte aligned, or NULL: a row of sequence b also sees every token before prefix[b], those behind it among them, whatever the window.
+ *            With a prefix the launch is chosen for max_length tokens also beside a window; a program whose prefixes are short says less there (window and longest prefix together:
+ *            it is a hint, here and for the workspace).
  *   visible  u64 [T] or NULL: the masks of flatquant_cache_tree_attention; window and sinks 0, slopes and prefix NULL then.
  * With any of them a row whose queries are not all finite gets NaN if it sees a token.  Everything else, the workspace and what a row that sees nothing or no number gets,
  * as for the other two.

@@ -458,12 +458,9 @@ static fq_status cache_attention(const fq_kv_cache* cache, const fq_kv_batch* ba
     if (empty) return FQ_OK;
     if (!q || !out || (tree && !visible)) return FQ_INVALID_ARG;
     const int64_t max_rows = batch->max_rows < batch->T ? batch->max_rows : batch->T;      // hints: any number is fine
-    fq::AttnPlan plan = fq::attention_plan(batch->B, batch->T, cache->H, Hq, max_rows, batch->max_length, batch->max_length);
-    if (workspace_bytes < plan.workspace || (plan.workspace > 0 && !workspace)) return FQ_INVALID_ARG;
-    if (window > 0) {   // steps of 32 tokens around a tile's windows, and the first tokens
-        const fq::AttnPlan fewer = fq::attention_plan(batch->B, batch->T, cache->H, Hq, max_rows, batch->max_length, (int64_t)window + sinks + max_rows + 64);
-        if (fewer.workspace <= plan.workspace) plan = fewer;
-    }
+    const fq::AttnPlan plan = fq::attention_plan_window(batch->B, batch->T, cache->H, Hq, max_rows, batch->max_length, window, sinks, scores && scores->prefix);
+    const int64_t need = window <= 0 ? plan.workspace : fq::attention_plan(batch->B, batch->T, cache->H, Hq, max_rows, batch->max_length, batch->max_length).workspace;
+    if (workspace_bytes < need || (need > 0 && !workspace)) return FQ_INVALID_ARG;
     auto bad = [](const void* p, int a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; };
     if (bad(q, 16) || bad(out, 16) || (q_stride & 7) || (out_stride & 7) || bad(workspace, 16) || bad(visible, 8)) return FQ_MISALIGNED;
     const int64_t qbytes = ((batch->T - 1) * q_stride + row) * 2, obytes = ((batch->T - 1) * out_stride + row) * 2;

@@ -393,8 +393,20 @@ __device__ __forceinline__ float largest_of(const DEV& p, const Span& span) {
     if constexpr (kScored<DEV>) return p.bend && span.steps <= kLowReferenceSteps ? 2.0f : 7.0f;
     return 7.0f;
 }
-__device__ __forceinline__ int splits_used(const AttnDev& p, int steps) {
-    const int per = p.chunk / ATT_STEP, used = (steps + per - 1) / per;
+// Steps of a split: the plan's, or with other scores as many as all splits need to go through a span that is longer than the plan knows (a prefix beside a window: the host
+// plans for splits of 256 tokens).
+template <typename DEV>
+__device__ __forceinline__ int steps_of_split(const DEV& p, int steps) {
+    const int per = p.chunk / ATT_STEP;
+    if constexpr (kScored<DEV>) {
+        const int even = ((steps + p.splits - 1) / p.splits + 3) & ~3;
+        return even > per ? even : per;
+    }
+    return per;
+}
+template <typename DEV>
+__device__ __forceinline__ int splits_used(const DEV& p, int steps) {
+    const int per = steps_of_split(p, steps), used = (steps + per - 1) / per;
     return used < 1 ? 1 : used < p.splits ? used : p.splits;
 }
 // Rows of a sequence, cut to the row tensors.
@@ -1160,7 +1172,7 @@ __global__ __launch_bounds__(64 * NW, 2) void shared_attention_kernel(DEV p) {
         const Span span = span_of(p, seq.length, before + row0 / p.G, before + (row_end - 1) / p.G, prefix);
         const int used = splits_used(p, span.steps);
         if ((int)blockIdx.z >= used) continue;
-        const int per = p.chunk / ATT_STEP;
+        const int per = steps_of_split(p, span.steps);
         const int x_begin = (int)blockIdx.z * per;
         const int x_end = (int)blockIdx.z == p.splits - 1 ? span.steps : min(span.steps, x_begin + per);
 

@@ -221,6 +221,7 @@ struct AttnPlan {
     int64_t workspace;        // bytes
 };
 AttnPlan attention_plan(int64_t B, int64_t T, int H, int Hq, int64_t max_rows, int64_t length, int64_t seen);
+AttnPlan attention_plan_window(int64_t B, int64_t T, int H, int Hq, int64_t max_rows, int64_t length, int window, int sinks, bool prefix);
 hipError_t attention_launch(const CacheDev& c, const AttnArgs& a, const AttnPlan& plan, hipStream_t stream);
 struct ScoreArgs {
     float cap;                // 0: none
