@@ -612,16 +612,34 @@ fq_status fq_inverse_transpose(const void* P, int n, void* out, double* max_resi
     return FQ_OK;
 }
 
+namespace {
+// Digits i + 1 .. i + 64 behind the binary point of 1 / (2 pi); those before it are zero.  (Doubles are whole numbers times 2^971 at most: 1163 digits
+// are looked at.)
+uint64_t turn_digits(int i) {
+    static const uint64_t digits[19] = {
+        0x28be60db9391054au, 0x7f09d5f47d4d3770u, 0x36d8a5664f10e410u, 0x7f9458eaf7aef158u, 0x6dc91b8e909374b8u, 0x01924bba82746487u, 0x3f877ac72c4a69cfu,
+        0xba208d7d4baed121u, 0x3a671c09ad17df90u, 0x4e64758e60d4ce7du, 0x272117e2ef7e4a0eu, 0xc7fe25fff7816603u, 0xfbcbc462d6829b47u, 0xdb4d9fb3c9f2c26du,
+        0xd3d18fd9a797fa8bu, 0x5d49eeb1faf97c5eu, 0xcf41ce7de294a4bau, 0x9afed7ec47e35742u, 0x1580cc11bf1edaeau};
+    if (i <= -64) return 0;
+    if (i < 0) return digits[0] >> -i;
+    const int k = i / 64, s = i % 64;
+    return s == 0 ? digits[k] : digits[k] << s | digits[k + 1] >> (64 - s);
+}
+}  // namespace
+
 fq_status fq_rope_turns(const double* frequencies, int n, uint64_t* turns) {
     if (!frequencies || !turns || n < 0) return FQ_INVALID_ARG;
     for (int i = 0; i < n; ++i)
         if (!std::isfinite(frequencies[i])) return FQ_INVALID_ARG;
     for (int i = 0; i < n; ++i) {
-        const long double pi2 = 6.283185307179586476925286766559005768L;
-        long double turn = fmodl((long double)frequencies[i], pi2) / pi2;      // (64 bits of fraction)
-        if (turn < 0) turn += 1.0L;
-        const long double whole = rintl(turn * 0x1p64L);
-        turns[i] = whole >= 0x1p64L ? 0 : (uint64_t)whole;
+        // m 2^e / (2 pi) 2^64 modulo 2^64, in whole numbers: digits before the (e + 1)th make whole turns, those behind the (e + 192)th less than 2^-75 of a unit
+        int e;
+        const uint64_t m = (uint64_t)std::ldexp(std::frexp(std::fabs(frequencies[i]), &e), 53);
+        e -= 53;
+        typedef unsigned __int128 wide;
+        const wide low = (wide)m * turn_digits(e + 64) + ((wide)m * turn_digits(e + 128) >> 64);
+        const uint64_t nearest = m * turn_digits(e) + (uint64_t)(low >> 64) + ((uint64_t)low >> 63);
+        turns[i] = std::signbit(frequencies[i]) ? 0 - nearest : nearest;
     }
     return FQ_OK;
 }
