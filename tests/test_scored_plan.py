@@ -39,7 +39,7 @@ def test_a_prefix_is_planned_for(B, rows, length, window, sinks):
 @pytest.mark.parametrize("rows,lengths,prefix", [([1, 1], [20000, 9000], [15000, 3]), ([5, 2], [16000, 12000], [9999, 12000]), ([64], [20000], [15001]), ([64, 33], [9000, 20000], [0, 17000]),
                                                  ([300, 1], [6000, 12000], [5600, 11000])])
 def test_long_prefixes_beside_short_windows(rows, lengths, prefix, hint):
-    from cache_util import Batch
+    from cache_util import D, Batch
     from oracle import step_oracle as so
     from test_gpu_scored import expect, run_scored
     print(f"[case] {rows} of {lengths}, prefixes {prefix}, hint {hint}", flush=True)
