@@ -292,7 +292,7 @@ fq_status flatquant_cache_read(const fq_kv_cache* cache, const fq_kv_batch* batc
  * k_j and v_j the de-quantized rows of key/value head h / (Hq / H).  A row at position p sees token j of its sequence if j <= p and, with a
  * window (window > 0), j > p - window or j < sinks: the last `window` tokens and the first `sinks`.  window == 0 is no window, and sinks
  * is then not looked at.  A row that sees nothing gets zeros.  What lies in places that a row does not see, whatever it is, does not change it.
- * A row that sees a group whose step is an infinity or a NaN gets NaN.
+ * A row that sees a group whose step is an infinity, as flatquant_cache_write leaves it (zero codes), or a NaN gets NaN.
  * Scores, maxima and sums are fp32; the weights (times the value's step) are rounded to fp16 for the matrix instructions.
  *   q, out  fp16 [T, Hq, 128], rows q_stride / out_stride halves apart (multiples of 8, >= 128 Hq), 16-byte aligned, not overlapping.
  *   Hq      a multiple of H.
@@ -324,7 +324,8 @@ int64_t fq_cache_attention_workspace(const fq_kv_cache* cache, const fq_kv_batch
  *
  * The ring of free pages (a HOST struct that holds device pointers, like the others):
  *   ring   i32 [capacity]: pages; the free ones are entries state[0] .. state[1] - 1, each modulo the capacity.  At the start a program puts all of its pages
- *          in (capacity = pages, ring[i] = i, state = {0, pages}).
+ *          in (capacity = pages, ring[i] = i, state = {0, pages}).  The capacity has to be as many as the pages that go round, as what is given back beyond it takes the
+ *          place of free ones.
  *   state  i64 [2]: pages that have been taken from the ring, and that have been put into it, since the start
  *   next   i64 [3]: both behind the call, and how many pages were missing.  next may be state (of three numbers then): the next call goes on from there.
  */

@@ -9,7 +9,7 @@
 // last entry, and those between by bisection in LDS.
 //
 // Bound by latency, and on its one CU by the instructions of an entry: 64 decoding sequences 4.7 us (replayed; a launch, the sequences' loads, three running sums, rows), 512 in mixed states
-// (1150 pages taken, 15800 given back) 10.5 and 4 for their 18500 rows, 16 prompts of 65536 tokens (42900 pages, 686000 rows) 11.5 and 6.  Rows of more than a few
+// (1150 pages taken, 15800 given back) 11 and 4 for their 18500 rows, 16 prompts of 65536 tokens (42900 pages, 686000 rows) 12 and 6.  Rows of more than a few
 // thousand tokens are worked out by a second kernel on all CUs.
 #include "fq_internal.h"
 #include "fq_cache_device.h"

@@ -74,7 +74,7 @@ __device__ __forceinline__ float outcome(float x) {
     return x;
 }
 // Whether a span's steps are gone through from the last one on: with slopes, whose scores are highest there, so that references need not be raised at every step
-// (2048 rows at 8192 tokens 1110 -> 560 us).  A step behind the last one in this order has tokens below zero.
+// (2048 rows at 8192 tokens 1077 -> 586 us, 64 sequences of 4096 51.5 -> 47.0).  A step behind the last one in this order has tokens below zero.
 template <typename DEV>
 __device__ __forceinline__ bool backwards(const DEV& p) {
     if constexpr (kScored<DEV>) return p.slopes != nullptr;
@@ -384,8 +384,8 @@ __device__ __forceinline__ Span span_of(const AttnDev& p, int length, int pos_lo
     return s;
 }
 // The power of 2 of a row's largest product behind a raised reference (many rows).  With a cap scores spread over its range and cost more to weigh again: 2 instead of 7, so that
-// references are raised less often (2048 rows at 8192 tokens capped 742 -> 704 us, 64 at 1500 of 32 sequences 100 -> 92, trees of 13 49.5 -> 46.6; few rows, bound by memory, gain
-// nothing).  Products in fp16's subnormals then lose 2^-27 of the row's largest each, 2^-32 before: up to 2^14 tokens, that is 2^-13 in all, an eighth of what one product in fp16 is
+// references are raised less often (2048 rows at 8192 tokens capped 744 -> 715 us, 64 at 1500 of 32 sequences 100 -> 93, trees of 13 49.6 -> 46.8; few rows, bound by memory, gain
+// nothing).  Products in fp16's subnormals then lose 2^-27 of the row's largest each, 2^-32 before: up to 2^14 tokens, that is 2^-13 in all, a quarter of what one product in fp16 is
 // rounded by.
 constexpr int kLowReferenceSteps = (1 << 14) / ATT_STEP;
 template <typename DEV>
@@ -466,7 +466,7 @@ __device__ __forceinline__ float zero_sum(uint32_t pair, uint32_t params, float 
 // Scores of N tokens (all factors taken in; none infinite), capped and lowered; `distance(k)` is the token's position less the row's.  What is no number stays none.
 //   cap tanh(x / cap) = cap - 2 cap / (1 + e^(2 x / cap)): the exponent of 2 is what comes in, the cap alone is a constant of the row, which weights do not depend on, and the
 //   rest goes on in units of 2 cap: an exponential, an addition and a reciprocal.  It is off by 2^-21 of the cap, whatever the score.
-//   Caps beyond kLargeCap take the series of tanh below a quarter instead, so that the error is 2^-19 of the score there (2048 rows at 8192 tokens 670 us, so 930); up to
+//   Caps beyond kLargeCap take the series of tanh below a quarter instead, so that the error is 2^-19 of the score there (2048 rows at 8192 tokens 715 us, so 919); up to
 //   there it is below 2^-13, a quarter of what the weights are rounded by.
 constexpr float kLargeCap = 256.0f;        // base 2
 template <int N, typename Distance>

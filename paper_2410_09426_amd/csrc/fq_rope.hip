@@ -541,7 +541,7 @@ static hipError_t rope_matrix_launch(const RopeDev& d, const RopeDev& plain, hip
         return launch(kernel, dim3((unsigned)gx, matrices), dim3(RP_NT), lds, stream, d, plain);
     };
     static OccCache caches[2];
-    // (8192 rows of 32 + 8 heads: 52.7 us with the table, 58.0 without)
+    // (8192 rows of 32 + 8 heads, the queries through one matrix: 38.5 us with the table, 45.5 without)
     if (rows_of_groups(d) <= RM_ROWS) return many(rope_matrix_kernel<R, PAIRS, false>, RM_LDS_TABLE, caches[0]);
     return many(rope_matrix_kernel<R, PAIRS, true>, RM_LDS_DIRECT, caches[1]);
 }
