@@ -81,7 +81,7 @@ AttnPlan attention_plan(int64_t B, int64_t T, int H, int Hq, int64_t max_rows, i
 // The plan of a call: with a window, of the steps of 32 tokens around a tile's windows and the first tokens, if that needs no more workspace than the whole length, which the
 // caller has for it.  With a prefix beside it rows see any number of tokens, which the device alone knows: the plan of the whole length, whose balanced launch cuts what there is,
 // and whose splits the kernels lengthen from 256 tokens on.  us, 1024 tokens of window planned alone / as it is now: 1 sequence of 131072 tokens (8 x 4 heads) with a prefix of
-// 100000 592 / 37, 64 rows of it 6462 / 271; with one of 5 tokens 10.7 / 19.0 and 24.8 / 25.3; 16 sequences of 8192, prefixes of 6000 47.4 / 38.9, of 5 11.4 / 12.5.
+// 100000 592 / 37, 64 rows of it 6462 / 271; with one of 5 tokens 10.6 / 18.5 and 24.5 / 25.2; 16 sequences of 8192, prefixes of 6000 47.4 / 38.9, of 5 11.4 / 12.5.
 AttnPlan attention_plan_window(int64_t B, int64_t T, int H, int Hq, int64_t max_rows, int64_t length, int window, int sinks, bool prefix) {
     AttnPlan plan = attention_plan(B, T, H, Hq, max_rows, length, length);
     if (window <= 0) return plan;
